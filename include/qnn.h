@@ -21,8 +21,9 @@
  *    qnn_device_status().
  *  - Arguments are validated before anything is launched; a call that returns
  *    an error has enqueued nothing.  Nothing is thrown across the ABI.
- *  - Tensors are dense and contiguous; there are no stride arguments.  Input
- *    and output buffers must not overlap.
+ *  - Tensors are dense and contiguous; there are no stride arguments (the
+ *    language-model block operators at the end take row strides).  Input and
+ *    output buffers must not overlap.
  *  - Sub-byte storage: element e of a packed Q-bit stream sits in byte
  *    e / (8/Q) at bits [(e mod (8/Q)) * Q, +Q), the first element in the least
  *    significant bits.  Activations are unsigned, weights two's-complement.
@@ -355,6 +356,111 @@ const char *qnn_status_string(qnn_status s);
 
 /* Library version, for ABI checks: major * 10000 + minor * 100 + patch. */
 int32_t qnn_version(void);
+
+/* ------------------------------------------------------------------------
+ * Operators of a language model's block, for serving: the norms around a
+ * block, the routing to experts, the matrix product with a fused epilogue and
+ * the experts' products.  Activations are floating point here; weights may be
+ * packed INT-8/4/2 in the order above with one scale per output channel.
+ * These entry points take row strides (elements); columns are contiguous.
+ * ---------------------------------------------------------------------- */
+
+/* Element types of activations, residuals and parameters. */
+enum { QNN_F16 = 0, QNN_BF16 = 1, QNN_F32 = 2 };
+
+/* Norm of qnn_block_norm(). */
+enum {
+    QNN_NORM_RMS = 0,          /* v / sqrt(mean(v^2) + eps) */
+    QNN_NORM_LAYER = 1         /* (v - mean) / sqrt(var + eps), var the mean square of v - mean */
+};
+
+/*
+ * One call between two blocks.  x is [t][d] with row stride ldx; residual, r
+ * and h likewise.  Row i uses gate row i / (t / gates); the gate is
+ * [gates][d], contiguous.  d is at most 32768.
+ */
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_norm_desc) */
+    int32_t kind;              /* QNN_NORM_* of both norms */
+    int32_t dtype;             /* of x and h */
+    int32_t residual_dtype;    /* of residual and r: dtype or QNN_F32 */
+    int32_t param_dtype;       /* of gate, weights and biases: dtype or QNN_F32 */
+    int32_t post_norm;         /* 0: u = x; 1: u = N(x) * post_w + post_b */
+    int32_t gates;             /* rows of the gate; t must be a multiple of it (ignored without a gate) */
+    int32_t d;                 /* row length */
+    int64_t t;                 /* rows; may be 0 */
+    int64_t ldx, ldres, ldr, ldh;
+    float scale;               /* of the gated branch */
+    float eps;
+} qnn_norm_desc;
+
+/*
+ *   u = post_norm ? N(x) * post_w + post_b : x
+ *   r = residual + scale * gate * u
+ *   h = N(r) * pre_w + pre_b
+ *
+ * in 32 bits, each output rounded once (h from the unrounded r).  residual,
+ * gate, every weight and bias may be NULL (0, 1, 1, 0); r or h may be NULL
+ * (not written), not both.  r may be the residual itself and h may be x (same
+ * pointer and stride); no other overlap.  Pointers are aligned to their
+ * element; 16-byte aligned rows take the faster loads.
+ */
+qnn_status qnn_block_norm(const qnn_norm_desc *d, const void *x, const void *residual, const void *gate,
+                          const void *post_w, const void *post_b, const void *pre_w, const void *pre_b, void *r,
+                          void *h, void *stream);
+
+/* Scores and group scores of qnn_route_topk(). */
+enum { QNN_SCORE_SOFTMAX = 0, QNN_SCORE_SIGMOID = 1 };
+enum {
+    QNN_GROUP_MAX = 0,         /* a group counts as its best expert */
+    QNN_GROUP_TOP2 = 1         /* ... as the sum of its two best */
+};
+
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_route_desc) */
+    int32_t dtype;             /* of the logits */
+    int32_t experts;           /* 1 .. 1024 */
+    int32_t k;                 /* experts a token goes to: 1 .. 32, at most experts */
+    int32_t score;             /* QNN_SCORE_* */
+    int32_t groups;            /* experts are split evenly into this many groups: 1 .. 32, dividing experts */
+    int32_t top_groups;        /* groups a token may choose from: 1 .. groups */
+    int32_t group_score;       /* QNN_GROUP_* */
+    int32_t renormalise;       /* weights divided by their sum */
+    float scale;               /* of the weights */
+    int64_t t;                 /* tokens; may be 0 */
+    int64_t ld;                /* row stride of the logits */
+} qnn_route_desc;
+
+/*
+ * Chooses each token's k experts.  s = softmax or sigmoid of the logits; the
+ * choice goes by s + bias (bias float[experts], may be NULL), first among
+ * groups when top_groups < groups, in falling order, ties to the lowest index.
+ * The weights are s of the chosen experts without the bias, divided by their
+ * sum when renormalise is set, times scale.
+ *
+ * An expert whose logit is -inf or NaN cannot be chosen and counts for
+ * nothing; a token that runs out of experts gets id -1 and weight 0 for the
+ * rest (a row of -inf: all of them).
+ *
+ *   weights  device float[t][k]      ids  device int32[t][k]
+ */
+qnn_status qnn_route_topk(const qnn_route_desc *d, const void *logits, const float *bias, float *weights,
+                          int32_t *ids, void *stream);
+
+/*
+ * The slots (token * k + choice) sorted by expert, each expert's in rising
+ * order; ids outside [0, experts) are in no expert's list.
+ *
+ *   offsets   device int32[experts + 1]: expert e has places offsets[e] .. offsets[e+1]
+ *   order     device int32[slots]: the slot at each place, -1 after the last
+ *   position  device int32[slots]: the place of each slot, -1 for one left out
+ *
+ * slots below 2^31 - 2048, experts 1 .. 1024; workspace as
+ * qnn_expert_plan_workspace_size() says (256-byte aligned; NULL when 0).
+ */
+qnn_status qnn_expert_plan_workspace_size(int64_t slots, int32_t experts, size_t *bytes);
+qnn_status qnn_expert_plan(const int32_t *ids, int64_t slots, int32_t experts, int32_t *offsets, int32_t *order,
+                           int32_t *position, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

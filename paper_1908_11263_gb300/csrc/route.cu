@@ -1,0 +1,346 @@
+// qnn_route_topk() and qnn_expert_plan(): which experts a token goes to, and the tokens each expert gets.
+//
+// route_topk_kernel: one warp owns one token; lane l holds experts l, l + 32, ...  Scores are compared as 32-bit keys
+// whose unsigned order is the order of the floats, so the warp's best expert is one integer maximum over the lanes and
+// the lowest index among equals one integer minimum: ties go to the lowest index by construction.  The choice uses the
+// score itself (the logit where softmax scores carry no bias: the same order without rounding).
+//
+// expert plan: a stable counting sort of the slots (token * top + choice) by expert.  Ranks come from ordered per-warp
+// counts, never from the order in which atomics land, so the plan is the same on every run.
+#include "block_common.cuh"
+#include "block_internal.h"
+
+namespace qnn {
+namespace {
+
+constexpr int kRouteWarps = 8;
+constexpr uint32_t kFull = 0xffffffffu;
+
+struct RouteArgs {
+    const void *logits;
+    const float *bias;
+    float *weights;
+    int32_t *ids;
+    int64_t t, ld;
+    int e, k, sigmoid, groups, top_groups, two, renorm;
+    int group_size;
+    uint32_t group_magic;  // expert / group_size = (expert * magic) >> 20 for experts below 1024
+    float scale;
+};
+
+// Key whose unsigned order is the float order; 0 for an expert that cannot be chosen (-inf or NaN).
+__device__ __forceinline__ uint32_t order_key(float v)
+{
+    const uint32_t b = __float_as_uint(v + 0.f);  // -0 becomes +0
+    if (!(v > -INFINITY)) return 0u;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+__device__ __forceinline__ float exp_from(float v, float top) { return top == INFINITY ? (v == INFINITY ? 1.f : 0.f) : expf(v - top); }
+
+__device__ __forceinline__ float score_of(float v, int sigmoid, float top)
+{
+    if (!(v > -INFINITY)) return 0.f;
+    // the sum rounded by itself, so that a score is the same wherever it is computed
+    return sigmoid ? 1.f / __fadd_rn(1.f, expf(-v)) : exp_from(v, top);
+}
+
+template <typename T, int NV>
+__global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const RouteArgs a)
+{
+    extern __shared__ float sm_scores[];  // one row of group_size * groups scores a warp (grouped calls only)
+    const int lane = threadIdx.x & 31;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5);
+    if (token >= a.t) return;
+    const T *row = static_cast<const T *>(a.logits) + token * a.ld;
+
+    float x[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = i * 32 + lane;
+        x[i] = e < a.e ? to_f32<T>(row[e]) : -INFINITY;
+    }
+    float top = 0.f, total = 1.f;
+    if (!a.sigmoid) {
+        top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) top = fmaxf(top, x[i]);  // fmaxf drops NaN
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+        if (!a.renorm || a.bias) {
+            total = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) total += score_of(x[i], 0, top);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
+            total = total > 0.f ? total : 1.f;
+        }
+    }
+    // what the choice goes by
+    uint32_t key[NV];
+    float *sc = sm_scores + (threadIdx.x >> 5) * a.e;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = i * 32 + lane;
+        float c = x[i];
+        if (c > -INFINITY && (a.sigmoid || a.bias)) {
+            c = score_of(x[i], a.sigmoid, top);
+            if (!a.sigmoid) c /= total;
+            if (a.bias) c += a.bias[e];
+        }
+        key[i] = order_key(c);
+        if (a.groups > 1 && e < a.e) {
+            if (!a.sigmoid && !a.bias && a.two && key[i]) c = score_of(x[i], 0, top);  // sums need the scores themselves
+            sc[e] = key[i] ? c : -INFINITY;
+        }
+    }
+    if (a.groups > 1) {
+        __syncwarp();
+        // lane g scores group g: its best expert, or the sum of its two best
+        float best = -INFINITY;
+        if (lane < a.groups) {
+            float second = -INFINITY;
+            int j = lane % a.group_size;  // a start of its own a lane: fewer bank conflicts
+            for (int n = 0; n < a.group_size; ++n) {
+                const float v = sc[lane * a.group_size + j];
+                second = fmaxf(second, fminf(best, v));
+                best = fmaxf(best, v);
+                j = j + 1 == a.group_size ? 0 : j + 1;
+            }
+            if (a.two && second > -INFINITY) best += second;
+        }
+        const uint32_t mine = lane < a.groups ? order_key(best) : 0u;
+        int rank = 0;
+        for (int g = 0; g < a.groups; ++g) {
+            const uint32_t o = __shfl_sync(kFull, mine, g);
+            rank += o > mine || (o == mine && g < lane);
+        }
+        const uint32_t keep = __ballot_sync(kFull, lane < a.groups && rank < a.top_groups);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t e = i * 32 + lane;
+            const uint32_t g = (e * a.group_magic) >> 20;
+            if (e >= static_cast<uint32_t>(a.e) || !((keep >> (g & 31)) & 1)) key[i] = 0u;
+        }
+    }
+    // the k best, one warp maximum each; lane j keeps choice j
+    int id = -1;
+    for (int j = 0; j < a.k; ++j) {
+        uint32_t best = key[0];
+        int at = 0;
+#pragma unroll
+        for (int i = 1; i < NV; ++i)
+            if (key[i] > best) {
+                best = key[i];
+                at = i;
+            }
+        const uint32_t top_key = __reduce_max_sync(kFull, best);
+        if (top_key == 0u) break;
+        const uint32_t e = __reduce_min_sync(kFull, best == top_key ? static_cast<uint32_t>(at * 32 + lane) : kFull);
+        if (lane == j) id = static_cast<int>(e);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (e == static_cast<uint32_t>(i * 32 + lane)) key[i] = 0u;
+    }
+    float w = 0.f;
+    if (id >= 0) {
+        w = score_of(to_f32<T>(row[id]), a.sigmoid, top);
+        if (!a.sigmoid && !a.renorm) w /= total;
+    }
+    if (a.renorm) {
+        float s = w;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+        w = s > 0.f ? w / s : w;
+    }
+    if (lane < a.k) {
+        a.weights[token * a.k + lane] = w * a.scale;
+        a.ids[token * a.k + lane] = id;
+    }
+}
+
+// ---------------------------------------------------------------- plan
+
+constexpr int kPlanThreads = 512;
+constexpr int kPlanWarps = kPlanThreads / 32;
+constexpr int kPlanChunk = 2048;  // slots a block
+
+int plan_blocks(int64_t slots, int64_t *chunk)
+{
+    int64_t c = kPlanChunk;
+    while ((slots + c - 1) / c > 128) c *= 2;
+    *chunk = c;
+    return static_cast<int>(slots ? (slots + c - 1) / c : 1);
+}
+
+__device__ __forceinline__ int expert_of(const int32_t *ids, int64_t slot, int64_t end, int experts)
+{
+    if (slot >= end) return -1;
+    const int e = ids[slot];
+    return e >= 0 && e < experts ? e : -1;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const int32_t *ids, int64_t slots, int64_t chunk,
+                                                                  int experts, int32_t *counts)
+{
+    extern __shared__ int32_t sm_plan[];
+    for (int e = threadIdx.x; e < experts; e += kPlanThreads) sm_plan[e] = 0;
+    __syncthreads();
+    const int64_t begin = blockIdx.x * chunk, end = begin + chunk < slots ? begin + chunk : slots;
+    for (int64_t s = begin + threadIdx.x; s < end; s += kPlanThreads) {
+        const int e = expert_of(ids, s, end, experts);
+        if (e >= 0) atomicAdd(&sm_plan[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < experts; e += kPlanThreads) counts[static_cast<int64_t>(blockIdx.x) * experts + e] = sm_plan[e];
+}
+
+// counts: per-block counts of plan_count_kernel, or NULL when one block holds all slots.
+__global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t *ids, int64_t slots, int64_t chunk,
+                                                                  int experts, const int32_t *counts, int32_t *offsets,
+                                                                  int32_t *order, int32_t *position)
+{
+    extern __shared__ int32_t sm_plan[];  // [warps][experts] counts, then [experts] starts
+    __shared__ int32_t part[32];
+    int32_t *start = sm_plan + kPlanWarps * experts;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < kPlanWarps * experts; i += kPlanThreads) sm_plan[i] = 0;
+    __syncthreads();
+    const int64_t begin = blockIdx.x * chunk, end = begin + chunk < slots ? begin + chunk : slots;
+    const int64_t span = chunk / kPlanWarps;  // a multiple of 32
+    const int64_t wb = begin + warp * span, we = wb + span < end ? wb + span : end;
+    int32_t *mine = sm_plan + warp * experts;
+    for (int64_t s = wb + lane; s < we; s += 32) {
+        const int e = expert_of(ids, s, we, experts);
+        if (e >= 0) atomicAdd(&mine[e], 1);
+    }
+    __syncthreads();
+    // exclusive counts over the warps; totals over all blocks, and over the blocks before this one
+    int32_t running = 0;
+    for (int base = 0; base < experts; base += kPlanThreads) {
+        const int e = base + threadIdx.x;
+        int32_t total = 0, before = 0;
+        if (e < experts) {
+            int32_t own = 0;
+            for (int w = 0; w < kPlanWarps; ++w) {
+                const int32_t c = sm_plan[w * experts + e];
+                sm_plan[w * experts + e] = own;
+                own += c;
+            }
+            total = own;
+            if (counts) {
+                total = 0;
+                for (int b = 0; b < static_cast<int>(gridDim.x); ++b) {
+                    const int32_t c = counts[static_cast<int64_t>(b) * experts + e];
+                    before += b < static_cast<int>(blockIdx.x) ? c : 0;
+                    total += c;
+                }
+            }
+        }
+        // exclusive scan of the totals over the experts
+        int32_t inc = total;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t v = __shfl_up_sync(kFull, inc, o);
+            if (lane >= o) inc += v;
+        }
+        if (lane == 31) part[warp] = inc;
+        __syncthreads();
+        int32_t lower = running, all = running;
+        for (int w = 0; w < kPlanWarps; ++w) {
+            lower += w < warp ? part[w] : 0;
+            all += part[w];
+        }
+        if (e < experts) {
+            start[e] = lower + inc - total + before;
+            if (blockIdx.x == 0) offsets[e] = lower + inc - total;
+        }
+        running = all;
+        __syncthreads();
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) offsets[experts] = running;
+    // ranks: 32 slots at a time in order, equal experts by lane
+    for (int64_t s0 = wb; s0 < we; s0 += 32) {
+        const int64_t s = s0 + lane;
+        const int e = expert_of(ids, s, we, experts);
+        const uint32_t same = __match_any_sync(kFull, e);
+        const int below = __popc(same & ((1u << lane) - 1u));
+        const int32_t base = e >= 0 ? mine[e] : 0;
+        __syncwarp();
+        if (e >= 0 && below == 0) mine[e] = base + __popc(same);
+        __syncwarp();
+        if (s < we) {
+            const int32_t at = e >= 0 ? start[e] + base + below : -1;
+            position[s] = at;
+            if (at >= 0) order[at] = static_cast<int32_t>(s);
+        }
+    }
+    // the places after the last planned slot
+    const int64_t from = begin > running ? begin : running;
+    for (int64_t s = from + threadIdx.x; s < end; s += kPlanThreads) order[s] = -1;
+}
+
+template <typename T>
+cudaError_t launch_route_type(const RouteArgs &a, cudaStream_t stream)
+{
+    const unsigned grid = static_cast<unsigned>((a.t + kRouteWarps - 1) / kRouteWarps);
+    const int threads = kRouteWarps * 32;
+    const size_t smem = a.groups > 1 ? sizeof(float) * kRouteWarps * a.e : 0;  // at most 32 KB
+    const int nv = (a.e + 31) / 32;
+    if (nv <= 1) route_topk_kernel<T, 1><<<grid, threads, smem, stream>>>(a);
+    else if (nv <= 2) route_topk_kernel<T, 2><<<grid, threads, smem, stream>>>(a);
+    else if (nv <= 4) route_topk_kernel<T, 4><<<grid, threads, smem, stream>>>(a);
+    else if (nv <= 8) route_topk_kernel<T, 8><<<grid, threads, smem, stream>>>(a);
+    else if (nv <= 16) route_topk_kernel<T, 16><<<grid, threads, smem, stream>>>(a);
+    else route_topk_kernel<T, 32><<<grid, threads, smem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_route_topk(const qnn_route_desc &d, const void *logits, const float *bias, float *weights,
+                              int32_t *ids, cudaStream_t stream)
+{
+    if (d.t == 0) return cudaSuccess;
+    RouteArgs a;
+    a.logits = logits; a.bias = bias; a.weights = weights; a.ids = ids;
+    a.t = d.t; a.ld = d.ld; a.e = d.experts; a.k = d.k; a.sigmoid = d.score == QNN_SCORE_SIGMOID;
+    // limiting the choice to all groups limits nothing
+    a.groups = d.top_groups < d.groups ? d.groups : 1;
+    a.top_groups = d.top_groups; a.two = d.group_score == QNN_GROUP_TOP2; a.renorm = d.renormalise; a.scale = d.scale;
+    a.group_size = d.experts / d.groups;
+    a.group_magic = ((1u << 20) + a.group_size - 1) / a.group_size;
+    if (d.dtype == QNN_F32) return launch_route_type<float>(a, stream);
+    if (d.dtype == QNN_F16) return launch_route_type<__half>(a, stream);
+    return launch_route_type<__nv_bfloat16>(a, stream);
+}
+
+size_t expert_plan_workspace(int64_t slots, int experts)
+{
+    int64_t chunk;
+    const int nb = plan_blocks(slots, &chunk);
+    return nb > 1 ? static_cast<size_t>(nb) * experts * sizeof(int32_t) : 0;
+}
+
+cudaError_t launch_expert_plan(const int32_t *ids, int64_t slots, int experts, int32_t *offsets, int32_t *order,
+                               int32_t *position, void *workspace, cudaStream_t stream)
+{
+    int64_t chunk;
+    const int nb = plan_blocks(slots, &chunk);
+    int32_t *counts = nb > 1 ? static_cast<int32_t *>(workspace) : nullptr;
+    const size_t smem = sizeof(int32_t) * (kPlanWarps + 1) * experts;
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   static_cast<int>(smem));
+        if (e != cudaSuccess) return e;
+    }
+    if (counts) {
+        plan_count_kernel<<<nb, kPlanThreads, sizeof(int32_t) * experts, stream>>>(ids, slots, chunk, experts, counts);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    plan_place_kernel<<<nb, kPlanThreads, smem, stream>>>(ids, slots, chunk, experts, counts, offsets, order, position);
+    return cudaGetLastError();
+}
+
+}  // namespace qnn

@@ -27,7 +27,11 @@ ALGO_AUTO, ALGO_DIRECT, ALGO_TENSORCORE, ALGO_TC_WINDOW, ALGO_TC_GENERAL = 0, 1,
 EXPORTED = ("qconv_hwc_workspace_size", "qconv_hwc", "qconv_hwc_prepare", "qconv_hwc_run", "qconv_hwc_algo", "qlinear", "qmaxpool", "pack_subbyte",
             "unpack_subbyte", "qnn_device_status", "qnn_status_string", "qnn_version", "qconv_hwc_noalloc",
             "qnn_selftest_wait_timeout", "qconv_hwc_thresholds", "qconv_hwc_binary", "qconv_hwc_pool2", "qconv_hwc_pool2_run",
-            "qconv_hwc_mma_operand_bits", "qconv_hwc_tc_kernel")
+            "qconv_hwc_mma_operand_bits", "qconv_hwc_tc_kernel", "qnn_block_norm", "qnn_route_topk",
+            "qnn_expert_plan_workspace_size", "qnn_expert_plan")
+
+F16, BF16, F32 = 0, 1, 2  # QNN_F16, QNN_BF16, QNN_F32
+_DTYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
 
 
 class QnnError(RuntimeError):
@@ -39,6 +43,18 @@ class QnnError(RuntimeError):
 class ConvDesc(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in (
         "n", "h", "w", "c", "m", "kh", "kw", "stride_h", "stride_w", "pad_h", "pad_w", "bits", "shift", "algo")]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in (
+        "kind", "dtype", "residual_dtype", "param_dtype", "post_norm", "gates", "d")] + [(f, ctypes.c_int64) for f in (
+            "t", "ldx", "ldres", "ldr", "ldh")] + [("scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class RouteDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in (
+        "dtype", "experts", "k", "score", "groups", "top_groups", "group_score", "renormalise")] + [
+            ("scale", ctypes.c_float), ("t", ctypes.c_int64), ("ld", ctypes.c_int64)]
 
 
 _lock = threading.Lock()
@@ -95,6 +111,14 @@ def load(build_if_missing: bool = False):
         lib.pack_subbyte.restype = I32
         lib.unpack_subbyte.argtypes = [P, P, I64, I32, I32, P]
         lib.unpack_subbyte.restype = I32
+        lib.qnn_block_norm.argtypes = [ctypes.POINTER(NormDesc)] + [P] * 10
+        lib.qnn_block_norm.restype = I32
+        lib.qnn_route_topk.argtypes = [ctypes.POINTER(RouteDesc)] + [P] * 5
+        lib.qnn_route_topk.restype = I32
+        lib.qnn_expert_plan_workspace_size.argtypes = [I64, I32, ctypes.POINTER(SZ)]
+        lib.qnn_expert_plan_workspace_size.restype = I32
+        lib.qnn_expert_plan.argtypes = [P, I64, I32, P, P, P, P, SZ, P]
+        lib.qnn_expert_plan.restype = I32
         lib.qnn_selftest_wait_timeout.argtypes = [I64, P]
         lib.qnn_selftest_wait_timeout.restype = I32
         lib.qnn_device_status.argtypes = [P]
@@ -450,6 +474,153 @@ def unpack_subbyte(src, bits, signed, *, out=None, stream=None):
     st = load().unpack_subbyte(_ptr(src), _ptr(out), out.numel(), bits, int(bool(signed)), _stream(stream))
     _check(st, "unpack_subbyte")
     return out
+
+
+# ---------------------------------------------------------------- language-model block operators
+
+def _rows(t: torch.Tensor, dtype, name, shape=None, device=None):
+    """A CUDA matrix with contiguous columns and any row stride; returns (pointer, row stride)."""
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be a CUDA tensor" + ("" if device is None else f" on {device}"))
+    if t.dtype != dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must have shape {'[rows, columns]' if shape is None else tuple(shape)}, got {tuple(t.shape)}")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and ld < cols):
+        raise ValueError(f"{name} must have contiguous columns and rows that do not overlap")
+    return t.data_ptr(), ld
+
+
+def _param(t, dtype, name, shape, device):
+    """An optional contiguous parameter; returns its pointer or None."""
+    if t is None:
+        return None
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _float_dtype(t, name):
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float16, bfloat16 or float32, got {t.dtype}")
+    return code
+
+
+_NORM_KINDS = {"rms": 0, "layer": 1}
+
+
+def block_norm(x, residual=None, *, pre_weight=None, pre_bias=None, pre_norm=True, post_norm=False, post_weight=None,
+               post_bias=None, gate=None, scale=1.0, eps=1e-6, kind="rms", residual_out=None, out=None, stream=None):
+    """What stands between two blocks, in one pass (qnn_block_norm):
+
+        u = N(x) * post_weight + post_bias if post_norm else x
+        r = residual + scale * gate * u
+        h = N(r) * pre_weight + pre_bias
+
+    x [t, d]; residual [t, d] in x's dtype or float32; gate [d] or [gates, d] (t a multiple of gates, consecutive rows
+    share one); weights and biases [d].  Gate, weights and biases have x's dtype, or are all float32.  Rows may be
+    strided.  Returns (r, h) in the residual's and x's dtypes; with pre_norm=False only r is computed and h is None.
+    residual_out may be the residual, out may be x."""
+    code = _float_dtype(x, "x")
+    if kind not in _NORM_KINDS:
+        raise ValueError(f"kind must be 'rms' or 'layer', got {kind!r}")
+    px, ldx = _rows(x, x.dtype, "x")
+    dev, (t, d) = x.device, x.shape
+    rdtype, pres, ldres = x.dtype, None, d
+    if residual is not None:
+        pres, ldres = _rows(residual, (x.dtype, torch.float32), "residual", (t, d), dev)
+        rdtype = residual.dtype
+    elif residual_out is not None:
+        rdtype = residual_out.dtype
+        if rdtype not in (x.dtype, torch.float32):
+            raise TypeError(f"residual_out must have x's dtype or float32, got {rdtype}")
+    params = [p for p in (gate, post_weight, post_bias, pre_weight, pre_bias) if p is not None]
+    pdtype = params[0].dtype if params else x.dtype
+    if pdtype not in (x.dtype, torch.float32):
+        raise TypeError(f"gate, weights and biases must have x's dtype or float32, got {pdtype}")
+    gates = 1 if gate is None or gate.dim() == 1 else gate.shape[0]
+    if gate is not None and (gates == 0 or t % gates):
+        raise ValueError(f"{t} rows do not split evenly over {gates} gate rows")
+    pgate = _param(gate, pdtype, "gate", (d,) if gate is not None and gate.dim() == 1 else (gates, d), dev)
+    ppw, ppb = _param(post_weight, pdtype, "post_weight", (d,), dev), _param(post_bias, pdtype, "post_bias", (d,), dev)
+    pw, pb = _param(pre_weight, pdtype, "pre_weight", (d,), dev), _param(pre_bias, pdtype, "pre_bias", (d,), dev)
+    if residual_out is None:
+        residual_out = torch.empty((t, d), dtype=rdtype, device=dev)
+    pr, ldr = _rows(residual_out, rdtype, "residual_out", (t, d), dev)
+    ph, ldh = None, d
+    if pre_norm:
+        if out is None:
+            out = torch.empty((t, d), dtype=x.dtype, device=dev)
+        ph, ldh = _rows(out, x.dtype, "out", (t, d), dev)
+    else:
+        out = None
+    desc = NormDesc(ctypes.sizeof(NormDesc), _NORM_KINDS[kind], code, _DTYPES[rdtype], _DTYPES[pdtype], int(bool(post_norm)),
+                    gates, d, t, ldx, ldres, ldr, ldh, scale, eps)
+    st = load().qnn_block_norm(ctypes.byref(desc), px, pres, pgate, ppw, ppb, pw, pb, pr, ph, _stream(stream))
+    _check(st, "qnn_block_norm")
+    return residual_out, out
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+_GROUP_SCORES = {"max": 0, "top2": 1}
+
+
+def route_topk(logits, k, *, score="softmax", bias=None, groups=1, top_groups=None, group_score="max", renormalise=True,
+               scale=1.0, stream=None):
+    """Each token's k experts and their weights (qnn_route_topk): logits [t, experts]; returns (weights float32 [t, k],
+    ids int32 [t, k]), best first, ties to the lowest index.  The choice goes by softmax or sigmoid scores plus `bias`
+    (float32 [experts]), first among `groups` when fewer than all are allowed; weights are the scores without the bias.
+    Experts at -inf or NaN are closed; a token with too few open ones gets id -1 and weight 0."""
+    code = _float_dtype(logits, "logits")
+    if score not in _SCORES or group_score not in _GROUP_SCORES:
+        raise ValueError(f"score must be 'softmax' or 'sigmoid' and group_score 'max' or 'top2', got {score!r}, {group_score!r}")
+    p, ld = _rows(logits, logits.dtype, "logits")
+    dev, (t, e) = logits.device, logits.shape
+    pbias = _param(bias, torch.float32, "bias", (e,), dev)
+    weights = torch.empty((t, max(k, 0)), dtype=torch.float32, device=dev)
+    ids = torch.empty((t, max(k, 0)), dtype=torch.int32, device=dev)
+    desc = RouteDesc(ctypes.sizeof(RouteDesc), code, e, k, _SCORES[score], groups, groups if top_groups is None else top_groups,
+                     _GROUP_SCORES[group_score], int(bool(renormalise)), scale, t, ld)
+    st = load().qnn_route_topk(ctypes.byref(desc), p, pbias, weights.data_ptr(), ids.data_ptr(), _stream(stream))
+    _check(st, "qnn_route_topk")
+    return weights, ids
+
+
+class ExpertPlan:
+    """Which slots (token * top + choice) each expert serves (qnn_expert_plan): `offsets` int32 [experts + 1], `order`
+    int32 [slots] (the slot at each place, -1 after the last) and `position` int32 [tokens, top] (the place of each
+    slot, -1 for one that goes to no expert)."""
+
+    __slots__ = ("tokens", "top", "experts", "offsets", "order", "position")
+
+    def __init__(self, tokens, top, experts, offsets, order, position):
+        self.tokens, self.top, self.experts = tokens, top, experts
+        self.offsets, self.order, self.position = offsets, order, position
+
+
+def expert_plan(ids, experts, *, stream=None) -> ExpertPlan:
+    """The plan of ids int32 [tokens, top] over `experts`; ids outside [0, experts) go to no expert."""
+    _dev(ids, torch.int32, "ids")
+    if ids.dim() != 2:
+        raise ValueError(f"ids must have shape [tokens, top], got {tuple(ids.shape)}")
+    dev, slots = ids.device, ids.numel()
+    lib, need = load(), ctypes.c_size_t(0)
+    _check(lib.qnn_expert_plan_workspace_size(slots, experts, ctypes.byref(need)), "qnn_expert_plan_workspace_size")
+    ws = _workspace(need.value, dev, stream)
+    offsets = torch.empty(experts + 1, dtype=torch.int32, device=dev)
+    order = torch.empty(slots, dtype=torch.int32, device=dev)
+    position = torch.empty(ids.shape, dtype=torch.int32, device=dev)
+    st = lib.qnn_expert_plan(ids.data_ptr(), slots, experts, offsets.data_ptr(), order.data_ptr(), position.data_ptr(),
+                             _ptr(ws), need.value, _stream(stream))
+    _check(st, "qnn_expert_plan")
+    return ExpertPlan(ids.shape[0], ids.shape[1], experts, offsets, order, position)
 
 
 def selftest_wait_timeout(limit_cycles: int, stream=None):
