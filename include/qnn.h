@@ -462,6 +462,79 @@ qnn_status qnn_expert_plan_workspace_size(int64_t slots, int32_t experts, size_t
 qnn_status qnn_expert_plan(const int32_t *ids, int64_t slots, int32_t experts, int32_t *offsets, int32_t *order,
                            int32_t *position, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Activation of the matrix products. */
+enum {
+    QNN_ACT_NONE = 0,
+    QNN_ACT_RELU = 1,
+    QNN_ACT_SILU = 2,          /* v / (1 + exp(-v)) */
+    QNN_ACT_GELU = 3,          /* v * Phi(v), with erf */
+    QNN_ACT_GELU_TANH = 4      /* its tanh form */
+};
+
+/*
+ * A weight matrix [rows][k], or one for each of `experts` experts; rows is m,
+ * or 2 m for a gated product: m gate rows, then m up rows.  Weights are 16-bit
+ * floats of type `dtype`, or packed signed 8/4/2-bit codes in the sub-byte
+ * order above with one float scale a row.
+ */
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_matmul_desc) */
+    int32_t experts;           /* matrices: 1 for qnn_matmul_run(), 1 .. 1024 for the experts' products */
+    int32_t m;                 /* output channels */
+    int32_t k;                 /* input channels, a multiple of 8/bits for packed weights */
+    int32_t bits;              /* 16, 8, 4 or 2 */
+    int32_t dtype;             /* QNN_F16 or QNN_BF16: x, residual, outputs and 16-bit weights */
+    int32_t gated;             /* 1: y = act(gate) * up */
+    int32_t act;               /* QNN_ACT_* */
+} qnn_matmul_desc;
+
+/*
+ * Lays the weights out once, as the kernels read them, with scale and bias
+ * beside them; the caller's buffers may be freed afterwards.  The image needs
+ * qnn_matmul_image_size() bytes, 256-byte aligned, and may be used by any
+ * number of concurrent calls.
+ *
+ *   w      device [experts][rows][k], 16-bit floats or packed codes (aligned to their element)
+ *   scale  device float[experts][rows] or NULL (1); bias likewise or NULL (0)
+ */
+qnn_status qnn_matmul_image_size(const qnn_matmul_desc *d, size_t *bytes);
+qnn_status qnn_matmul_prepare(const qnn_matmul_desc *d, const void *w, const float *scale, const float *bias,
+                              void *image, size_t image_bytes, void *stream);
+
+/*
+ *   v = scale * (x w^T) + bias        (codes are multiplied as they are; 32-bit accumulation)
+ *   y = residual + act(v)             or  residual + act(v_gate) * v_up
+ *
+ * rounded once.  x [t][k], residual [t][m] or NULL, y [t][m] of type dtype, or
+ * float when out_f32 is set.  y may be the residual itself (same pointer,
+ * stride and type), no other overlap.  Workspace (256-byte aligned) as
+ * qnn_matmul_workspace_size() says for the same d, t, x and ldx.
+ */
+qnn_status qnn_matmul_workspace_size(const qnn_matmul_desc *d, int64_t t, const void *x, int64_t ldx, size_t *bytes);
+qnn_status qnn_matmul_run(const qnn_matmul_desc *d, const void *image, size_t image_bytes, int64_t t, const void *x,
+                          int64_t ldx, const void *residual, int64_t ldres, void *y, int64_t ldy, int32_t out_f32,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The experts' products over a plan of qnn_expert_plan() (tokens * top slots).
+ *
+ * qnn_experts_dispatch: row p of y is the product of x[order[p] / top] with
+ *   the weights of the expert that place p belongs to; x [tokens][k],
+ *   y [tokens * top][m].  Rows after the last place are zero.
+ * qnn_experts_combine: x has a row per place, x [tokens * top][k];
+ *   y[t] = residual[t] + sum_j weights[t][j] * product(position[t][j]), the sum in 32 bits in the order of j;
+ *   choices without a place add nothing.  weights float[tokens][top].
+ */
+qnn_status qnn_experts_workspace_size(const qnn_matmul_desc *d, int64_t tokens, int32_t top, int32_t combine,
+                                      const void *x, int64_t ldx, size_t *bytes);
+qnn_status qnn_experts_dispatch(const qnn_matmul_desc *d, const void *image, size_t image_bytes, int64_t tokens,
+                                int32_t top, const int32_t *offsets, const int32_t *order, const void *x, int64_t ldx,
+                                void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+qnn_status qnn_experts_combine(const qnn_matmul_desc *d, const void *image, size_t image_bytes, int64_t tokens,
+                               int32_t top, const int32_t *offsets, const int32_t *position, const float *weights,
+                               const void *x, int64_t ldx, const void *residual, int64_t ldres, void *y, int64_t ldy,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

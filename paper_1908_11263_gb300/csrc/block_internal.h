@@ -22,4 +22,14 @@ size_t expert_plan_workspace(int64_t slots, int experts);
 cudaError_t launch_expert_plan(const int32_t *ids, int64_t slots, int experts, int32_t *offsets, int32_t *order,
                                int32_t *position, void *workspace, cudaStream_t st);
 
+// ---- matrix products: weight image and the sum over a token's experts -- matmul_prep.cu
+struct MatmulArgs;
+cudaError_t launch_matmul_prep(const qnn_matmul_desc &d, const void *w, const float *scale, const float *bias,
+                               void *image, cudaStream_t st);
+cudaError_t launch_combine(int dtype, const float *z, int64_t ldz, const float *weights, const int32_t *position,
+                           int64_t tokens, int top, int m, const void *residual, int64_t ldres, void *y, int64_t ldy,
+                           cudaStream_t st);
+// ---- few rows: streamed weights -- matmul_stream.cu
+cudaError_t launch_matmul_stream(const MatmulArgs &a, int dtype, int bits, cudaStream_t st);
+
 }  // namespace qnn

@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "block_internal.h"
+#include "matmul.cuh"
 
 namespace qnn {
 namespace {
@@ -12,6 +13,50 @@ qnn_status from_cuda(cudaError_t e) { return e == cudaSuccess ? QNN_OK : QNN_ECU
 bool dtype_ok(int32_t t) { return t == QNN_F16 || t == QNN_BF16 || t == QNN_F32; }
 uintptr_t dtype_size(int32_t t) { return t == QNN_F32 ? 4 : 2; }
 bool flag_ok(int32_t v) { return v == 0 || v == 1; }
+
+qnn_status check_matmul(const qnn_matmul_desc *d)
+{
+    if (!d || d->struct_size != sizeof(qnn_matmul_desc)) return QNN_EINVAL;
+    if (d->experts <= 0 || d->m <= 0 || d->k <= 0 || !flag_ok(d->gated)) return QNN_EINVAL;
+    if (d->act < QNN_ACT_NONE || d->act > QNN_ACT_GELU_TANH || !dtype_ok(d->dtype)) return QNN_EINVAL;
+    if (d->dtype == QNN_F32 || (d->bits != 16 && d->bits != 8 && d->bits != 4 && d->bits != 2)) return QNN_EUNSUPPORTED;
+    if (d->experts > 1024 || d->m > (1 << 24) || d->k > (1 << 24)) return QNN_EUNSUPPORTED;
+    if (d->bits < 8 && d->k % (8 / d->bits)) return QNN_EUNSUPPORTED;
+    return QNN_OK;
+}
+
+constexpr int64_t kMaxRows = 1 << 20;  // rows of x in one call
+
+MatmulArgs base_args(const qnn_matmul_desc &d, const void *image, const void *x, int64_t ldx, void *y, int64_t ldy)
+{
+    const MatmulImage g = matmul_image(d.experts, d.m, d.k, d.bits, d.gated);
+    MatmulArgs a = {};
+    a.image = static_cast<const uint8_t *>(image);
+    a.params = reinterpret_cast<const float2 *>(a.image + g.param_off);
+    a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy;
+    a.m = d.m; a.k = d.k; a.kb = g.kb; a.mb = g.mb; a.experts = d.experts; a.top = 1;
+    a.act = d.act; a.gated = d.gated;
+    a.x_vec = aligned(x, 16) && ldx % 8 == 0;
+    return a;
+}
+
+qnn_status check_image(const qnn_matmul_desc &d, const void *image, size_t bytes)
+{
+    if (!image || bytes < matmul_image(d.experts, d.m, d.k, d.bits, d.gated).bytes) return QNN_EINVAL;
+    return aligned(image, 256) ? QNN_OK : QNN_EALIGN;
+}
+
+// Rows of the 32-bit products that a combine sums over.
+int64_t combine_ld(const qnn_matmul_desc &d) { return (static_cast<int64_t>(d.m) + 7) / 8 * 8; }
+
+qnn_status check_slots(const qnn_matmul_desc *d, int64_t tokens, int32_t top)
+{
+    const qnn_status st = check_matmul(d);
+    if (st != QNN_OK) return st;
+    if (tokens < 0 || top <= 0) return QNN_EINVAL;
+    if (top > 1024 || tokens > kMaxRows || tokens * top > kMaxRows) return QNN_EUNSUPPORTED;
+    return QNN_OK;
+}
 
 }  // namespace
 }  // namespace qnn
@@ -80,6 +125,111 @@ qnn_status qnn_expert_plan(const int32_t *ids, int64_t slots, int32_t experts, i
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return QNN_EWORKSPACE;
     return from_cuda(launch_expert_plan(ids, slots, experts, offsets, order, position, workspace,
                                         static_cast<cudaStream_t>(stream)));
+}
+
+qnn_status qnn_matmul_image_size(const qnn_matmul_desc *d, size_t *bytes)
+{
+    if (!bytes) return QNN_EINVAL;
+    const qnn_status st = check_matmul(d);
+    if (st != QNN_OK) return st;
+    *bytes = matmul_image(d->experts, d->m, d->k, d->bits, d->gated).bytes;
+    return QNN_OK;
+}
+
+qnn_status qnn_matmul_prepare(const qnn_matmul_desc *d, const void *w, const float *scale, const float *bias,
+                              void *image, size_t image_bytes, void *stream)
+{
+    qnn_status st = check_matmul(d);
+    if (st != QNN_OK) return st;
+    if (!w) return QNN_EINVAL;
+    st = check_image(*d, image, image_bytes);
+    if (st != QNN_OK) return st;
+    if (!aligned(w, d->bits == 16 ? 2 : 1) || !aligned(scale, 4) || !aligned(bias, 4)) return QNN_EALIGN;
+    return from_cuda(launch_matmul_prep(*d, w, scale, bias, image, static_cast<cudaStream_t>(stream)));
+}
+
+qnn_status qnn_matmul_workspace_size(const qnn_matmul_desc *d, int64_t t, const void *x, int64_t ldx, size_t *bytes)
+{
+    (void)x;
+    if (!bytes) return QNN_EINVAL;
+    const qnn_status st = check_matmul(d);
+    if (st != QNN_OK) return st;
+    if (t < 0 || ldx < d->k) return QNN_EINVAL;
+    if (t > kMaxRows) return QNN_EUNSUPPORTED;
+    *bytes = 0;
+    return QNN_OK;
+}
+
+qnn_status qnn_matmul_run(const qnn_matmul_desc *d, const void *image, size_t image_bytes, int64_t t, const void *x,
+                          int64_t ldx, const void *residual, int64_t ldres, void *y, int64_t ldy, int32_t out_f32,
+                          void *workspace, size_t workspace_bytes, void *stream)
+{
+    size_t need = 0;
+    qnn_status st = qnn_matmul_workspace_size(d, t, x, ldx, &need);
+    if (st != QNN_OK) return st;
+    if (d->experts != 1 || !flag_ok(out_f32) || (t > 0 && (!x || !y))) return QNN_EINVAL;
+    if (ldy < d->m || (residual && ldres < d->m)) return QNN_EINVAL;
+    st = check_image(*d, image, image_bytes);
+    if (st != QNN_OK) return st;
+    if (!aligned(x, 2) || !aligned(residual, 2) || !aligned(y, out_f32 ? 4 : 2)) return QNN_EALIGN;
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return QNN_EWORKSPACE;
+    MatmulArgs a = base_args(*d, image, x, ldx, y, ldy);
+    a.residual = residual; a.ldres = ldres; a.out_f32 = out_f32; a.rows = t;
+    return from_cuda(launch_matmul_stream(a, d->dtype, d->bits, static_cast<cudaStream_t>(stream)));
+}
+
+qnn_status qnn_experts_workspace_size(const qnn_matmul_desc *d, int64_t tokens, int32_t top, int32_t combine,
+                                      const void *x, int64_t ldx, size_t *bytes)
+{
+    (void)x;
+    if (!bytes || !flag_ok(combine)) return QNN_EINVAL;
+    const qnn_status st = check_slots(d, tokens, top);
+    if (st != QNN_OK) return st;
+    if (ldx < d->k) return QNN_EINVAL;
+    *bytes = combine ? static_cast<size_t>(tokens) * top * combine_ld(*d) * sizeof(float) : 0;
+    return QNN_OK;
+}
+
+qnn_status qnn_experts_dispatch(const qnn_matmul_desc *d, const void *image, size_t image_bytes, int64_t tokens,
+                                int32_t top, const int32_t *offsets, const int32_t *order, const void *x, int64_t ldx,
+                                void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream)
+{
+    size_t need = 0;
+    qnn_status st = qnn_experts_workspace_size(d, tokens, top, 0, x, ldx, &need);
+    if (st != QNN_OK) return st;
+    if (!offsets || ldy < d->m || (tokens > 0 && (!order || !x || !y))) return QNN_EINVAL;
+    st = check_image(*d, image, image_bytes);
+    if (st != QNN_OK) return st;
+    if (!aligned(x, 2) || !aligned(y, 2) || !aligned(offsets, 4) || !aligned(order, 4)) return QNN_EALIGN;
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return QNN_EWORKSPACE;
+    MatmulArgs a = base_args(*d, image, x, ldx, y, ldy);
+    a.offsets = offsets; a.order = order; a.top = top; a.gather = 1; a.zero_tail = 1; a.rows = tokens * top;
+    return from_cuda(launch_matmul_stream(a, d->dtype, d->bits, static_cast<cudaStream_t>(stream)));
+}
+
+qnn_status qnn_experts_combine(const qnn_matmul_desc *d, const void *image, size_t image_bytes, int64_t tokens,
+                               int32_t top, const int32_t *offsets, const int32_t *position, const float *weights,
+                               const void *x, int64_t ldx, const void *residual, int64_t ldres, void *y, int64_t ldy,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    size_t need = 0;
+    qnn_status st = qnn_experts_workspace_size(d, tokens, top, 1, x, ldx, &need);
+    if (st != QNN_OK) return st;
+    if (!offsets || ldy < d->m || (residual && ldres < d->m)) return QNN_EINVAL;
+    if (tokens > 0 && (!position || !weights || !x || !y)) return QNN_EINVAL;
+    st = check_image(*d, image, image_bytes);
+    if (st != QNN_OK) return st;
+    if (!aligned(x, 2) || !aligned(residual, 2) || !aligned(y, 2)) return QNN_EALIGN;
+    if (!aligned(offsets, 4) || !aligned(position, 4) || !aligned(weights, 4)) return QNN_EALIGN;
+    if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return QNN_EWORKSPACE;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    float *z = static_cast<float *>(workspace);
+    MatmulArgs a = base_args(*d, image, x, ldx, z, combine_ld(*d));
+    a.offsets = offsets; a.out_f32 = 1; a.rows = tokens * top; a.top = top;
+    const cudaError_t e = launch_matmul_stream(a, d->dtype, d->bits, s);
+    if (e != cudaSuccess) return QNN_ECUDA;
+    return from_cuda(launch_combine(d->dtype, z, combine_ld(*d), weights, position, tokens, top, d->m, residual, ldres,
+                                    y, ldy, s));
 }
 
 }  // extern "C"

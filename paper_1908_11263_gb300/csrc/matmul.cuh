@@ -1,0 +1,191 @@
+// Shared by the matrix-product kernels: the weight image qnn_matmul_prepare() writes, the arguments of a launch, the
+// expansion of packed codes and the fused epilogue.
+//
+// Image.  Rows of the weight matrix are taken 32 at a time and columns 64 at a time; blocks follow one another along K,
+// then along the rows, then along the experts, so that a kernel streams whole blocks with bulk copies.  A gated matrix
+// (gate rows, then up rows) is interleaved eight by eight: rows 16 i .. 16 i + 7 of the image are gate channels 8 i ..,
+// the next eight the same channels' up rows, so one thread or one pair of lanes meets both.
+//   16-bit weights: 32 rows of 128 bytes, 16-byte chunk c of row r at chunk c ^ (r & 7): the 128-byte swizzle that
+//     tcgen05.mma reads, so a block goes to shared memory as it is.
+//   packed weights: codes biased to unsigned, in the order of the m16n8k16 A fragment: lane 4 g + t of a warp holds rows
+//     g and g + 8 of each 16, columns 16 t .. 16 t + 15.  Within a 32-bit word the codes of a column pair sit 16 bits
+//     apart, so one mask and one or expand two codes at once.
+// After the blocks: one {scale, bias} pair of floats a row.
+//
+// Exactness.  A code of at most 8 bits is a whole number of at most 2^7 and exact in f16 and bf16, so the tensor cores
+// multiply the codes themselves; the channel's scale is applied once, in 32 bits, in the epilogue.
+#pragma once
+
+#include "block_common.cuh"
+#include "block_internal.h"
+#include "device.cuh"
+
+namespace qnn {
+
+struct MatmulImage {
+    int rows;        // image rows of one expert (multiple of 32)
+    int mb, kb;      // blocks along the rows and along K
+    uint32_t block_bytes;
+    size_t param_off, bytes;
+};
+
+__host__ __device__ inline MatmulImage matmul_image(int experts, int m, int k, int bits, int gated)
+{
+    MatmulImage g;
+    const int rows = gated ? (m + 7) / 8 * 16 : m;
+    g.mb = (rows + 31) / 32;
+    g.rows = g.mb * 32;
+    g.kb = (k + 63) / 64;
+    g.block_bytes = 32 * 64 * bits / 8;
+    g.param_off = static_cast<size_t>(experts) * g.mb * g.kb * g.block_bytes;
+    g.bytes = g.param_off + static_cast<size_t>(experts) * g.rows * sizeof(float2);
+    return g;
+}
+
+// One product launch.  Plain product: plan == nullptr, rows = t.  Experts: places are the plan's sorted places, and
+// `gather` says whether x has a row per token (order[place] / top) or per place.
+struct MatmulArgs {
+    const uint8_t *image;
+    const float2 *params;      // [experts][image rows]
+    const void *x;
+    const void *residual;      // plain product only
+    void *y;                   // T, or float when out_f32
+    const int32_t *offsets;    // experts + 1 places, or null
+    const int32_t *order;      // slot of each place (gather)
+    int64_t ldx, ldres, ldy;
+    int64_t rows;              // tokens of a plain product; slots of an experts' product
+    int m, k, kb, mb, experts, top;
+    int act, gated, out_f32, gather, zero_tail;
+    int x_vec;                 // rows of x are 16-byte aligned
+};
+
+// ---------------------------------------------------------------- codes
+
+template <typename T>
+struct CodeConst;
+template <>
+struct CodeConst<__half> {
+    static constexpr uint32_t kMagic = 0x64006400u;  // 1024 + v, v < 1024
+    static constexpr uint32_t kMid4 = 0x64086408u, kMid2 = 0x64026402u, kMid8 = 0x64806480u;
+};
+template <>
+struct CodeConst<__nv_bfloat16> {
+    static constexpr uint32_t kMagic = 0x43004300u;  // 128 + v, v < 128
+    static constexpr uint32_t kMid4 = 0x43084308u, kMid2 = 0x43024302u, kMid8 = 0u;
+};
+
+template <typename T>
+__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b);
+template <>
+__device__ __forceinline__ uint32_t sub2<__half>(uint32_t a, uint32_t b)
+{
+    const __half2 r = __hsub2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+template <>
+__device__ __forceinline__ uint32_t sub2<__nv_bfloat16>(uint32_t a, uint32_t b)
+{
+    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+
+// 16 biased codes of one row (BITS / 2 words) to 8 words of value pairs in column order.  All differences are exact.
+template <typename T, int BITS>
+__device__ __forceinline__ void expand16(const uint32_t *w, uint32_t (&v)[8])
+{
+    using C = CodeConst<T>;
+    if constexpr (BITS == 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t c = w[i >> 1] >> (8 * (i & 1));
+            if constexpr (C::kMid8 != 0) {
+                v[i] = sub2<T>((c & 0x00FF00FFu) | C::kMagic, C::kMid8);
+            } else {
+                // bf16 holds seven bits beside the leading one: the low seven from 128 + v, the top bit in what is
+                // subtracted (128 where it is set, 256 where it is not)
+                v[i] = sub2<T>((c & 0x007F007Fu) | C::kMagic, (c & 0x00800080u) ^ 0x43804380u);
+            }
+        }
+    } else if constexpr (BITS == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = sub2<T>(((w[i >> 2] >> (4 * (i & 3))) & 0x000F000Fu) | C::kMagic, C::kMid4);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = sub2<T>(((w[0] >> (2 * i)) & 0x00030003u) | C::kMagic, C::kMid2);
+    }
+}
+
+// ---------------------------------------------------------------- epilogue
+
+__device__ __forceinline__ float activate(float v, int act)
+{
+    switch (act) {
+        case QNN_ACT_RELU: return v > 0.f ? v : v == v ? 0.f : v;
+        case QNN_ACT_SILU: return v / (1.f + expf(-v));
+        case QNN_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+        case QNN_ACT_GELU_TANH: return 0.5f * v * (1.f + tanhf(0.79788456080286536f * (v + 0.044715f * v * v * v)));
+        default: return v;
+    }
+}
+
+// One output element: product row value(s) already scaled and biased.
+template <typename T>
+__device__ __forceinline__ void finish(const MatmulArgs &a, int64_t row, int64_t col, float v)
+{
+    if (a.residual) v += to_f32<T>(static_cast<const T *>(a.residual)[row * a.ldres + col]);
+    if (a.out_f32)
+        static_cast<float *>(a.y)[row * a.ldy + col] = v;
+    else
+        static_cast<T *>(a.y)[row * a.ldy + col] = from_f32<T>(v);
+}
+
+// Tile `u` of the experts' places, `tile` places at most to a tile: {expert, first place, places}, or expert -1 after
+// the last.  All lanes of a warp call it together.
+struct ExpertTile {
+    int expert, first, count;
+};
+
+__device__ __forceinline__ ExpertTile expert_tile(const int32_t *offsets, int experts, int tile, int u)
+{
+    const int lane = threadIdx.x & 31;
+    const int per = (experts + 31) / 32;
+    const int lo = min(lane * per, experts), hi = min(lo + per, experts);
+    int mine = 0, prev = offsets[lo];
+    for (int e = lo; e < hi; ++e) {
+        const int next = offsets[e + 1];
+        mine += (next - prev + tile - 1) / tile;
+        prev = next;
+    }
+    int inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
+    }
+    ExpertTile r = {-1, 0, 0};
+    int left = u - (inc - mine);
+    const bool here = left >= 0 && left < mine;
+    if (here) {
+        prev = offsets[lo];
+        for (int e = lo; e < hi; ++e) {
+            const int next = offsets[e + 1];
+            const int n = (next - prev + tile - 1) / tile;
+            if (left < n) {
+                r.expert = e;
+                r.first = prev + left * tile;
+                r.count = min(tile, next - r.first);
+                break;
+            }
+            left -= n;
+            prev = next;
+        }
+    }
+    const uint32_t who = __ballot_sync(0xffffffffu, here);
+    const int src = who ? __ffs(who) - 1 : 0;
+    r.expert = __shfl_sync(0xffffffffu, r.expert, src);
+    r.first = __shfl_sync(0xffffffffu, r.first, src);
+    r.count = __shfl_sync(0xffffffffu, r.count, src);
+    return r;
+}
+
+}  // namespace qnn

@@ -1,0 +1,175 @@
+// The weight image of the matrix products (qnn_matmul_prepare) and the weighted sum over a token's experts that ends
+// qnn_experts_combine.  Both are bound by memory: each byte is read and written once.
+#include "matmul.cuh"
+
+namespace qnn {
+namespace {
+
+struct PrepArgs {
+    const void *w;
+    const float *scale, *bias;
+    uint8_t *image;
+    float2 *params;
+    int experts, m, k, bits, gated, rows_src;
+    MatmulImage g;
+};
+
+// Row of the caller's matrix behind an image row, or -1 for padding.
+__device__ __forceinline__ int source_row(const PrepArgs &a, int row)
+{
+    if (!a.gated) return row < a.m ? row : -1;
+    const int ch = (row >> 4) * 8 + (row & 7);
+    if (ch >= a.m) return -1;
+    return row & 8 ? a.m + ch : ch;
+}
+
+// Biased code of column k of a packed source row (padding: the code of zero).
+template <int BITS>
+__device__ __forceinline__ uint32_t code_at(const uint8_t *row, int k, int kmax)
+{
+    constexpr uint32_t kMask = (1u << BITS) - 1u, kMid = 1u << (BITS - 1);
+    if (!row || k >= kmax) return kMid;
+    constexpr int kPer = 8 / BITS;
+    return ((row[k / kPer] >> (BITS * (k % kPer))) & kMask) ^ kMid;
+}
+
+// One 16-byte vector of the image a thread.
+template <int BITS>
+__global__ void matmul_prep_kernel(const PrepArgs a)
+{
+    constexpr int kVecs = 32 * 64 * BITS / 8 / 16;
+    const int64_t total = static_cast<int64_t>(a.experts) * a.g.mb * a.g.kb * kVecs;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < total;
+         i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        const int v = static_cast<int>(i % kVecs);
+        const int64_t block = i / kVecs;
+        const int kb = static_cast<int>(block % a.g.kb);
+        const int mb = static_cast<int>(block / a.g.kb % a.g.mb);
+        const int64_t e = block / a.g.kb / a.g.mb;
+        uint32_t out[4];
+        if constexpr (BITS == 16) {
+            const int r = v >> 3, c = (v & 7) ^ (r & 7);
+            const int src = source_row(a, mb * 32 + r);
+            const uint16_t *row = static_cast<const uint16_t *>(a.w) + (e * a.rows_src + (src < 0 ? 0 : src)) * a.k;
+            uint16_t h[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = kb * 64 + c * 8 + j;
+                h[j] = src >= 0 && k < a.k ? row[k] : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) out[j] = h[2 * j] | static_cast<uint32_t>(h[2 * j + 1]) << 16;
+        } else {
+            constexpr int kRuns = 8 / BITS;  // runs of 16 codes in the vector
+            constexpr int kWords = BITS / 2; // words of a run
+#pragma unroll
+            for (int s = 0; s < kRuns; ++s) {
+                // run s of vector v: half-row index h (8 rows each, 4 of them) and the lane it belongs to
+                const int h = BITS == 8 ? v >> 5 : BITS == 4 ? (v >> 5) * 2 + s : s;
+                const int lane = v & 31;
+                const int src = source_row(a, mb * 32 + h * 8 + (lane >> 2));
+                const int k0 = kb * 64 + (lane & 3) * 16;
+                const uint8_t *row = src < 0 ? nullptr
+                                             : static_cast<const uint8_t *>(a.w) +
+                                                   (e * a.rows_src + src) * (static_cast<int64_t>(a.k) * BITS / 8);
+                uint32_t word[kWords];
+#pragma unroll
+                for (int q = 0; q < kWords; ++q) word[q] = 0;
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {  // column pair p of the run
+                    constexpr int kPairs = 16 / BITS;  // pairs a word
+                    const int sh = BITS * (p % kPairs);
+                    word[p / kPairs] |= code_at<BITS>(row, k0 + 2 * p, a.k) << sh;
+                    word[p / kPairs] |= code_at<BITS>(row, k0 + 2 * p + 1, a.k) << (sh + 16);
+                }
+#pragma unroll
+                for (int q = 0; q < kWords; ++q) out[s * kWords + q] = word[q];
+            }
+        }
+        *reinterpret_cast<uint4 *>(a.image + i * 16) = make_uint4(out[0], out[1], out[2], out[3]);
+    }
+    const int64_t prows = static_cast<int64_t>(a.experts) * a.g.rows;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < prows;
+         i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        const int64_t e = i / a.g.rows;
+        const int src = source_row(a, static_cast<int>(i % a.g.rows));
+        float2 p = make_float2(0.f, 0.f);
+        if (src >= 0) {
+            p.x = a.scale ? a.scale[e * a.rows_src + src] : 1.f;
+            p.y = a.bias ? a.bias[e * a.rows_src + src] : 0.f;
+        }
+        a.params[i] = p;
+    }
+}
+
+// y[t] = residual[t] + sum over the token's experts of weight * z[place], in the order of the choices.
+struct CombineArgs {
+    const float *z, *weights;
+    const int32_t *position;
+    const void *residual;
+    void *y;
+    int64_t ldz, ldres, ldy, tokens;
+    int m, top;
+};
+
+template <typename T>
+__global__ void combine_kernel(const CombineArgs a)
+{
+    const int64_t t = blockIdx.x;
+    for (int c = (blockIdx.y * blockDim.x + threadIdx.x) * 4; c < a.m; c += gridDim.y * blockDim.x * 4) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int j = 0; j < a.top; ++j) {
+            const int p = a.position[t * a.top + j];
+            if (p < 0) continue;
+            const float w = a.weights[t * a.top + j];
+            const float4 v = *reinterpret_cast<const float4 *>(a.z + p * a.ldz + c);
+            s.x = fmaf(w, v.x, s.x);
+            s.y = fmaf(w, v.y, s.y);
+            s.z = fmaf(w, v.z, s.z);
+            s.w = fmaf(w, v.w, s.w);
+        }
+        const float q[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < a.m) {
+                float v = q[j];
+                if (a.residual) v += to_f32<T>(static_cast<const T *>(a.residual)[t * a.ldres + c + j]);
+                static_cast<T *>(a.y)[t * a.ldy + c + j] = from_f32<T>(v);
+            }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_matmul_prep(const qnn_matmul_desc &d, const void *w, const float *scale, const float *bias,
+                               void *image, cudaStream_t st)
+{
+    PrepArgs a;
+    a.g = matmul_image(d.experts, d.m, d.k, d.bits, d.gated);
+    a.w = w; a.scale = scale; a.bias = bias;
+    a.image = static_cast<uint8_t *>(image);
+    a.params = reinterpret_cast<float2 *>(a.image + a.g.param_off);
+    a.experts = d.experts; a.m = d.m; a.k = d.k; a.bits = d.bits; a.gated = d.gated;
+    a.rows_src = d.gated ? 2 * d.m : d.m;
+    const size_t vecs = a.g.param_off / 16;
+    const unsigned grid = static_cast<unsigned>(vecs / 256 + 1 < 65536 ? vecs / 256 + 1 : 65536);
+    if (d.bits == 16) matmul_prep_kernel<16><<<grid, 256, 0, st>>>(a);
+    else if (d.bits == 8) matmul_prep_kernel<8><<<grid, 256, 0, st>>>(a);
+    else if (d.bits == 4) matmul_prep_kernel<4><<<grid, 256, 0, st>>>(a);
+    else matmul_prep_kernel<2><<<grid, 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_combine(int dtype, const float *z, int64_t ldz, const float *weights, const int32_t *position,
+                           int64_t tokens, int top, int m, const void *residual, int64_t ldres, void *y, int64_t ldy,
+                           cudaStream_t st)
+{
+    if (tokens == 0) return cudaSuccess;
+    const CombineArgs a = {z, weights, position, residual, y, ldz, ldres, ldy, tokens, m, top};
+    const dim3 grid(static_cast<unsigned>(tokens), (m + 1023) / 1024);
+    if (dtype == QNN_F16) combine_kernel<__half><<<grid, 256, 0, st>>>(a);
+    else combine_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace qnn

@@ -28,7 +28,9 @@ EXPORTED = ("qconv_hwc_workspace_size", "qconv_hwc", "qconv_hwc_prepare", "qconv
             "unpack_subbyte", "qnn_device_status", "qnn_status_string", "qnn_version", "qconv_hwc_noalloc",
             "qnn_selftest_wait_timeout", "qconv_hwc_thresholds", "qconv_hwc_binary", "qconv_hwc_pool2", "qconv_hwc_pool2_run",
             "qconv_hwc_mma_operand_bits", "qconv_hwc_tc_kernel", "qnn_block_norm", "qnn_route_topk",
-            "qnn_expert_plan_workspace_size", "qnn_expert_plan")
+            "qnn_expert_plan_workspace_size", "qnn_expert_plan", "qnn_matmul_image_size", "qnn_matmul_prepare",
+            "qnn_matmul_workspace_size", "qnn_matmul_run", "qnn_experts_workspace_size", "qnn_experts_dispatch",
+            "qnn_experts_combine")
 
 F16, BF16, F32 = 0, 1, 2  # QNN_F16, QNN_BF16, QNN_F32
 _DTYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
@@ -55,6 +57,11 @@ class RouteDesc(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in (
         "dtype", "experts", "k", "score", "groups", "top_groups", "group_score", "renormalise")] + [
             ("scale", ctypes.c_float), ("t", ctypes.c_int64), ("ld", ctypes.c_int64)]
+
+
+class MatmulDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in (
+        "experts", "m", "k", "bits", "dtype", "gated", "act")]
 
 
 _lock = threading.Lock()
@@ -119,6 +126,21 @@ def load(build_if_missing: bool = False):
         lib.qnn_expert_plan_workspace_size.restype = I32
         lib.qnn_expert_plan.argtypes = [P, I64, I32, P, P, P, P, SZ, P]
         lib.qnn_expert_plan.restype = I32
+        MP = ctypes.POINTER(MatmulDesc)
+        lib.qnn_matmul_image_size.argtypes = [MP, ctypes.POINTER(SZ)]
+        lib.qnn_matmul_image_size.restype = I32
+        lib.qnn_matmul_prepare.argtypes = [MP, P, P, P, P, SZ, P]
+        lib.qnn_matmul_prepare.restype = I32
+        lib.qnn_matmul_workspace_size.argtypes = [MP, I64, P, I64, ctypes.POINTER(SZ)]
+        lib.qnn_matmul_workspace_size.restype = I32
+        lib.qnn_matmul_run.argtypes = [MP, P, SZ, I64, P, I64, P, I64, P, I64, I32, P, SZ, P]
+        lib.qnn_matmul_run.restype = I32
+        lib.qnn_experts_workspace_size.argtypes = [MP, I64, I32, I32, P, I64, ctypes.POINTER(SZ)]
+        lib.qnn_experts_workspace_size.restype = I32
+        lib.qnn_experts_dispatch.argtypes = [MP, P, SZ, I64, I32, P, P, P, I64, P, I64, P, SZ, P]
+        lib.qnn_experts_dispatch.restype = I32
+        lib.qnn_experts_combine.argtypes = [MP, P, SZ, I64, I32, P, P, P, P, I64, P, I64, P, I64, P, SZ, P]
+        lib.qnn_experts_combine.restype = I32
         lib.qnn_selftest_wait_timeout.argtypes = [I64, P]
         lib.qnn_selftest_wait_timeout.restype = I32
         lib.qnn_device_status.argtypes = [P]
@@ -210,7 +232,9 @@ def _workspace(nbytes: int, device, stream):
     key = (device.index, stream.cuda_stream if stream is not None else torch.cuda.current_stream(device).cuda_stream)
     buf = _workspaces.get(key)
     if buf is None or buf.numel() < nbytes:
-        buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        # allocated on the stream that uses it, so that a buffer outgrown while calls are queued is not handed on early
+        with torch.cuda.stream(stream):
+            buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
         _workspaces[key] = buf
     return buf
 
@@ -621,6 +645,132 @@ def expert_plan(ids, experts, *, stream=None) -> ExpertPlan:
                              _ptr(ws), need.value, _stream(stream))
     _check(st, "qnn_expert_plan")
     return ExpertPlan(ids.shape[0], ids.shape[1], experts, offsets, order, position)
+
+
+_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+
+class _Prepared:
+    """Weights laid out once for the matrix-product kernels (qnn_matmul_prepare)."""
+
+    def __init__(self, w, scale, bias, bits, dtype, gated, act, experts, stream):
+        if act not in _ACTS:
+            raise ValueError(f"act must be one of {sorted(_ACTS)}, got {act!r}")
+        if bits == 16:
+            if w.dtype not in (torch.float16, torch.bfloat16) or dtype not in (None, w.dtype):
+                raise TypeError(f"16-bit weights must be float16 or bfloat16 and dtype, if given, theirs; got {w.dtype}, {dtype}")
+            _dev(w, None, "w")
+            dtype, per = w.dtype, 1
+        elif bits in (8, 4, 2):
+            _dev(w, (torch.uint8, torch.int8), "w")
+            dtype, per = torch.bfloat16 if dtype is None else dtype, 8 // bits
+            if dtype not in (torch.float16, torch.bfloat16):
+                raise TypeError(f"dtype must be float16 or bfloat16, got {dtype}")
+        else:
+            raise QnnError(QNN_EUNSUPPORTED, "qnn_matmul_prepare")
+        if w.dim() != (3 if experts else 2):
+            raise ValueError(f"w must have shape {'[experts, rows, k]' if experts else '[rows, k]'}, got {tuple(w.shape)}")
+        rows = w.shape[-2]
+        if gated and rows % 2:
+            raise ValueError("a gated product needs as many gate rows as up rows")
+        self.dtype, self.device, self.experts = dtype, w.device, w.shape[0] if experts else 1
+        self.m, self.k = rows // 2 if gated else rows, w.shape[-1] * per
+        pscale = _param(scale, torch.float32, "scale", w.shape[:-1], w.device)
+        pbias = _param(bias, torch.float32, "bias", w.shape[:-1], w.device)
+        self.desc = MatmulDesc(ctypes.sizeof(MatmulDesc), self.experts, self.m, self.k, bits, _DTYPES[dtype], int(bool(gated)),
+                               _ACTS[act])
+        self._desc = ctypes.byref(self.desc)
+        lib, need = load(), ctypes.c_size_t(0)
+        _check(lib.qnn_matmul_image_size(self._desc, ctypes.byref(need)), "qnn_matmul_image_size")
+        self.nbytes = need.value
+        self.image = torch.empty(self.nbytes, dtype=torch.uint8, device=w.device)
+        st = lib.qnn_matmul_prepare(self._desc, _ptr(w), pscale, pbias, self.image.data_ptr(), self.nbytes, _stream(stream))
+        _check(st, "qnn_matmul_prepare")
+
+
+class PreparedMatmul(_Prepared):
+    """A matrix product with its epilogue fused: y = residual + act(scale * (x w^T) + bias), or with gated=True
+    residual + act(gate) * up, where w holds the gate rows and then the up rows.
+
+    w: float16/bfloat16 [rows, k] (bits=16), or packed signed codes uint8/int8 [rows, k*bits/8] (bits 8, 4 or 2) with
+    scale float32 [rows]; bias float32 [rows].  dtype: of x, residual and outputs (for 16-bit weights, theirs)."""
+
+    def __init__(self, w, *, scale=None, bias=None, bits=16, dtype=None, gated=False, act="none", stream=None):
+        super().__init__(w, scale, bias, bits, dtype, gated, act, False, stream)
+
+    def __call__(self, x, residual=None, *, out=None, out_dtype=None, stream=None):
+        """x [t, k] -> [t, m] in x's dtype, or float32 with out_dtype=torch.float32.  out may be the residual."""
+        px, ldx = _rows(x, self.dtype, "x", None, self.device)
+        t = x.shape[0]
+        if x.shape[1] != self.k:
+            raise ValueError(f"x must have {self.k} columns, got {x.shape[1]}")
+        pres, ldres = (None, self.m) if residual is None else _rows(residual, self.dtype, "residual", (t, self.m), self.device)
+        if out is None:
+            out = torch.empty((t, self.m), dtype=self.dtype if out_dtype is None else out_dtype, device=self.device)
+        elif out_dtype not in (None, out.dtype):
+            raise TypeError(f"out has dtype {out.dtype}, not {out_dtype}")
+        po, ldo = _rows(out, (self.dtype, torch.float32), "out", (t, self.m), self.device)
+        lib, need = load(), ctypes.c_size_t(0)
+        _check(lib.qnn_matmul_workspace_size(self._desc, t, px, ldx, ctypes.byref(need)), "qnn_matmul_workspace_size")
+        ws = _workspace(need.value, self.device, stream)
+        st = lib.qnn_matmul_run(self._desc, self.image.data_ptr(), self.nbytes, t, px, ldx, pres, ldres, po, ldo,
+                                int(out.dtype == torch.float32), _ptr(ws), need.value, _stream(stream))
+        _check(st, "qnn_matmul_run")
+        return out
+
+
+class PreparedExperts(_Prepared):
+    """One weight matrix an expert, as PreparedMatmul: w [experts, rows, ...], scale and bias float32 [experts, rows]."""
+
+    def __init__(self, w, *, scale=None, bias=None, bits=16, dtype=None, gated=False, act="none", stream=None):
+        super().__init__(w, scale, bias, bits, dtype, gated, act, True, stream)
+
+    def _check_plan(self, plan):
+        if plan.experts != self.experts:
+            raise ValueError(f"the plan is over {plan.experts} experts, the weights over {self.experts}")
+        if plan.order.device != self.device:
+            raise ValueError(f"the plan must be on {self.device}")
+
+    def _workspace(self, plan, combine, px, ldx, stream):
+        need = ctypes.c_size_t(0)
+        _check(load().qnn_experts_workspace_size(self._desc, plan.tokens, plan.top, combine, px, ldx, ctypes.byref(need)),
+               "qnn_experts_workspace_size")
+        return _workspace(need.value, self.device, stream), need.value
+
+    def dispatch(self, x, plan, *, out=None, stream=None):
+        """Each place's token through its expert (qnn_experts_dispatch): x [tokens, k] -> [tokens * top, m] in the
+        plan's order; rows after the last place are zero."""
+        self._check_plan(plan)
+        px, ldx = _rows(x, self.dtype, "x", (plan.tokens, self.k), self.device)
+        if out is None:
+            out = torch.empty((plan.tokens * plan.top, self.m), dtype=self.dtype, device=self.device)
+        po, ldo = _rows(out, self.dtype, "out", (plan.tokens * plan.top, self.m), self.device)
+        ws, need = self._workspace(plan, 0, px, ldx, stream)
+        st = load().qnn_experts_dispatch(self._desc, self.image.data_ptr(), self.nbytes, plan.tokens, plan.top,
+                                         plan.offsets.data_ptr(), plan.order.data_ptr(), px, ldx, po, ldo, _ptr(ws), need,
+                                         _stream(stream))
+        _check(st, "qnn_experts_dispatch")
+        return out
+
+    def combine(self, x, plan, weights, residual=None, *, out=None, stream=None):
+        """The places' rows through their experts and back to the tokens (qnn_experts_combine):
+        y[t] = residual[t] + sum_j weights[t, j] * product(position[t, j]); x [tokens * top, k] -> [tokens, m]."""
+        self._check_plan(plan)
+        px, ldx = _rows(x, self.dtype, "x", (plan.tokens * plan.top, self.k), self.device)
+        pw = _param(weights, torch.float32, "weights", (plan.tokens, plan.top), self.device)
+        if pw is None:
+            raise ValueError("weights are needed")
+        shape = (plan.tokens, self.m)
+        pres, ldres = (None, self.m) if residual is None else _rows(residual, self.dtype, "residual", shape, self.device)
+        if out is None:
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        po, ldo = _rows(out, self.dtype, "out", shape, self.device)
+        ws, need = self._workspace(plan, 1, px, ldx, stream)
+        st = load().qnn_experts_combine(self._desc, self.image.data_ptr(), self.nbytes, plan.tokens, plan.top,
+                                        plan.offsets.data_ptr(), plan.position.data_ptr(), pw, px, ldx, pres, ldres, po, ldo,
+                                        _ptr(ws), need, _stream(stream))
+        _check(st, "qnn_experts_combine")
+        return out
 
 
 def selftest_wait_timeout(limit_cycles: int, stream=None):
