@@ -46,6 +46,36 @@ qnn_status check_image(const qnn_matmul_desc &d, const void *image, size_t bytes
     return aligned(image, 256) ? QNN_OK : QNN_EALIGN;
 }
 
+// The tensor-core kernel takes over where a matrix meets more rows of x than this (on average, for experts).
+constexpr int64_t kStreamRows = 32, kStreamExpertRows = 16;
+
+bool on_tensor_cores(int64_t rows, int experts)
+{
+    return experts ? rows > kStreamExpertRows * experts : rows > kStreamRows;
+}
+
+int64_t align8(int64_t v) { return (v + 7) / 8 * 8; }
+size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+
+// Bytes for x with 16-byte aligned rows, where the tensor-core kernel needs them and x has none.
+size_t staging_bytes(const qnn_matmul_desc &d, int64_t rows, int experts, int64_t x_rows, const void *x, int64_t ldx)
+{
+    if (!on_tensor_cores(rows, experts) || (aligned(x, 16) && ldx % 8 == 0)) return 0;
+    return static_cast<size_t>(x_rows) * align8(d.k) * 2;
+}
+
+cudaError_t run_product(MatmulArgs a, const qnn_matmul_desc &d, void *staging, cudaStream_t st)
+{
+    if (!on_tensor_cores(a.rows, a.offsets ? a.experts : 0)) return launch_matmul_stream(a, d.dtype, d.bits, st);
+    if (!a.x_vec) {
+        const cudaError_t e = launch_align_rows(a.x, a.ldx, staging, align8(d.k), a.x_rows, d.k, st);
+        if (e != cudaSuccess) return e;
+        a.x = staging;
+        a.ldx = align8(d.k);
+    }
+    return launch_matmul_tc(a, d.dtype, d.bits, st);
+}
+
 // Rows of the 32-bit products that a combine sums over.
 int64_t combine_ld(const qnn_matmul_desc &d) { return (static_cast<int64_t>(d.m) + 7) / 8 * 8; }
 
@@ -150,13 +180,12 @@ qnn_status qnn_matmul_prepare(const qnn_matmul_desc *d, const void *w, const flo
 
 qnn_status qnn_matmul_workspace_size(const qnn_matmul_desc *d, int64_t t, const void *x, int64_t ldx, size_t *bytes)
 {
-    (void)x;
     if (!bytes) return QNN_EINVAL;
     const qnn_status st = check_matmul(d);
     if (st != QNN_OK) return st;
     if (t < 0 || ldx < d->k) return QNN_EINVAL;
     if (t > kMaxRows) return QNN_EUNSUPPORTED;
-    *bytes = 0;
+    *bytes = staging_bytes(*d, t, 0, t, x, ldx);
     return QNN_OK;
 }
 
@@ -174,19 +203,20 @@ qnn_status qnn_matmul_run(const qnn_matmul_desc *d, const void *image, size_t im
     if (!aligned(x, 2) || !aligned(residual, 2) || !aligned(y, out_f32 ? 4 : 2)) return QNN_EALIGN;
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return QNN_EWORKSPACE;
     MatmulArgs a = base_args(*d, image, x, ldx, y, ldy);
-    a.residual = residual; a.ldres = ldres; a.out_f32 = out_f32; a.rows = t;
-    return from_cuda(launch_matmul_stream(a, d->dtype, d->bits, static_cast<cudaStream_t>(stream)));
+    a.residual = residual; a.ldres = ldres; a.out_f32 = out_f32; a.rows = a.x_rows = t;
+    return from_cuda(run_product(a, *d, workspace, static_cast<cudaStream_t>(stream)));
 }
 
 qnn_status qnn_experts_workspace_size(const qnn_matmul_desc *d, int64_t tokens, int32_t top, int32_t combine,
                                       const void *x, int64_t ldx, size_t *bytes)
 {
-    (void)x;
     if (!bytes || !flag_ok(combine)) return QNN_EINVAL;
     const qnn_status st = check_slots(d, tokens, top);
     if (st != QNN_OK) return st;
     if (ldx < d->k) return QNN_EINVAL;
-    *bytes = combine ? static_cast<size_t>(tokens) * top * combine_ld(*d) * sizeof(float) : 0;
+    const int64_t slots = tokens * top;
+    *bytes = staging_bytes(*d, slots, d->experts, combine ? slots : tokens, x, ldx);
+    if (combine) *bytes += align256(static_cast<size_t>(slots) * combine_ld(*d) * sizeof(float));
     return QNN_OK;
 }
 
@@ -204,7 +234,8 @@ qnn_status qnn_experts_dispatch(const qnn_matmul_desc *d, const void *image, siz
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return QNN_EWORKSPACE;
     MatmulArgs a = base_args(*d, image, x, ldx, y, ldy);
     a.offsets = offsets; a.order = order; a.top = top; a.gather = 1; a.zero_tail = 1; a.rows = tokens * top;
-    return from_cuda(launch_matmul_stream(a, d->dtype, d->bits, static_cast<cudaStream_t>(stream)));
+    a.x_rows = tokens;
+    return from_cuda(run_product(a, *d, workspace, static_cast<cudaStream_t>(stream)));
 }
 
 qnn_status qnn_experts_combine(const qnn_matmul_desc *d, const void *image, size_t image_bytes, int64_t tokens,
@@ -225,8 +256,9 @@ qnn_status qnn_experts_combine(const qnn_matmul_desc *d, const void *image, size
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     float *z = static_cast<float *>(workspace);
     MatmulArgs a = base_args(*d, image, x, ldx, z, combine_ld(*d));
-    a.offsets = offsets; a.out_f32 = 1; a.rows = tokens * top; a.top = top;
-    const cudaError_t e = launch_matmul_stream(a, d->dtype, d->bits, s);
+    a.offsets = offsets; a.out_f32 = 1; a.rows = a.x_rows = tokens * top; a.top = top;
+    const size_t z_bytes = align256(static_cast<size_t>(a.rows) * combine_ld(*d) * sizeof(float));
+    const cudaError_t e = run_product(a, *d, static_cast<char *>(workspace) + z_bytes, s);
     if (e != cudaSuccess) return QNN_ECUDA;
     return from_cuda(launch_combine(d->dtype, z, combine_ld(*d), weights, position, tokens, top, d->m, residual, ldres,
                                     y, ldy, s));

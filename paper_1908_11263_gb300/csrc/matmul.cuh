@@ -54,6 +54,7 @@ struct MatmulArgs {
     const int32_t *order;      // slot of each place (gather)
     int64_t ldx, ldres, ldy;
     int64_t rows;              // tokens of a plain product; slots of an experts' product
+    int64_t x_rows;            // rows that x has
     int m, k, kb, mb, experts, top;
     int act, gated, out_f32, gather, zero_tail;
     int x_vec;                 // rows of x are 16-byte aligned

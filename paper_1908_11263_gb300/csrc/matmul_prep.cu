@@ -139,7 +139,21 @@ __global__ void combine_kernel(const CombineArgs a)
     }
 }
 
+__global__ void align_rows_kernel(const uint16_t *src, int64_t lds, uint16_t *dst, int64_t ldd, int cols)
+{
+    const int64_t row = blockIdx.x;
+    for (int c = threadIdx.x; c < cols; c += blockDim.x) dst[row * ldd + c] = src[row * lds + c];
+}
+
 }  // namespace
+
+cudaError_t launch_align_rows(const void *src, int64_t lds, void *dst, int64_t ldd, int64_t rows, int cols, cudaStream_t st)
+{
+    if (rows == 0) return cudaSuccess;
+    align_rows_kernel<<<static_cast<unsigned>(rows), 256, 0, st>>>(static_cast<const uint16_t *>(src), lds,
+                                                                 static_cast<uint16_t *>(dst), ldd, cols);
+    return cudaGetLastError();
+}
 
 cudaError_t launch_matmul_prep(const qnn_matmul_desc &d, const void *w, const float *scale, const float *bias,
                                void *image, cudaStream_t st)
