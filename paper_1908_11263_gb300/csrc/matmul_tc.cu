@@ -51,36 +51,8 @@ __device__ __forceinline__ void mbar_arrive_leader(uint64_t *bar)
     asm volatile(
         "{\n\t.reg .b32 r;\n\t"
         "mapa.shared::cluster.u32 r, %0, 0;\n\t"
-        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n\t}" ::"r"(smem_addr(bar))
+        "mbarrier.arrive.shared::cluster.b64 _, [r];\n\t}" ::"r"(smem_addr(bar))
         : "memory");
-}
-
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_addr(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
-// mbar_wait_warp for a barrier that the other CTA arrives on.
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity, int *status,
-                                                  long long limit_cycles = kWaitLimitCycles)
-{
-    const long long t0 = clock64();
-    while (true) {
-        const bool ok = mbar_try_wait_cluster(bar, parity);
-        if (__all_sync(0xffffffffu, ok)) return true;
-        if (__any_sync(0xffffffffu, clock64() - t0 > limit_cycles)) {
-            if ((threadIdx.x & 31) == 0) report(status, QNN_ETIMEOUT);
-            return false;
-        }
-    }
 }
 
 __device__ __forceinline__ void mma2_f16_warp(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
@@ -337,14 +309,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 256 : 5
         uint32_t phase = 0;
         for (int id = pair; id < tiles && ok; id += pairs, ++it) {
             const int buf = it & 1;
-            if (!mbar_wait_cluster(acc_empty + buf, ((it >> 1) & 1) ^ 1, status)) {
+            if (!mbar_wait_warp(acc_empty + buf, ((it >> 1) & 1) ^ 1, status)) {
                 ok = false;
                 break;
             }
             tc_fence_after();
             const uint32_t d = tmem + buf * s.nt;
             for (int kb = 0; kb < a.kb; ++kb) {
-                if (!mbar_wait_cluster(ready + st, phase, status)) {
+                if (!mbar_wait_warp(ready + st, phase, status)) {
                     ok = false;
                     break;
                 }
