@@ -8,7 +8,7 @@
 //
 // Warps: 0 loads (x by tiled TMA, or one four-row gather per lane where an expert picks its tokens; weight blocks by
 // bulk copies), 1 issues the MMAs (first CTA of the pair), 2 hands complete stages of 16-bit weights on, 3 owns the
-// tensor memory, 4-7 run the epilogue, 8-15 expand packed codes into the A operand (packed weights only).
+// tensor memory, 4-11 run the epilogue, 12-19 expand packed codes into the A operand (packed weights only).
 // Every wait is bounded (mbar_wait_warp); a wait that gives up ends its role, and the kernel, with the status word set.
 #include <cuda.h>
 
@@ -106,58 +106,104 @@ __device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr)
 
 // ---------------------------------------------------------------- epilogue
 
-// Sixteen rows of x (columns of the accumulator) of one image row.
-template <typename T, int ACT>
-__device__ __forceinline__ void store16(const MatmulArgs &a, const uint32_t (&acc)[16], float2 p, int64_t row, int n,
-                                        int64_t ch, bool valid)
+// Activation of an array, the choice outside the loop.
+template <int N>
+__device__ __forceinline__ void activate_all(float (&v)[N], int act)
 {
-    if (!a.gated) {
-        if (!valid) return;
-        float res[16];
-        if (a.residual) {
-            const T *r = static_cast<const T *>(a.residual) + row * a.ldres + ch;
+    switch (act) {
+        case QNN_ACT_RELU:
 #pragma unroll
-            for (int i = 0; i < 16; ++i) res[i] = i < n ? to_f32<T>(r[i * a.ldres]) : 0.f;
-        }
+            for (int i = 0; i < N; ++i) v[i] = activate(v[i], QNN_ACT_RELU);
+            break;
+        case QNN_ACT_SILU:
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (i < n) {
-                float v = activate(fmaf(__uint_as_float(acc[i]), p.x, p.y), ACT);
-                if (a.residual) v += res[i];
-                if (a.out_f32)
-                    static_cast<float *>(a.y)[(row + i) * a.ldy + ch] = v;
-                else
-                    static_cast<T *>(a.y)[(row + i) * a.ldy + ch] = from_f32<T>(v);
-            }
-        return;
+            for (int i = 0; i < N; ++i) v[i] = activate(v[i], QNN_ACT_SILU);
+            break;
+        case QNN_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = activate(v[i], QNN_ACT_GELU);
+            break;
+        case QNN_ACT_GELU_TANH:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = activate(v[i], QNN_ACT_GELU_TANH);
+            break;
+        default: break;
     }
-    // gate and up rows of a channel are eight lanes apart: of each two rows of x the gate lane finishes the first, the
-    // up lane the second
-    const bool up = threadIdx.x & 8;
+}
+
+// N values of one channel to rows `step` elements apart, `n` of them at most.
+template <typename T, int N>
+__device__ __forceinline__ void store_rows(T *y, int64_t step, const float (&v)[N], int n)
+{
+    if (n >= N) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-        const float v0 = fmaf(__uint_as_float(acc[i]), p.x, p.y), v1 = fmaf(__uint_as_float(acc[i + 1]), p.x, p.y);
-        const float other = __shfl_xor_sync(0xffffffffu, up ? v0 : v1, 8);
-        const float gate = up ? other : v0, u = up ? v1 : other;
-        const int at = i + (up ? 1 : 0);
-        if (valid && at < n) {
-            const float v = activate(gate, ACT) * u;
-            finish<T>(a, row + at, ch, v);
+        for (int i = 0; i < N; ++i) {
+            *y = from_f32<T>(v[i]);
+            y += step;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i < n) *y = from_f32<T>(v[i]);
+            y += step;
         }
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void store16_act(const MatmulArgs &a, const uint32_t (&acc)[16], float2 p, int64_t row, int n,
-                                            int64_t ch, bool valid)
+// The residual of the same rows.
+template <typename T, int N>
+__device__ __forceinline__ void load_rows(const T *r, int64_t step, T (&v)[N], int n)
 {
-    switch (a.act) {
-        case QNN_ACT_RELU: store16<T, QNN_ACT_RELU>(a, acc, p, row, n, ch, valid); break;
-        case QNN_ACT_SILU: store16<T, QNN_ACT_SILU>(a, acc, p, row, n, ch, valid); break;
-        case QNN_ACT_GELU: store16<T, QNN_ACT_GELU>(a, acc, p, row, n, ch, valid); break;
-        case QNN_ACT_GELU_TANH: store16<T, QNN_ACT_GELU_TANH>(a, acc, p, row, n, ch, valid); break;
-        default: store16<T, QNN_ACT_NONE>(a, acc, p, row, n, ch, valid); break;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = i < n ? *r : from_f32<T>(0.f);
+        r += step;
     }
+}
+
+// Sixteen rows of x (columns of the accumulator) from `row` on, `n` of them in use, of one image row.  Without a gate a
+// lane finishes its own channel.  With one, a channel's gate and up rows are eight lanes apart: of each two rows of x the
+// gate lane finishes the first and the up lane the second.
+template <typename T, bool GATED>
+__device__ __forceinline__ void finish16(const MatmulArgs &a, uint32_t src, float2 p, int64_t row, int n, int64_t ch,
+                                         bool valid)
+{
+    constexpr int kN = GATED ? 8 : 16;
+    const bool up = GATED && (threadIdx.x & 8);
+    const int64_t rows = GATED ? 2 : 1;
+    if (up) ++row;
+    const int mine = !valid ? 0 : GATED ? (n + (up ? 0 : 1)) / 2 : n;  // rows that this lane finishes
+    T res[kN];
+    if (a.residual) load_rows(static_cast<const T *>(a.residual) + row * a.ldres + ch, rows * a.ldres, res, mine);
+    uint32_t acc[16];
+    __syncwarp();
+    tmem_ld16(src, acc);
+    tmem_wait_ld();
+    float v[kN];
+    if constexpr (GATED) {
+        float u[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const float v0 = fmaf(__uint_as_float(acc[2 * i]), p.x, p.y), v1 = fmaf(__uint_as_float(acc[2 * i + 1]), p.x, p.y);
+            const float other = __shfl_xor_sync(0xffffffffu, up ? v0 : v1, 8);
+            v[i] = up ? other : v0;
+            u[i] = up ? v1 : other;
+        }
+        activate_all(v, a.act);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] *= u[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] = fmaf(__uint_as_float(acc[i]), p.x, p.y);
+        activate_all(v, a.act);
+    }
+    if (a.residual)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] += to_f32<T>(res[i]);
+    if (a.out_f32)
+        store_rows(static_cast<float *>(a.y) + row * a.ldy + ch, rows * a.ldy, v, mine);
+    else
+        store_rows(static_cast<T *>(a.y) + row * a.ldy + ch, rows * a.ldy, v, mine);
 }
 
 // ---------------------------------------------------------------- tiles
@@ -194,7 +240,7 @@ __device__ __forceinline__ Tile tile_at(const MatmulArgs &a, const TcShape &s, c
 }
 
 template <typename T, int BITS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 256 : 512, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 640, 1)
     matmul_tc_kernel(const __grid_constant__ CUtensorMap xmap, const MatmulArgs a, const TcShape s, int *status)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -219,7 +265,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 256 : 5
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(acc_full + i, 1);
-            mbar_init(acc_empty + i, 8);
+            mbar_init(acc_empty + i, 16);
         }
         fence_mbar_init();
     }
@@ -350,9 +396,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 256 : 5
                     phase ^= 1;
                 }
             }
-    } else if (warp >= 4 && warp < 8) {
-        // ------------------------------------------------ epilogue
-        const int quarter = warp - 4;
+    } else if (warp >= 4 && warp < 12) {
+        // ------------------------------------------------ epilogue: two warps a quarter of the lanes
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
         int it = 0;
         for (int id = pair; id < tiles && ok; id += pairs, ++it) {
             const int buf = it & 1;
@@ -367,21 +413,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 256 : 5
             }
             tc_fence_after();
             const uint32_t src = tmem + buf * s.nt + (static_cast<uint32_t>(quarter * 32) << 16);
-            for (int c = 0; c < t.count; c += 16) {
-                uint32_t acc[16];
-                tmem_ld16(src + c, acc);
-                tmem_wait_ld();
-                store16_act<T>(a, acc, p, t.first + c, t.count - c, ch, valid);
-                __syncwarp();
+            for (int c = 16 * half; c < t.count; c += 32) {
+                if (a.gated)
+                    finish16<T, true>(a, src + c, p, t.first + c, t.count - c, ch, valid);
+                else
+                    finish16<T, false>(a, src + c, p, t.first + c, t.count - c, ch, valid);
             }
+            __syncwarp();
             tc_fence_before();
             if (lane == 0) mbar_arrive_leader(acc_empty + buf);
             __syncwarp();
         }
-    } else if (warp >= 8) {
+    } else if (warp >= 12) {
         // ------------------------------------------------ packed codes to the A operand
         if constexpr (kPacked) {
-            const int i = (warp - 8) >> 1, j = (warp - 8) & 1;  // 32-row block, its half
+            const int i = (warp - 12) >> 1, j = (warp - 12) & 1;  // 32-row block, its half
             const int g = lane >> 2, tt = lane & 3;
             int st = 0;
             uint32_t phase = 0;
@@ -490,7 +536,7 @@ cudaError_t launch_tc(const CUtensorMap &map, const MatmulArgs &a, const TcShape
     }
     const int64_t pairs = device_sm_count() / 2;
     const unsigned grid = static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs));
-    matmul_tc_kernel<T, BITS><<<grid, BITS == 16 ? 256 : 512, s.smem, st>>>(map, a, s, status);
+    matmul_tc_kernel<T, BITS><<<grid, BITS == 16 ? 384 : 640, s.smem, st>>>(map, a, s, status);
     return cudaGetLastError();
 }
 
