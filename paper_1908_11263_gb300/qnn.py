@@ -75,6 +75,8 @@ def library_path() -> str:
 def load(build_if_missing: bool = False):
     """Load libqnn.so (building it first only when asked)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
@@ -173,6 +175,17 @@ def _stream(stream):
     if stream is None:
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+# The current stream's handle without building a Stream object (three microseconds a call on the GB300 host), where
+# this torch has the function.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _stream_of(stream, device):
+    """Handle of `stream`, or of the device's current stream."""
+    return _raw_stream(device.index) if stream is None else stream.cuda_stream
 
 
 def _dev(t: torch.Tensor, dtype, name):
@@ -504,6 +517,16 @@ def unpack_subbyte(src, bits, signed, *, out=None, stream=None):
 
 def _rows(t: torch.Tensor, dtype, name, shape=None, device=None):
     """A CUDA matrix with contiguous columns and any row stride; returns (pointer, row stride)."""
+    if t.dtype is dtype and t.is_cuda and (device is None or t.device == device):
+        s = t.shape
+        if len(s) == 2 and (shape is None or s == shape):
+            ld, step = t.stride()
+            if step == 1 and ld >= s[1]:
+                return t.data_ptr(), ld
+    return _rows_slow(t, dtype, name, shape, device)
+
+
+def _rows_slow(t, dtype, name, shape, device):
     if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{name} must be a CUDA tensor" + ("" if device is None else f" on {device}"))
     if t.dtype != dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
@@ -521,13 +544,26 @@ def _param(t, dtype, name, shape, device):
     """An optional contiguous parameter; returns its pointer or None."""
     if t is None:
         return None
+    if t.dtype is dtype and t.device == device and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
     if t.device != device:
         raise ValueError(f"{name} must be on {device}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _run_with_workspace(call, size, device, stream):
+    """call(pointer, bytes) with the workspace that this device and stream have; where the library says that it is too
+    small (nothing is queued then), with one of size() bytes."""
+    handle = _stream_of(stream, device)
+    ws = _workspaces.get((device.index, handle))
+    st = call(None, 0, handle) if ws is None else call(ws.data_ptr(), ws.numel(), handle)
+    if st == QNN_EWORKSPACE:
+        need = size()
+        ws = _workspace(need, device, stream)
+        st = call(_ptr(ws), need, handle)
+    return st
 
 
 def _float_dtype(t, name):
@@ -555,39 +591,55 @@ def block_norm(x, residual=None, *, pre_weight=None, pre_bias=None, pre_norm=Tru
     code = _float_dtype(x, "x")
     if kind not in _NORM_KINDS:
         raise ValueError(f"kind must be 'rms' or 'layer', got {kind!r}")
-    px, ldx = _rows(x, x.dtype, "x")
-    dev, (t, d) = x.device, x.shape
-    rdtype, pres, ldres = x.dtype, None, d
+    dtype = x.dtype
+    px, ldx = _rows(x, dtype, "x")
+    dev, shape = x.device, x.shape
+    t, d = shape
+    row = shape[1:]
+    rdtype, pres, ldres = dtype, None, d
     if residual is not None:
-        pres, ldres = _rows(residual, (x.dtype, torch.float32), "residual", (t, d), dev)
         rdtype = residual.dtype
+        if rdtype is not dtype and rdtype is not torch.float32:
+            raise TypeError(f"residual must have x's dtype or float32, got {rdtype}")
+        pres, ldres = _rows(residual, rdtype, "residual", shape, dev)
     elif residual_out is not None:
         rdtype = residual_out.dtype
-        if rdtype not in (x.dtype, torch.float32):
+        if rdtype not in (dtype, torch.float32):
             raise TypeError(f"residual_out must have x's dtype or float32, got {rdtype}")
-    params = [p for p in (gate, post_weight, post_bias, pre_weight, pre_bias) if p is not None]
-    pdtype = params[0].dtype if params else x.dtype
-    if pdtype not in (x.dtype, torch.float32):
-        raise TypeError(f"gate, weights and biases must have x's dtype or float32, got {pdtype}")
-    gates = 1 if gate is None or gate.dim() == 1 else gate.shape[0]
-    if gate is not None and (gates == 0 or t % gates):
-        raise ValueError(f"{t} rows do not split evenly over {gates} gate rows")
-    pgate = _param(gate, pdtype, "gate", (d,) if gate is not None and gate.dim() == 1 else (gates, d), dev)
-    ppw, ppb = _param(post_weight, pdtype, "post_weight", (d,), dev), _param(post_bias, pdtype, "post_bias", (d,), dev)
-    pw, pb = _param(pre_weight, pdtype, "pre_weight", (d,), dev), _param(pre_bias, pdtype, "pre_bias", (d,), dev)
+    pdtype = dtype
+    for p in (gate, post_weight, post_bias, pre_weight, pre_bias):
+        if p is not None:
+            pdtype = p.dtype
+            if pdtype is not dtype and pdtype is not torch.float32:
+                raise TypeError(f"gate, weights and biases must have x's dtype or float32, got {pdtype}")
+            break
+    gates, pgate = 1, None
+    if gate is not None:
+        if gate.dim() == 1:
+            pgate = _param(gate, pdtype, "gate", row, dev)
+        else:
+            gates = gate.shape[0]
+            if gates == 0 or t % gates:
+                raise ValueError(f"{t} rows do not split evenly over {gates} gate rows")
+            pgate = _param(gate, pdtype, "gate", (gates, d), dev)
+    ppw, ppb = _param(post_weight, pdtype, "post_weight", row, dev), _param(post_bias, pdtype, "post_bias", row, dev)
+    pw, pb = _param(pre_weight, pdtype, "pre_weight", row, dev), _param(pre_bias, pdtype, "pre_bias", row, dev)
     if residual_out is None:
-        residual_out = torch.empty((t, d), dtype=rdtype, device=dev)
-    pr, ldr = _rows(residual_out, rdtype, "residual_out", (t, d), dev)
-    ph, ldh = None, d
-    if pre_norm:
-        if out is None:
-            out = torch.empty((t, d), dtype=x.dtype, device=dev)
-        ph, ldh = _rows(out, x.dtype, "out", (t, d), dev)
+        residual_out = torch.empty(shape, dtype=rdtype, device=dev)
+        pr, ldr = residual_out.data_ptr(), d
     else:
+        pr, ldr = _rows(residual_out, rdtype, "residual_out", shape, dev)
+    ph, ldh = None, d
+    if not pre_norm:
         out = None
+    elif out is None:
+        out = torch.empty(shape, dtype=dtype, device=dev)
+        ph = out.data_ptr()
+    else:
+        ph, ldh = _rows(out, dtype, "out", shape, dev)
     desc = NormDesc(ctypes.sizeof(NormDesc), _NORM_KINDS[kind], code, _DTYPES[rdtype], _DTYPES[pdtype], int(bool(post_norm)),
                     gates, d, t, ldx, ldres, ldr, ldh, scale, eps)
-    st = load().qnn_block_norm(ctypes.byref(desc), px, pres, pgate, ppw, ppb, pw, pb, pr, ph, _stream(stream))
+    st = load().qnn_block_norm(ctypes.byref(desc), px, pres, pgate, ppw, ppb, pw, pb, pr, ph, _stream_of(stream, dev))
     _check(st, "qnn_block_norm")
     return residual_out, out
 
@@ -612,7 +664,8 @@ def route_topk(logits, k, *, score="softmax", bias=None, groups=1, top_groups=No
     ids = torch.empty((t, max(k, 0)), dtype=torch.int32, device=dev)
     desc = RouteDesc(ctypes.sizeof(RouteDesc), code, e, k, _SCORES[score], groups, groups if top_groups is None else top_groups,
                      _GROUP_SCORES[group_score], int(bool(renormalise)), scale, t, ld)
-    st = load().qnn_route_topk(ctypes.byref(desc), p, pbias, weights.data_ptr(), ids.data_ptr(), _stream(stream))
+    st = load().qnn_route_topk(ctypes.byref(desc), p, pbias, weights.data_ptr(), ids.data_ptr(),
+                               _stream_of(stream, dev))
     _check(st, "qnn_route_topk")
     return weights, ids
 
@@ -620,13 +673,30 @@ def route_topk(logits, k, *, score="softmax", bias=None, groups=1, top_groups=No
 class ExpertPlan:
     """Which slots (token * top + choice) each expert serves (qnn_expert_plan): `offsets` int32 [experts + 1], `order`
     int32 [slots] (the slot at each place, -1 after the last) and `position` int32 [tokens, top] (the place of each
-    slot, -1 for one that goes to no expert)."""
+    slot, -1 for one that goes to no expert).  The three are views of one buffer."""
 
-    __slots__ = ("tokens", "top", "experts", "offsets", "order", "position")
+    __slots__ = ("tokens", "top", "experts", "device", "_buffer", "_offsets", "_order", "_position")
 
-    def __init__(self, tokens, top, experts, offsets, order, position):
-        self.tokens, self.top, self.experts = tokens, top, experts
-        self.offsets, self.order, self.position = offsets, order, position
+    def __init__(self, tokens, top, experts, device):
+        self.tokens, self.top, self.experts, self.device = tokens, top, experts, device
+        slots = tokens * top
+        self._buffer = torch.empty(2 * slots + experts + 1, dtype=torch.int32, device=device)
+        self._order = self._buffer.data_ptr()  # pointers
+        self._position = self._order + 4 * slots
+        self._offsets = self._position + 4 * slots
+
+    @property
+    def order(self):
+        return self._buffer[:self.tokens * self.top]
+
+    @property
+    def position(self):
+        slots = self.tokens * self.top
+        return self._buffer[slots:2 * slots].view(self.tokens, self.top)
+
+    @property
+    def offsets(self):
+        return self._buffer[2 * self.tokens * self.top:]
 
 
 def expert_plan(ids, experts, *, stream=None) -> ExpertPlan:
@@ -634,17 +704,20 @@ def expert_plan(ids, experts, *, stream=None) -> ExpertPlan:
     _dev(ids, torch.int32, "ids")
     if ids.dim() != 2:
         raise ValueError(f"ids must have shape [tokens, top], got {tuple(ids.shape)}")
-    dev, slots = ids.device, ids.numel()
-    lib, need = load(), ctypes.c_size_t(0)
-    _check(lib.qnn_expert_plan_workspace_size(slots, experts, ctypes.byref(need)), "qnn_expert_plan_workspace_size")
-    ws = _workspace(need.value, dev, stream)
-    offsets = torch.empty(experts + 1, dtype=torch.int32, device=dev)
-    order = torch.empty(slots, dtype=torch.int32, device=dev)
-    position = torch.empty(ids.shape, dtype=torch.int32, device=dev)
-    st = lib.qnn_expert_plan(ids.data_ptr(), slots, experts, offsets.data_ptr(), order.data_ptr(), position.data_ptr(),
-                             _ptr(ws), need.value, _stream(stream))
+    if experts <= 0:
+        raise QnnError(QNN_EINVAL, "qnn_expert_plan")
+    lib, p, (tokens, top) = load(), ids.data_ptr(), ids.shape
+    plan = ExpertPlan(tokens, top, experts, ids.device)
+
+    def size():
+        need = ctypes.c_size_t(0)
+        _check(lib.qnn_expert_plan_workspace_size(tokens * top, experts, ctypes.byref(need)), "qnn_expert_plan_workspace_size")
+        return need.value
+
+    st = _run_with_workspace(lambda ws, n, handle: lib.qnn_expert_plan(
+        p, tokens * top, experts, plan._offsets, plan._order, plan._position, ws, n, handle), size, plan.device, stream)
     _check(st, "qnn_expert_plan")
-    return ExpertPlan(ids.shape[0], ids.shape[1], experts, offsets, order, position)
+    return plan
 
 
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
@@ -684,6 +757,7 @@ class _Prepared:
         _check(lib.qnn_matmul_image_size(self._desc, ctypes.byref(need)), "qnn_matmul_image_size")
         self.nbytes = need.value
         self.image = torch.empty(self.nbytes, dtype=torch.uint8, device=w.device)
+        self._image = self.image.data_ptr()
         st = lib.qnn_matmul_prepare(self._desc, _ptr(w), pscale, pbias, self.image.data_ptr(), self.nbytes, _stream(stream))
         _check(st, "qnn_matmul_prepare")
 
@@ -700,21 +774,33 @@ class PreparedMatmul(_Prepared):
 
     def __call__(self, x, residual=None, *, out=None, out_dtype=None, stream=None):
         """x [t, k] -> [t, m] in x's dtype, or float32 with out_dtype=torch.float32.  out may be the residual."""
-        px, ldx = _rows(x, self.dtype, "x", None, self.device)
-        t = x.shape[0]
-        if x.shape[1] != self.k:
-            raise ValueError(f"x must have {self.k} columns, got {x.shape[1]}")
-        pres, ldres = (None, self.m) if residual is None else _rows(residual, self.dtype, "residual", (t, self.m), self.device)
+        dtype, dev, m = self.dtype, self.device, self.m
+        px, ldx = _rows(x, dtype, "x", None, dev)
+        t, k = x.shape
+        if k != self.k:
+            raise ValueError(f"x must have {self.k} columns, got {k}")
+        pres, ldres = (None, m) if residual is None else _rows(residual, dtype, "residual", (t, m), dev)
         if out is None:
-            out = torch.empty((t, self.m), dtype=self.dtype if out_dtype is None else out_dtype, device=self.device)
-        elif out_dtype not in (None, out.dtype):
-            raise TypeError(f"out has dtype {out.dtype}, not {out_dtype}")
-        po, ldo = _rows(out, (self.dtype, torch.float32), "out", (t, self.m), self.device)
-        lib, need = load(), ctypes.c_size_t(0)
-        _check(lib.qnn_matmul_workspace_size(self._desc, t, px, ldx, ctypes.byref(need)), "qnn_matmul_workspace_size")
-        ws = _workspace(need.value, self.device, stream)
-        st = lib.qnn_matmul_run(self._desc, self.image.data_ptr(), self.nbytes, t, px, ldx, pres, ldres, po, ldo,
-                                int(out.dtype == torch.float32), _ptr(ws), need.value, _stream(stream))
+            odtype = dtype if out_dtype is None else out_dtype
+            if odtype is not dtype and odtype is not torch.float32:
+                raise TypeError(f"out_dtype must be {dtype} or float32, got {odtype}")
+            out = torch.empty((t, m), dtype=odtype, device=dev)
+            po, ldo = out.data_ptr(), m
+        else:
+            odtype = out.dtype
+            if out_dtype not in (None, odtype):
+                raise TypeError(f"out has dtype {odtype}, not {out_dtype}")
+            po, ldo = _rows(out, dtype if odtype is dtype else torch.float32, "out", (t, m), dev)
+        lib = load()
+
+        def size():
+            need = ctypes.c_size_t(0)
+            _check(lib.qnn_matmul_workspace_size(self._desc, t, px, ldx, ctypes.byref(need)), "qnn_matmul_workspace_size")
+            return need.value
+
+        wide = int(odtype is torch.float32)
+        st = _run_with_workspace(lambda ws, n, handle: lib.qnn_matmul_run(
+            self._desc, self._image, self.nbytes, t, px, ldx, pres, ldres, po, ldo, wide, ws, n, handle), size, dev, stream)
         _check(st, "qnn_matmul_run")
         return out
 
@@ -728,48 +814,52 @@ class PreparedExperts(_Prepared):
     def _check_plan(self, plan):
         if plan.experts != self.experts:
             raise ValueError(f"the plan is over {plan.experts} experts, the weights over {self.experts}")
-        if plan.order.device != self.device:
+        if plan.device != self.device:
             raise ValueError(f"the plan must be on {self.device}")
 
-    def _workspace(self, plan, combine, px, ldx, stream):
-        need = ctypes.c_size_t(0)
-        _check(load().qnn_experts_workspace_size(self._desc, plan.tokens, plan.top, combine, px, ldx, ctypes.byref(need)),
-               "qnn_experts_workspace_size")
-        return _workspace(need.value, self.device, stream), need.value
+    def _run(self, call, plan, combine, px, ldx, stream):
+        def size():
+            need = ctypes.c_size_t(0)
+            _check(load().qnn_experts_workspace_size(self._desc, plan.tokens, plan.top, combine, px, ldx, ctypes.byref(need)),
+                   "qnn_experts_workspace_size")
+            return need.value
+
+        _check(_run_with_workspace(call, size, self.device, stream), "qnn_experts_combine" if combine else "qnn_experts_dispatch")
 
     def dispatch(self, x, plan, *, out=None, stream=None):
         """Each place's token through its expert (qnn_experts_dispatch): x [tokens, k] -> [tokens * top, m] in the
         plan's order; rows after the last place are zero."""
         self._check_plan(plan)
-        px, ldx = _rows(x, self.dtype, "x", (plan.tokens, self.k), self.device)
+        tokens, top = plan.tokens, plan.top
+        px, ldx = _rows(x, self.dtype, "x", (tokens, self.k), self.device)
+        shape = (tokens * top, self.m)
         if out is None:
-            out = torch.empty((plan.tokens * plan.top, self.m), dtype=self.dtype, device=self.device)
-        po, ldo = _rows(out, self.dtype, "out", (plan.tokens * plan.top, self.m), self.device)
-        ws, need = self._workspace(plan, 0, px, ldx, stream)
-        st = load().qnn_experts_dispatch(self._desc, self.image.data_ptr(), self.nbytes, plan.tokens, plan.top,
-                                         plan.offsets.data_ptr(), plan.order.data_ptr(), px, ldx, po, ldo, _ptr(ws), need,
-                                         _stream(stream))
-        _check(st, "qnn_experts_dispatch")
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        po, ldo = _rows(out, self.dtype, "out", shape, self.device)
+        lib = load()
+        self._run(lambda ws, n, handle: lib.qnn_experts_dispatch(
+            self._desc, self._image, self.nbytes, tokens, top, plan._offsets, plan._order, px, ldx, po, ldo, ws, n, handle),
+            plan, 0, px, ldx, stream)
         return out
 
     def combine(self, x, plan, weights, residual=None, *, out=None, stream=None):
         """The places' rows through their experts and back to the tokens (qnn_experts_combine):
         y[t] = residual[t] + sum_j weights[t, j] * product(position[t, j]); x [tokens * top, k] -> [tokens, m]."""
         self._check_plan(plan)
-        px, ldx = _rows(x, self.dtype, "x", (plan.tokens * plan.top, self.k), self.device)
-        pw = _param(weights, torch.float32, "weights", (plan.tokens, plan.top), self.device)
+        tokens, top = plan.tokens, plan.top
+        px, ldx = _rows(x, self.dtype, "x", (tokens * top, self.k), self.device)
+        pw = _param(weights, torch.float32, "weights", (tokens, top), self.device)
         if pw is None:
             raise ValueError("weights are needed")
-        shape = (plan.tokens, self.m)
+        shape = (tokens, self.m)
         pres, ldres = (None, self.m) if residual is None else _rows(residual, self.dtype, "residual", shape, self.device)
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
         po, ldo = _rows(out, self.dtype, "out", shape, self.device)
-        ws, need = self._workspace(plan, 1, px, ldx, stream)
-        st = load().qnn_experts_combine(self._desc, self.image.data_ptr(), self.nbytes, plan.tokens, plan.top,
-                                        plan.offsets.data_ptr(), plan.position.data_ptr(), pw, px, ldx, pres, ldres, po, ldo,
-                                        _ptr(ws), need, _stream(stream))
-        _check(st, "qnn_experts_combine")
+        lib = load()
+        self._run(lambda ws, n, handle: lib.qnn_experts_combine(
+            self._desc, self._image, self.nbytes, tokens, top, plan._offsets, plan._position, pw, px, ldx, pres, ldres, po,
+            ldo, ws, n, handle), plan, 1, px, ldx, stream)
         return out
 
 
