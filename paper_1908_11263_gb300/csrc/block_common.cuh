@@ -7,7 +7,38 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include "device.cuh"
+
 namespace qnn {
+
+// Launches a kernel that may start while its predecessor in the stream still runs.  Every such kernel calls pdl_begin()
+// in all of its threads before it touches global memory: it lets its own successor start, then waits until the
+// predecessor has ended and its writes are visible.  Only the launch latency and the kernel's set-up overlap.
+template <typename... P, typename... A>
+inline cudaError_t launch_pdl(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
+__device__ __forceinline__ void pdl_begin()
+{
+    pdl_trigger();
+    pdl_wait();
+}
 
 template <typename T>
 __device__ __forceinline__ float to_f32(T v);

@@ -150,53 +150,36 @@ __device__ __forceinline__ void finish(const MatmulArgs &a, int64_t row, int64_t
         static_cast<T *>(a.y)[row * a.ldy + col] = from_f32<T>(v);
 }
 
-// Tile `u` of the experts' places, `tile` places at most to a tile: {expert, first place, places}, or expert -1 after
-// the last.  All lanes of a warp call it together.
-struct ExpertTile {
-    int expert, first, count;
-};
-
-__device__ __forceinline__ ExpertTile expert_tile(const int32_t *offsets, int experts, int tile, int u)
+// tab[e] = tiles of `tile` places before expert e, tab[experts] = all of them.  A whole warp calls it.
+__device__ __forceinline__ void expert_tiles(const int32_t *offsets, int experts, int tile, int *tab)
 {
     const int lane = threadIdx.x & 31;
-    const int per = (experts + 31) / 32;
-    const int lo = min(lane * per, experts), hi = min(lo + per, experts);
-    int mine = 0, prev = offsets[lo];
-    for (int e = lo; e < hi; ++e) {
-        const int next = offsets[e + 1];
-        mine += (next - prev + tile - 1) / tile;
-        prev = next;
-    }
-    int inc = mine;
+    int before = 0;
+    for (int base = 0; base < experts; base += 32) {
+        const int e = base + lane;
+        const int n = e < experts ? (offsets[e + 1] - offsets[e] + tile - 1) / tile : 0;
+        int inc = n;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += v;
-    }
-    ExpertTile r = {-1, 0, 0};
-    int left = u - (inc - mine);
-    const bool here = left >= 0 && left < mine;
-    if (here) {
-        prev = offsets[lo];
-        for (int e = lo; e < hi; ++e) {
-            const int next = offsets[e + 1];
-            const int n = (next - prev + tile - 1) / tile;
-            if (left < n) {
-                r.expert = e;
-                r.first = prev + left * tile;
-                r.count = min(tile, next - r.first);
-                break;
-            }
-            left -= n;
-            prev = next;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += v;
         }
+        if (e < experts) tab[e] = before + inc - n;
+        before += __shfl_sync(0xffffffffu, inc, 31);
     }
-    const uint32_t who = __ballot_sync(0xffffffffu, here);
-    const int src = who ? __ffs(who) - 1 : 0;
-    r.expert = __shfl_sync(0xffffffffu, r.expert, src);
-    r.first = __shfl_sync(0xffffffffu, r.first, src);
-    r.count = __shfl_sync(0xffffffffu, r.count, src);
-    return r;
+    if (lane == 0) tab[experts] = before;
+}
+
+// The expert of tile `u`: the last one whose first tile is at most u.
+__device__ __forceinline__ int find_expert(const int *tab, int experts, int u)
+{
+    int lo = 0, hi = experts;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (tab[mid] <= u) lo = mid;
+        else hi = mid;
+    }
+    return lo;
 }
 
 }  // namespace qnn

@@ -116,6 +116,7 @@ template <typename T>
 __global__ void combine_kernel(const CombineArgs a)
 {
     const int64_t t = blockIdx.x;
+    pdl_begin();
     for (int c = (blockIdx.y * blockDim.x + threadIdx.x) * 4; c < a.m; c += gridDim.y * blockDim.x * 4) {
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int j = 0; j < a.top; ++j) {
@@ -142,6 +143,7 @@ __global__ void combine_kernel(const CombineArgs a)
 __global__ void align_rows_kernel(const uint16_t *src, int64_t lds, uint16_t *dst, int64_t ldd, int cols)
 {
     const int64_t row = blockIdx.x;
+    pdl_begin();
     for (int c = threadIdx.x; c < cols; c += blockDim.x) dst[row * ldd + c] = src[row * lds + c];
 }
 
@@ -150,9 +152,8 @@ __global__ void align_rows_kernel(const uint16_t *src, int64_t lds, uint16_t *ds
 cudaError_t launch_align_rows(const void *src, int64_t lds, void *dst, int64_t ldd, int64_t rows, int cols, cudaStream_t st)
 {
     if (rows == 0) return cudaSuccess;
-    align_rows_kernel<<<static_cast<unsigned>(rows), 256, 0, st>>>(static_cast<const uint16_t *>(src), lds,
-                                                                 static_cast<uint16_t *>(dst), ldd, cols);
-    return cudaGetLastError();
+    return launch_pdl(align_rows_kernel, dim3(static_cast<unsigned>(rows)), 256, 0, st, 1, static_cast<const uint16_t *>(src), lds,
+                      static_cast<uint16_t *>(dst), ldd, cols);
 }
 
 cudaError_t launch_matmul_prep(const qnn_matmul_desc &d, const void *w, const float *scale, const float *bias,
@@ -181,9 +182,8 @@ cudaError_t launch_combine(int dtype, const float *z, int64_t ldz, const float *
     if (tokens == 0) return cudaSuccess;
     const CombineArgs a = {z, weights, position, residual, y, ldz, ldres, ldy, tokens, m, top};
     const dim3 grid(static_cast<unsigned>(tokens), (m + 1023) / 1024);
-    if (dtype == QNN_F16) combine_kernel<__half><<<grid, 256, 0, st>>>(a);
-    else combine_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
-    return cudaGetLastError();
+    return dtype == QNN_F16 ? launch_pdl(combine_kernel<__half>, grid, 256, 0, st, 1, a)
+                            : launch_pdl(combine_kernel<__nv_bfloat16>, grid, 256, 0, st, 1, a);
 }
 
 }  // namespace qnn

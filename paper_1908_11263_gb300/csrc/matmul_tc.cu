@@ -222,12 +222,7 @@ __device__ __forceinline__ Tile tile_at(const MatmulArgs &a, const TcShape &s, c
     const int u = id / s.mt;
     t.expert = 0;
     if (a.offsets) {
-        int lo = 0, hi = a.experts;  // the last expert whose first tile is at most u
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (tab[mid] <= u) lo = mid;
-            else hi = mid;
-        }
+        const int lo = find_expert(tab, a.experts, u);
         t.expert = lo;
         const int begin = a.offsets[lo], end = a.offsets[lo + 1];
         t.first = begin + static_cast<int64_t>(u - tab[lo]) * s.nt;
@@ -269,26 +264,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 6
         }
         fence_mbar_init();
     }
+    pdl_begin();
     if (warp == 3) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(s.cols)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        if (a.offsets) {
-            int before = 0;
-            for (int base = 0; base < a.experts; base += 32) {
-                const int e = base + lane;
-                const int n = e < a.experts ? (a.offsets[e + 1] - a.offsets[e] + s.nt - 1) / s.nt : 0;
-                int inc = n;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int v = __shfl_up_sync(0xffffffffu, inc, o);
-                    if (lane >= o) inc += v;
-                }
-                if (e < a.experts) tab[e] = before + inc - n;
-                before += __shfl_sync(0xffffffffu, inc, 31);
-            }
-            if (lane == 0) tab[a.experts] = before;
-        }
+        if (a.offsets) expert_tiles(a.offsets, a.experts, s.nt, tab);
         tc_fence_before();
     }
     __syncthreads();
@@ -536,8 +517,7 @@ cudaError_t launch_tc(const CUtensorMap &map, const MatmulArgs &a, const TcShape
     }
     const int64_t pairs = device_sm_count() / 2;
     const unsigned grid = static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs));
-    matmul_tc_kernel<T, BITS><<<grid, BITS == 16 ? 384 : 640, s.smem, st>>>(map, a, s, status);
-    return cudaGetLastError();
+    return launch_pdl(matmul_tc_kernel<T, BITS>, dim3(grid), BITS == 16 ? 384 : 640, s.smem, st, 1, map, a, s, status);
 }
 
 template <typename T>

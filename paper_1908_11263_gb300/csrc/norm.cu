@@ -11,6 +11,7 @@
 // over the centred values, not a difference of two sums that would cancel.
 #include "block_common.cuh"
 #include "block_internal.h"
+#include "device.cuh"
 
 namespace qnn {
 namespace {
@@ -24,56 +25,95 @@ struct NormArgs {
     float scale, eps;
 };
 
-// Sum over the block.  Each reduction uses its own row of `part`, so one barrier a reduction is enough.
+// Sum over the block.  Each reduction uses its own row of `part` (zeros past the block's warps), so one barrier a
+// reduction is enough; every thread adds the warps' sums itself, in the same order.
 __device__ __forceinline__ float block_sum(float v, float *part)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    const int warps = blockDim.x >> 5;
-    if (warps == 1) return v;
+    if (blockDim.x == 32) return v;
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
-    float s = static_cast<int>(threadIdx.x & 31) < warps ? part[threadIdx.x & 31] : 0.f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    float s = 0.f;
+    for (int w = 0; w < static_cast<int>(blockDim.x >> 5); w += 4) {
+        const float4 q = *reinterpret_cast<const float4 *>(part + w);
+        s += (q.x + q.y) + (q.z + q.w);
+    }
     return s;
 }
 
-// A thread's values of a row.  VEC: chunks of 8 neighbours, chunk i at (i * threads + tid) * 8.  Otherwise
-// value e of the thread is element e * threads + tid, so that neighbouring lanes touch neighbouring elements
-// whatever the alignment.
-template <bool VEC, int ITEMS>
+template <typename T>
+__device__ __forceinline__ void load4(const T *p, float *v)
+{
+    if constexpr (sizeof(T) == 4) {
+        const float4 q = *reinterpret_cast<const float4 *>(p);
+        v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    } else {
+        const uint2 q = *reinterpret_cast<const uint2 *>(p);
+        const float2 a = unpack2<T>(q.x), b = unpack2<T>(q.y);
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T *p, const float *v)
+{
+    if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+        *reinterpret_cast<uint2 *>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+}
+
+// A thread's values of a row, eight to an item.  VEC = 8: eight neighbours, one 16-byte access of 16-bit values.
+// VEC = 4: two runs of four neighbours, a whole block's threads apart, for rows with a 32-bit tensor among them: its
+// 16-byte accesses then cover whole sectors (two halves of 32 bytes a lane made each store a partial one).  VEC = 1:
+// single elements a block's threads apart, so that neighbouring lanes touch neighbouring elements whatever the alignment.
+// EXACT: rows are whole vectors.
+template <int VEC, int ITEMS, bool EXACT = false>
 struct Row {
     static __device__ __forceinline__ int at(int i, int j)
     {
-        return VEC ? (i * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 8 + j
-                   : (i * 8 + j) * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x);
+        return ((i * 8 + j) / VEC * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * VEC + j % VEC;
     }
 
     template <typename T>
     static __device__ __forceinline__ void load(const T *p, int i, int d, float (&v)[8])
     {
-        if (VEC && at(i, 7) < d) {
-            Raw8<T> q;
-            q.load(p + at(i, 0));
-            q.get(v);
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = at(i, j) < d ? to_f32<T>(p[at(i, j)]) : 0.f;
+        for (int h = 0; h < 8; h += VEC) {
+            if (VEC > 1 && (EXACT ? at(i, h) : at(i, h + VEC - 1)) < d) {
+                if constexpr (VEC == 8) {
+                    Raw8<T> q;
+                    q.load(p + at(i, 0));
+                    q.get(v);
+                } else {
+                    load4(p + at(i, h), v + h);
+                }
+            } else {
+#pragma unroll
+                for (int j = h; j < h + VEC; ++j) v[j] = !EXACT && at(i, j) < d ? to_f32<T>(p[at(i, j)]) : 0.f;
+            }
         }
     }
 
     template <typename T>
     static __device__ __forceinline__ void store(T *p, int i, int d, const float (&v)[8])
     {
-        if (VEC && at(i, 7) < d) {
-            Raw8<T> q;
-            q.set(v);
-            q.store(p + at(i, 0));
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (at(i, j) < d) p[at(i, j)] = from_f32<T>(v[j]);
+        for (int h = 0; h < 8; h += VEC) {
+            if (VEC > 1 && (EXACT ? at(i, h) : at(i, h + VEC - 1)) < d) {
+                if constexpr (VEC == 8) {
+                    Raw8<T> q;
+                    q.set(v);
+                    q.store(p + at(i, 0));
+                } else {
+                    store4(p + at(i, h), v + h);
+                }
+            } else if (!EXACT) {
+#pragma unroll
+                for (int j = h; j < h + VEC; ++j)
+                    if (at(i, j) < d) p[at(i, j)] = from_f32<T>(v[j]);
+            }
         }
     }
 
@@ -104,11 +144,10 @@ struct Row {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (at(i, j) < a.d) {
-                    v[i][j] -= mean;
-                    q = fmaf(v[i][j], v[i][j], q);
-                }
+            for (int j = 0; j < 8; ++j) {
+                if (a.layer && at(i, EXACT ? j / VEC * VEC : j) < a.d) v[i][j] -= mean;  // values past the row's end stay zero
+                q = fmaf(v[i][j], v[i][j], q);
+            }
         const float f = rsqrtf(block_sum(q, part[1]) * inv_d + a.eps);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
@@ -136,11 +175,16 @@ struct Row {
     }
 };
 
-template <typename T, typename R, bool VEC, int ITEMS, int MAX_THREADS>
-__global__ void __launch_bounds__(MAX_THREADS) block_norm_kernel(const NormArgs a)
+template <typename T, typename R, int VEC, int ITEMS>
+__global__ void __launch_bounds__(1024) block_norm_kernel(const NormArgs a)
 {
-    __shared__ float part[4][32];
+    __shared__ __align__(16) float part[4][32];
     using Q = Row<VEC, ITEMS>;
+    if (threadIdx.x < 32)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[i][threadIdx.x] = 0.f;
+    __syncthreads();
+    pdl_begin();
     const int64_t row = blockIdx.x;
     const T *x = static_cast<const T *>(a.x) + row * a.ldx;
     float v[ITEMS][8], res[ITEMS][8];
@@ -181,30 +225,202 @@ __global__ void __launch_bounds__(MAX_THREADS) block_norm_kernel(const NormArgs 
     }
 }
 
+// The same over many rows: a block that stays on its SM and takes every gridDim-th row, fed by bulk copies `stages` rows
+// ahead, so that the loads of the next rows run under the reductions of this one (with a block a row, every SM waits for
+// its rows' loads, then for their reductions).  Rows are whole 16-byte vectors here.
+// Weights and a gate in the type of x stay in registers from row to row, as packed words.
+template <typename T, int VEC>
+struct Held {
+    uint32_t w[2][4];
+    __device__ __forceinline__ void load(const void *p, int64_t off, int d)
+    {
+        const uint32_t *q = reinterpret_cast<const uint32_t *>(static_cast<const T *>(p) + off);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int h = 0; h < 8; h += VEC) {
+                if (Row<VEC, 2>::at(i, h) >= d) {  // values past the row's end are zero and stay zero
+                    for (int j = h / 2; j < (h + VEC) / 2; ++j) w[i][j] = 0u;
+                    continue;
+                }
+                if constexpr (VEC == 8) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(q + Row<VEC, 2>::at(i, 0) / 2);
+                    w[i][0] = u.x; w[i][1] = u.y; w[i][2] = u.z; w[i][3] = u.w;
+                } else {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(q + Row<VEC, 2>::at(i, h) / 2);
+                    w[i][h / 2] = u.x; w[i][h / 2 + 1] = u.y;
+                }
+            }
+    }
+    __device__ __forceinline__ void scale(float (&v)[2][8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = unpack2<T>(w[i][j]);
+                v[i][2 * j] *= f.x;
+                v[i][2 * j + 1] *= f.y;
+            }
+    }
+};
+template <int VEC>
+struct Held<float, VEC> {  // 32-bit rows: read again for each row
+    __device__ __forceinline__ void load(const void *, int64_t, int) {}
+    __device__ __forceinline__ void scale(float (&)[2][8]) const {}
+};
+
+struct StreamShape {
+    int stages;
+    uint32_t x_bytes, res_bytes;  // of a row; res_bytes 0 without a residual
+};
+
+constexpr int kNormItems = 2;  // 16 values a thread
+
+template <typename T, typename R, int VEC>
+__global__ void __launch_bounds__(1024) block_norm_stream_kernel(const NormArgs a, const StreamShape s, int64_t t, int *status)
+{
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ __align__(16) float part[2][4][32];
+    __shared__ uint64_t full[8];
+    using Q = Row<VEC, kNormItems, true>;
+    const uint32_t stage_bytes = s.x_bytes + s.res_bytes;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < s.stages; ++i) mbar_init(full + i, 1);
+        fence_mbar_init();
+    }
+    if (threadIdx.x < 32)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[i >> 2][i & 3][threadIdx.x] = 0.f;
+    __syncthreads();
+    pdl_begin();
+    auto fetch = [&](int64_t row, int st) {
+        uint8_t *dst = ring + st * stage_bytes;
+        mbar_arrive_expect_tx(full + st, stage_bytes);
+        if (s.res_bytes) bulk_g2s(dst + s.x_bytes, static_cast<const R *>(a.residual) + row * a.ldres, s.res_bytes, full + st);
+        bulk_g2s(dst, static_cast<const T *>(a.x) + row * a.ldx, s.x_bytes, full + st);
+    };
+    if (threadIdx.x == 0)
+        for (int i = 0; i < s.stages; ++i) {
+            const int64_t row = blockIdx.x + static_cast<int64_t>(i) * gridDim.x;
+            if (row < t) fetch(row, i);
+        }
+    const bool hold = sizeof(T) == 2 && !a.param_f32;
+    const bool post_w = a.post && a.post_w;
+    Held<T, VEC> hold_post, hold_gate, hold_pre;
+    if (hold) {
+        if (post_w) hold_post.load(a.post_w, 0, a.d);
+        if (a.h && a.pre_w) hold_pre.load(a.pre_w, 0, a.d);
+    }
+    int64_t held_gate = -1;
+    int st = 0, n = 0;
+    uint32_t phase = 0;
+    for (int64_t row = blockIdx.x; row < t; row += gridDim.x, ++n) {
+        const int64_t gate_row = a.gate ? static_cast<uint32_t>(row) / static_cast<uint32_t>(a.rows_per_gate) : -1;
+        if (hold && gate_row != held_gate) {
+            hold_gate.load(a.gate, gate_row * a.d, a.d);
+            held_gate = gate_row;
+        }
+        // a thread that gives up goes on (the status word tells the caller), so that the block's barriers stay whole
+        mbar_wait_warp(full + st, phase, status);
+        const T *x = reinterpret_cast<const T *>(ring + st * stage_bytes);
+        const R *res = reinterpret_cast<const R *>(ring + st * stage_bytes + s.x_bytes);
+        float v[kNormItems][8];
+#pragma unroll
+        for (int i = 0; i < kNormItems; ++i) Q::load(x, i, a.d, v[i]);
+        if (a.post) {
+            Q::normalise(v, a, part[n & 1]);
+            if (post_w && hold) hold_post.scale(v);
+            Q::template affine<T>(v, hold ? nullptr : a.post_w, a.post_b, a);
+        }
+        if (a.gate && hold) hold_gate.scale(v);
+#pragma unroll
+        for (int i = 0; i < kNormItems; ++i) {
+            float g[8];
+            if (a.gate && !hold) {
+                Q::template param<T>(a.gate, a.param_f32, gate_row * a.d, i, a.d, g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
+            }
+            if (s.res_bytes) {
+                Q::load(res, i, a.d, g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = fmaf(a.scale, v[i][j], g[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] *= a.scale;
+            }
+        }
+        if (a.r) {
+            R *p = static_cast<R *>(a.r) + row * a.ldr;
+#pragma unroll
+            for (int i = 0; i < kNormItems; ++i) Q::store(p, i, a.d, v[i]);
+        }
+        if (a.h)
+            Q::normalise(v, a, part[n & 1] + 2);
+        else
+            __syncthreads();
+        // every thread is past its reads of the stage: the reduction's barrier (or the one above) lies between
+        const int64_t next = row + static_cast<int64_t>(s.stages) * gridDim.x;
+        if (threadIdx.x == 0 && next < t) fetch(next, st);
+        if (a.h) {
+            if (a.pre_w && hold) hold_pre.scale(v);
+            Q::template affine<T>(v, hold ? nullptr : a.pre_w, a.pre_b, a);
+            T *p = static_cast<T *>(a.h) + row * a.ldh;
+#pragma unroll
+            for (int i = 0; i < kNormItems; ++i) Q::store(p, i, a.d, v[i]);
+        }
+        if (++st == s.stages) {
+            st = 0;
+            phase ^= 1;
+        }
+    }
+}
+
+template <typename T, typename R, int VEC>
+cudaError_t launch_stream(const NormArgs &a, int64_t t, cudaStream_t stream, bool *taken)
+{
+    *taken = false;
+    if (a.d % 8 || a.d > 8192 * kNormItems) return cudaSuccess;
+    int *status = device_status_ptr();
+    if (!status) return cudaErrorNotSupported;
+    StreamShape s;
+    s.x_bytes = a.d * sizeof(T);
+    s.res_bytes = a.residual ? a.d * sizeof(R) : 0;
+    int threads = ((a.d + 8 * kNormItems - 1) / (8 * kNormItems) + 31) / 32 * 32;
+    if (threads < 64) threads = 64;
+    const int sms = device_sm_count();
+    const uint32_t room = 208 * 1024, stage = s.x_bytes + s.res_bytes;
+    int per_sm = 1024 / threads;
+    while (per_sm > 1 && room / per_sm < 2 * stage) --per_sm;
+    const uint32_t fit = room / per_sm / stage;
+    s.stages = fit > 4 ? 4 : static_cast<int>(fit);
+    // a few rows a block at least, or the ring does not pay for itself
+    if (s.stages < 2 || t < 3ll * per_sm * sms) return cudaSuccess;
+    const size_t smem = static_cast<size_t>(s.stages) * stage;
+    const cudaError_t e = cudaFuncSetAttribute(block_norm_stream_kernel<T, R, VEC>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(room));
+    if (e != cudaSuccess) return e;
+    *taken = true;
+    return launch_pdl(block_norm_stream_kernel<T, R, VEC>, dim3(per_sm * sms), threads, smem, stream, 1, a, s, t, status);
+}
+
 bool rows_aligned(const void *p, int64_t ld, int size)
 {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (ld * size) % 16 == 0;
 }
 
-template <typename T, typename R, bool VEC>
+template <typename T, typename R, int VEC>
 cudaError_t launch_items(const NormArgs &a, int64_t t, cudaStream_t stream)
 {
-    // Values a thread: few rows want many threads a row (latency), many rows want fewer and longer ones, which leave
-    // more loads in flight for each barrier.  At most 1024 threads.
+    // Eight values a thread up to rows of 8192, the most threads and the shortest chain; longer rows take more.
     const int chunks = (a.d + 7) / 8;
-    int items = t > 2 * device_sm_count() ? (chunks >= 1024 ? 4 : chunks >= 256 ? 2 : 1) : 1;
-    while (items < 4 && (chunks + items - 1) / items > 1024) items *= 2;
+    const int items = chunks <= 1024 ? 1 : chunks <= 2048 ? 2 : 4;
     const int threads = ((chunks + items - 1) / items + 31) / 32 * 32;
     const dim3 grid(static_cast<unsigned>(t));
-    if (items == 1)
-        block_norm_kernel<T, R, VEC, 1, 1024><<<grid, threads, 0, stream>>>(a);
-    else if (items == 2)
-        block_norm_kernel<T, R, VEC, 2, 1024><<<grid, threads, 0, stream>>>(a);
-    else if (threads <= 512)
-        block_norm_kernel<T, R, VEC, 4, 512><<<grid, threads, 0, stream>>>(a);
-    else  // rows above 16384: 64 registers a thread are all there are
-        block_norm_kernel<T, R, VEC, 4, 1024><<<grid, threads, 0, stream>>>(a);
-    return cudaGetLastError();
+    if (items == 1) return launch_pdl(block_norm_kernel<T, R, VEC, 1>, grid, threads, 0, stream, 1, a);
+    if (items == 2) return launch_pdl(block_norm_kernel<T, R, VEC, 2>, grid, threads, 0, stream, 1, a);
+    return launch_pdl(block_norm_kernel<T, R, VEC, 4>, grid, threads, 0, stream, 1, a);
 }
 
 template <typename T, typename R>
@@ -215,7 +431,11 @@ cudaError_t launch_vec(const NormArgs &a, int64_t t, cudaStream_t stream)
                      rows_aligned(a.r, a.r ? a.ldr : 0, sr) && rows_aligned(a.h, a.h ? a.ldh : 0, sx) &&
                      rows_aligned(a.gate, a.gate ? a.d : 0, sp) && rows_aligned(a.post_w, 0, sp) &&
                      rows_aligned(a.post_b, 0, sp) && rows_aligned(a.pre_w, 0, sp) && rows_aligned(a.pre_b, 0, sp);
-    return vec ? launch_items<T, R, true>(a, t, stream) : launch_items<T, R, false>(a, t, stream);
+    if (!vec) return launch_items<T, R, 1>(a, t, stream);
+    constexpr int kVec = sizeof(R) == 4 ? 4 : 8;
+    bool taken = false;
+    const cudaError_t e = launch_stream<T, R, kVec>(a, t, stream, &taken);
+    return e != cudaSuccess || taken ? e : launch_items<T, R, kVec>(a, t, stream);
 }
 
 }  // namespace

@@ -51,6 +51,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
     extern __shared__ float sm_scores[];  // one row of group_size * groups scores a warp (grouped calls only)
     const int lane = threadIdx.x & 31;
     const int64_t token = static_cast<int64_t>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5);
+    pdl_begin();
     if (token >= a.t) return;
     const T *row = static_cast<const T *>(a.logits) + token * a.ld;
 
@@ -186,6 +187,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const int32_t 
     extern __shared__ int32_t sm_plan[];
     for (int e = threadIdx.x; e < experts; e += kPlanThreads) sm_plan[e] = 0;
     __syncthreads();
+    pdl_begin();
     const int64_t begin = blockIdx.x * chunk, end = begin + chunk < slots ? begin + chunk : slots;
     for (int64_t s = begin + threadIdx.x; s < end; s += kPlanThreads) {
         const int e = expert_of(ids, s, end, experts);
@@ -206,6 +208,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int i = threadIdx.x; i < kPlanWarps * experts; i += kPlanThreads) sm_plan[i] = 0;
     __syncthreads();
+    pdl_begin();
     const int64_t begin = blockIdx.x * chunk, end = begin + chunk < slots ? begin + chunk : slots;
     const int64_t span = chunk / kPlanWarps;  // a multiple of 32
     const int64_t wb = begin + warp * span, we = wb + span < end ? wb + span : end;
@@ -287,13 +290,12 @@ cudaError_t launch_route_type(const RouteArgs &a, cudaStream_t stream)
     const int threads = kRouteWarps * 32;
     const size_t smem = a.groups > 1 ? sizeof(float) * kRouteWarps * a.e : 0;  // at most 32 KB
     const int nv = (a.e + 31) / 32;
-    if (nv <= 1) route_topk_kernel<T, 1><<<grid, threads, smem, stream>>>(a);
-    else if (nv <= 2) route_topk_kernel<T, 2><<<grid, threads, smem, stream>>>(a);
-    else if (nv <= 4) route_topk_kernel<T, 4><<<grid, threads, smem, stream>>>(a);
-    else if (nv <= 8) route_topk_kernel<T, 8><<<grid, threads, smem, stream>>>(a);
-    else if (nv <= 16) route_topk_kernel<T, 16><<<grid, threads, smem, stream>>>(a);
-    else route_topk_kernel<T, 32><<<grid, threads, smem, stream>>>(a);
-    return cudaGetLastError();
+    if (nv <= 1) return launch_pdl(route_topk_kernel<T, 1>, dim3(grid), threads, smem, stream, 1, a);
+    if (nv <= 2) return launch_pdl(route_topk_kernel<T, 2>, dim3(grid), threads, smem, stream, 1, a);
+    if (nv <= 4) return launch_pdl(route_topk_kernel<T, 4>, dim3(grid), threads, smem, stream, 1, a);
+    if (nv <= 8) return launch_pdl(route_topk_kernel<T, 8>, dim3(grid), threads, smem, stream, 1, a);
+    if (nv <= 16) return launch_pdl(route_topk_kernel<T, 16>, dim3(grid), threads, smem, stream, 1, a);
+    return launch_pdl(route_topk_kernel<T, 32>, dim3(grid), threads, smem, stream, 1, a);
 }
 
 }  // namespace
@@ -335,12 +337,12 @@ cudaError_t launch_expert_plan(const int32_t *ids, int64_t slots, int experts, i
         if (e != cudaSuccess) return e;
     }
     if (counts) {
-        plan_count_kernel<<<nb, kPlanThreads, sizeof(int32_t) * experts, stream>>>(ids, slots, chunk, experts, counts);
-        const cudaError_t e = cudaGetLastError();
+        const cudaError_t e = launch_pdl(plan_count_kernel, dim3(nb), kPlanThreads, sizeof(int32_t) * experts, stream, 1, ids, slots,
+                                         chunk, experts, counts);
         if (e != cudaSuccess) return e;
     }
-    plan_place_kernel<<<nb, kPlanThreads, smem, stream>>>(ids, slots, chunk, experts, counts, offsets, order, position);
-    return cudaGetLastError();
+    return launch_pdl(plan_place_kernel, dim3(nb), kPlanThreads, smem, stream, 1, ids, slots, chunk, experts, counts, offsets,
+                      order, position);
 }
 
 }  // namespace qnn
