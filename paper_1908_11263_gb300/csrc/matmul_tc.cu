@@ -6,9 +6,14 @@
 // With the weights on the M side a thread of the epilogue owns one output channel: its scale and bias are two
 // registers, and the number of rows of x can be any multiple of 16 up to 256.
 //
-// Warps: 0 loads (x by tiled TMA, or one four-row gather per lane where an expert picks its tokens; weight blocks by
-// bulk copies), 1 issues the MMAs (first CTA of the pair), 2 hands complete stages of 16-bit weights on, 3 owns the
-// tensor memory, 4-11 run the epilogue, 12-19 expand packed codes into the A operand (packed weights only).
+// Where the tiles fill half of the pairs at most, a cluster of several pairs takes one tile and splits its K; the other
+// pairs write their sums into the first pair's shared memory, which adds them in order.
+//
+// Warps: 0 loads (x by tiled TMA, weight blocks by bulk copies), 1 issues the MMAs (first CTA of the pair), 2 hands
+// complete stages of 16-bit weights on, 3 owns the tensor memory, 4-11 run the epilogue, 12-19 expand packed codes into
+// the A operand, two groups on alternate stages.  Rows that an expert picks from x are copied by two more warps (2 and 3
+// of a packed product, 12 and 13 otherwise) with cp.async: four-row TMA gathers took about 80 cycles each, five times
+// what the MMAs of a stage do.
 // Every wait is bounded (mbar_wait_warp); a wait that gives up ends its role, and the kernel, with the status word set.
 #include <cuda.h>
 
@@ -27,6 +32,7 @@ constexpr uint32_t kBarBytes = 8 * (3 * kMaxStages + 4) + 16;
 
 struct TcShape {
     int nt, mt, stages;       // rows of x a tile, tiles along the image rows, pipeline stages
+    int ranks;                // pairs of a cluster that split K
     uint32_t cols;            // tensor-memory columns (power of two)
     uint32_t off_x, off_raw, off_bar, off_tab, smem;
 };
@@ -45,14 +51,29 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Arrives on the barrier at this address in the pair's first CTA.
-__device__ __forceinline__ void mbar_arrive_leader(uint64_t *bar)
+// Arrives on the barrier at this address in the CTA of this rank (the pair's first).
+__device__ __forceinline__ void mbar_arrive_at(uint64_t *bar, int rank)
 {
     asm volatile(
         "{\n\t.reg .b32 r;\n\t"
-        "mapa.shared::cluster.u32 r, %0, 0;\n\t"
-        "mbarrier.arrive.shared::cluster.b64 _, [r];\n\t}" ::"r"(smem_addr(bar))
+        "mapa.shared::cluster.u32 r, %0, %1;\n\t"
+        "mbarrier.arrive.shared::cluster.b64 _, [r];\n\t}" ::"r"(smem_addr(bar)),
+        "r"(rank)
         : "memory");
+}
+
+// Stores a float at this shared-memory address of the CTA of this rank.
+__device__ __forceinline__ void st_cluster(uint32_t at, int rank, float v)
+{
+    asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %0, %1;\n\tst.shared::cluster.f32 [r], %2;\n\t}" ::"r"(at),
+                 "r"(rank), "f"(v)
+                 : "memory");
+}
+
+// The first `bytes` of the 16, zeros after them.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
 __device__ __forceinline__ void mma2_f16_warp(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
@@ -66,15 +87,15 @@ __device__ __forceinline__ void mma2_f16_warp(uint32_t d, uint64_t a, uint64_t b
         : "memory");
 }
 
-// Arrives on this barrier in both CTAs of the pair when the MMAs issued so far have completed.
-__device__ __forceinline__ void mma2_commit_warp(uint64_t *bar)
+// Arrives on this barrier in both CTAs of the pair (bits of `mask`) when the MMAs issued so far have completed.
+__device__ __forceinline__ void mma2_commit_warp(uint64_t *bar, uint32_t mask)
 {
     asm volatile(
         "{\n\t.reg .pred e;\n\t"
         "elect.sync _|e, 0xffffffff;\n\t"
         "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(
             smem_addr(bar)),
-        "h"(static_cast<uint16_t>(3))
+        "h"(static_cast<uint16_t>(mask))
         : "memory");
 }
 
@@ -84,16 +105,6 @@ __device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int 
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
             smem_addr(dst)),
         "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar))
-        : "memory");
-}
-
-// Four rows of the map (box one row high) to four consecutive rows of shared memory.
-__device__ __forceinline__ void tma_gather4(void *dst, const CUtensorMap *map, int x, const int (&y)[4], uint64_t *bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], "
-        "[%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(smem_addr(dst)),
-        "l"(map), "r"(x), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]), "r"(smem_addr(bar))
         : "memory");
 }
 
@@ -164,9 +175,10 @@ __device__ __forceinline__ void load_rows(const T *r, int64_t step, T (&v)[N], i
 // Sixteen rows of x (columns of the accumulator) from `row` on, `n` of them in use, of one image row.  Without a gate a
 // lane finishes its own channel.  With one, a channel's gate and up rows are eight lanes apart: of each two rows of x the
 // gate lane finishes the first and the up lane the second.
+// `others` sums of other pairs (one float a lane and column, `step` floats apart) are added first.
 template <typename T, bool GATED>
 __device__ __forceinline__ void finish16(const MatmulArgs &a, uint32_t src, float2 p, int64_t row, int n, int64_t ch,
-                                         bool valid)
+                                         bool valid, const float *extra, int others, int step)
 {
     constexpr int kN = GATED ? 8 : 16;
     const bool up = GATED && (threadIdx.x & 8);
@@ -179,6 +191,9 @@ __device__ __forceinline__ void finish16(const MatmulArgs &a, uint32_t src, floa
     __syncwarp();
     tmem_ld16(src, acc);
     tmem_wait_ld();
+    for (int o = 0; o < others; ++o)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) + extra[o * step + i * 128]);
     float v[kN];
     if constexpr (GATED) {
         float u[kN];
@@ -234,8 +249,11 @@ __device__ __forceinline__ Tile tile_at(const MatmulArgs &a, const TcShape &s, c
     return t;
 }
 
+template <int BITS>
+constexpr int kTcThreads = BITS == 16 ? 448 : 640;
+
 template <typename T, int BITS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 640, 1)
+__global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     matmul_tc_kernel(const __grid_constant__ CUtensorMap xmap, const MatmulArgs a, const TcShape s, int *status)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -248,14 +266,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 6
     uint32_t *slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
     int *tab = reinterpret_cast<int *>(smem + s.off_tab);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = static_cast<int>(cluster_rank());
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int cluster = static_cast<int>(cluster_rank());
+    const int rank = cluster & 1, leader = cluster & ~1, split = cluster >> 1;  // CTA of the pair, its first CTA, share of K
+    const int pair = blockIdx.x / (2 * s.ranks), pairs = gridDim.x / (2 * s.ranks);
     const uint32_t x_bytes = s.nt / 2 * 128;
+    const int kb0 = a.kb * split / s.ranks, kb1 = a.kb * (split + 1) / s.ranks;  // this pair's 64-column blocks
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < s.stages; ++i) {
             mbar_init(full + i, 1);
-            mbar_init(ready + i, kPacked ? 16 : 2);
+            mbar_init(ready + i, (kPacked ? 8 : 2) + (a.gather ? 4 : 0));
             mbar_init(empty + i, 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -264,11 +284,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 6
         }
         fence_mbar_init();
     }
-    pdl_begin();
     if (warp == 3) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(s.cols)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    pdl_begin();
+    if (warp == 3) {
         if (a.offsets) expert_tiles(a.offsets, a.experts, s.nt, tab);
         tc_fence_before();
     }
@@ -282,42 +304,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 6
         for (int64_t r = a.offsets[a.experts] + blockIdx.x; r < a.rows; r += gridDim.x)
             for (int c = threadIdx.x; c < a.m; c += blockDim.x) static_cast<T *>(a.y)[r * a.ldy + c] = from_f32<T>(0.f);
 
+    const int loader = !a.gather ? -1 : kPacked ? warp - 2 : warp - 12;  // 0 or 1: copies rows of x
     bool ok = true;
+    int st = 0;          // stage, and the parity of its barriers' current phase
+    uint32_t phase = 0;
+    auto advance = [&]() {
+        if (++st == s.stages) {
+            st = 0;
+            phase ^= 1;
+        }
+    };
     if (warp == 0) {
         // ------------------------------------------------ loads
-        int st = 0, uses = 0;
-        uint32_t phase = 0;
+        int uses = 0;
         for (int id = pair; id < tiles && ok; id += pairs) {
             const Tile t = tile_at(a, s, tab, id);
-            int rows[4] = {0, 0, 0, 0};
-            const bool gathers = a.gather && lane < s.nt / 8;
-            if (gathers)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = rank * (s.nt / 2) + lane * 4 + i;
-                    rows[i] = a.order[t.first + (r < t.count ? r : 0)] / a.top;  // rows past the count are not stored
-                }
             const int mb = min((t.mtile * 2 + rank) * 4 + (lane & 3), a.mb - 1);  // rows past the image are not stored
             const uint8_t *src = a.image + (static_cast<size_t>(t.expert) * a.mb + mb) * a.kb * kBlock;
-            for (int kb = 0; kb < a.kb; ++kb) {
+            for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait_warp(empty + st, phase ^ 1, status)) {
                     ok = false;
                     break;
                 }
-                if (lane == 0) mbar_arrive_expect_tx(full + st, x_bytes + 4 * kBlock);
+                if (lane == 0) mbar_arrive_expect_tx(full + st, (a.gather ? 0 : x_bytes) + 4 * kBlock);
                 __syncwarp();
                 uint8_t *dst = kPacked ? sm_raw + st * 4 * kBlock : sm_a + st * kABytes;
-                if (lane < 4) bulk_g2s(dst + lane * kBlock, src + static_cast<size_t>(kb) * kBlock, kBlock, full + st);
-                if (gathers)
-                    tma_gather4(sm_x + st * x_bytes + lane * 512, &xmap, kb * 64, rows, full + st);
-                else if (!a.gather && lane == 4)
+                if (lane < 4)
+                    bulk_g2s(dst + lane * kBlock, src + static_cast<size_t>(kb) * kBlock, kBlock, full + st);
+                else if (lane == 4 && !a.gather)
                     tma_tile(sm_x + st * x_bytes, &xmap, kb * 64, static_cast<int>(t.first) + rank * (s.nt / 2), full + st);
                 __syncwarp();
                 ++uses;
-                if (++st == s.stages) {
-                    st = 0;
-                    phase ^= 1;
-                }
+                advance();
             }
         }
         // copies still in flight land before the CTA may end
@@ -332,8 +350,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 6
         // ------------------------------------------------ MMAs
         constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
         const uint32_t idesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (static_cast<uint32_t>(s.nt >> 3) << 17) | (16u << 24);
-        int st = 0, it = 0;
-        uint32_t phase = 0;
+        const uint32_t both = 3u << leader;
+        int it = 0;
         for (int id = pair; id < tiles && ok; id += pairs, ++it) {
             const int buf = it & 1;
             if (!mbar_wait_warp(acc_empty + buf, ((it >> 1) & 1) ^ 1, status)) {
@@ -342,7 +360,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 6
             }
             tc_fence_after();
             const uint32_t d = tmem + buf * s.nt;
-            for (int kb = 0; kb < a.kb; ++kb) {
+            for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait_warp(ready + st, phase, status)) {
                     ok = false;
                     break;
@@ -351,31 +369,65 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 6
                 const uint64_t da = desc_sw128(smem_addr(sm_a + st * kABytes));
                 const uint64_t db = desc_sw128(smem_addr(sm_x + st * x_bytes));
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mma2_f16_warp(d, da + 2 * k, db + 2 * k, idesc, kb | k);
-                mma2_commit_warp(empty + st);
-                if (++st == s.stages) {
-                    st = 0;
-                    phase ^= 1;
-                }
+                for (int k = 0; k < 4; ++k) mma2_f16_warp(d, da + 2 * k, db + 2 * k, idesc, (kb - kb0) | k);
+                mma2_commit_warp(empty + st, both);
+                advance();
             }
-            if (ok) mma2_commit_warp(acc_full + buf);
+            if (ok) mma2_commit_warp(acc_full + buf, both);
         }
+    } else if (loader == 0 || loader == 1) {
+        // ------------------------------------------------ rows of x that the expert picks
+        constexpr int kDeep = 3;  // stages in flight; below the number of stages, so that every stage is handed on
+        const int per = s.nt / 16, r0 = loader * (s.nt / 4) + (lane >> 3);  // this lane copies rows r0 + 4 i, i < per
+        const int c = lane & 7;
+        int old = 0, issued = 0;  // stage to hand on next
+        auto hand_on = [&]() {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(ready + old, leader);
+            if (++old == s.stages) old = 0;
+        };
+        for (int id = pair; id < tiles && ok; id += pairs) {
+            const Tile t = tile_at(a, s, tab, id);
+            int rows[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = rank * (s.nt / 2) + r0 + 4 * i;  // rows past the count repeat the first; they are not stored
+                rows[i] = i < per ? a.order[t.first + (r < t.count ? r : 0)] / a.top : 0;
+            }
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!mbar_wait_warp(empty + st, phase ^ 1, status)) {
+                    ok = false;
+                    break;
+                }
+                const int k = kb * 64 + c * 8;
+                const uint32_t bytes = max(0, min(16, 2 * (a.k - k)));
+                const uint32_t dst = smem_addr(sm_x + st * x_bytes) + r0 * 128;
+                const T *x = static_cast<const T *>(a.x) + (bytes ? k : 0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i < per) cp_async16(dst + i * 512 + (c ^ ((r0 + 4 * i) & 7)) * 16, x + rows[i] * a.ldx, bytes);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (++issued > kDeep) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kDeep) : "memory");
+                    hand_on();
+                }
+                advance();
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        for (int i = 0; i < min(issued, kDeep); ++i) hand_on();
     } else if (warp == 2 && !kPacked) {
         // ------------------------------------------------ complete stages of 16-bit weights
-        int st = 0;
-        uint32_t phase = 0;
         for (int id = pair; id < tiles && ok; id += pairs)
-            for (int kb = 0; kb < a.kb; ++kb) {
+            for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait_warp(full + st, phase, status)) {
                     ok = false;
                     break;
                 }
-                if (lane == 0) mbar_arrive_leader(ready + st);
+                if (lane == 0) mbar_arrive_at(ready + st, leader);
                 __syncwarp();
-                if (++st == s.stages) {
-                    st = 0;
-                    phase ^= 1;
-                }
+                advance();
             }
     } else if (warp >= 4 && warp < 12) {
         // ------------------------------------------------ epilogue: two warps a quarter of the lanes
@@ -393,63 +445,93 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BITS == 16 ? 384 : 6
                 break;
             }
             tc_fence_after();
+            if (s.ranks > 1) break;  // one tile a cluster: the sums of its pairs meet below
             const uint32_t src = tmem + buf * s.nt + (static_cast<uint32_t>(quarter * 32) << 16);
             for (int c = 16 * half; c < t.count; c += 32) {
                 if (a.gated)
-                    finish16<T, true>(a, src + c, p, t.first + c, t.count - c, ch, valid);
+                    finish16<T, true>(a, src + c, p, t.first + c, t.count - c, ch, valid, nullptr, 0, 0);
                 else
-                    finish16<T, false>(a, src + c, p, t.first + c, t.count - c, ch, valid);
+                    finish16<T, false>(a, src + c, p, t.first + c, t.count - c, ch, valid, nullptr, 0, 0);
             }
             __syncwarp();
             tc_fence_before();
-            if (lane == 0) mbar_arrive_leader(acc_empty + buf);
+            if (lane == 0) mbar_arrive_at(acc_empty + buf, leader);
             __syncwarp();
         }
     } else if (warp >= 12) {
         // ------------------------------------------------ packed codes to the A operand
         if constexpr (kPacked) {
-            const int i = (warp - 12) >> 1, j = (warp - 12) & 1;  // 32-row block, its half
+            const int block = (warp - 12) & 3, group = (warp - 12) >> 2;  // 32-row block; stages taken by turns
             const int g = lane >> 2, tt = lane & 3;
-            int st = 0;
-            uint32_t phase = 0;
+            int turn = 0;
             for (int id = pair; id < tiles && ok; id += pairs)
-                for (int kb = 0; kb < a.kb; ++kb) {
+                for (int kb = kb0; kb < kb1; ++kb, turn ^= 1) {
+                    if (turn != group) {
+                        advance();
+                        continue;
+                    }
                     if (!mbar_wait_warp(full + st, phase, status)) {
                         ok = false;
                         break;
                     }
-                    const uint8_t *raw = sm_raw + st * 4 * kBlock + i * kBlock;
-                    uint32_t w[BITS];  // two runs of 16 codes: rows g and g + 8 of the half
-                    if constexpr (BITS == 8) {
+                    const uint8_t *raw = sm_raw + st * 4 * kBlock + block * kBlock;
+                    uint32_t w[2 * BITS];  // four runs of 16 codes: rows g, g + 8, g + 16, g + 24
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            *reinterpret_cast<uint4 *>(w + 4 * h) =
-                                reinterpret_cast<const uint4 *>(raw)[(2 * j + h) * 32 + lane];
-                    } else if constexpr (BITS == 4) {
-                        *reinterpret_cast<uint4 *>(w) = reinterpret_cast<const uint4 *>(raw)[j * 32 + lane];
-                    } else {
-                        *reinterpret_cast<uint2 *>(w) = reinterpret_cast<const uint2 *>(raw)[lane * 2 + j];
-                    }
+                    for (int i = 0; i < BITS / 2; ++i)
+                        *reinterpret_cast<uint4 *>(w + 4 * i) = reinterpret_cast<const uint4 *>(raw)[i * 32 + lane];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < 4; ++h) {
                         uint32_t v[8];
                         expand16<T, BITS>(w + h * (BITS / 2), v);
-                        uint8_t *dst = sm_a + st * kABytes + (i * 32 + j * 16 + h * 8 + g) * 128;
+                        uint8_t *dst = sm_a + st * kABytes + (block * 32 + h * 8 + g) * 128;
                         *reinterpret_cast<uint4 *>(dst + ((2 * tt) ^ g) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
                         *reinterpret_cast<uint4 *>(dst + ((2 * tt + 1) ^ g) * 16) = make_uint4(v[4], v[5], v[6], v[7]);
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_leader(ready + st);
+                    if (lane == 0) mbar_arrive_at(ready + st, leader);
                     __syncwarp();
-                    if (++st == s.stages) {
-                        st = 0;
-                        phase ^= 1;
-                    }
+                    advance();
                 }
         }
     }
     __syncwarp();
+    if (s.ranks > 1) {
+        // The other pairs' sums go to the first pair's stages, which no copy or MMA uses any more: [pair - 1][column][lane].
+        tc_fence_before();
+        __syncthreads();
+        cluster_sync();
+        tc_fence_after();
+        float *sums = reinterpret_cast<float *>(smem);
+        const bool epilogue = warp >= 4 && warp < 12;
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t src = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+        const Tile t = tile_at(a, s, tab, pair);
+        if (epilogue && split > 0)
+            for (int c = 16 * half; c < t.count; c += 32) {
+                uint32_t acc[16];
+                tmem_ld16(src + c, acc);
+                tmem_wait_ld();
+                const uint32_t at = smem_addr(sums + ((split - 1) * s.nt + c) * 128 + quarter * 32 + lane);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st_cluster(at + i * 512, rank, __uint_as_float(acc[i]));
+            }
+        __syncwarp();
+        cluster_sync();
+        if (epilogue && split == 0) {
+            const int row = t.mtile * 256 + rank * 128 + quarter * 32 + lane;
+            const int ch = a.gated ? (row >> 4) * 8 + (row & 7) : row;
+            const float2 p = row < a.mb * 32 ? a.params[row] : make_float2(0.f, 0.f);
+            for (int c = 16 * half; c < t.count; c += 32) {
+                const float *extra = sums + c * 128 + quarter * 32 + lane;
+                if (a.gated)
+                    finish16<T, true>(a, src + c, p, t.first + c, t.count - c, ch, ch < a.m, extra, s.ranks - 1, s.nt * 128);
+                else
+                    finish16<T, false>(a, src + c, p, t.first + c, t.count - c, ch, ch < a.m, extra, s.ranks - 1, s.nt * 128);
+            }
+        }
+        __syncwarp();
+    }
     tc_fence_before();
     __syncthreads();
     cluster_sync();  // the pair's MMAs, copies and remote arrivals are done
@@ -480,10 +562,11 @@ EncodeTiled encode_tiled()
     return fn;
 }
 
-TcShape shape_of(const MatmulArgs &a, int bits, int nt)
+TcShape shape_of(const MatmulArgs &a, int bits, int nt, int ranks)
 {
     TcShape s;
     s.nt = nt;
+    s.ranks = ranks;
     s.mt = (a.mb + 7) / 8;
     const uint32_t raw = bits == 16 ? 0 : 4 * (32 * 64 * bits / 8), x = nt / 2 * 128, stage = kABytes + x + raw;
     const uint32_t tab = (4 * (a.experts + 1) + 15) / 16 * 16;
@@ -516,8 +599,8 @@ cudaError_t launch_tc(const CUtensorMap &map, const MatmulArgs &a, const TcShape
         }
     }
     const int64_t pairs = device_sm_count() / 2;
-    const unsigned grid = static_cast<unsigned>(2 * (tiles < pairs ? tiles : pairs));
-    return launch_pdl(matmul_tc_kernel<T, BITS>, dim3(grid), BITS == 16 ? 384 : 640, s.smem, st, 1, map, a, s, status);
+    const unsigned grid = static_cast<unsigned>(s.ranks > 1 ? 2 * s.ranks * tiles : 2 * (tiles < pairs ? tiles : pairs));
+    return launch_pdl(matmul_tc_kernel<T, BITS>, dim3(grid), kTcThreads<BITS>, s.smem, st, 2 * s.ranks, map, a, s, status);
 }
 
 template <typename T>
@@ -530,31 +613,37 @@ cudaError_t launch_bits(const CUtensorMap &map, const MatmulArgs &a, const TcSha
     return launch_tc<T, 2>(map, a, s, tiles, status, st);
 }
 
-// Rows of x a tile.  A tile's MMAs take about 2 nt cycles for each 64 columns, but never less than the A operand takes to
-// stage and read (kFloor), and a tile has a fixed cost (kFixed); the width with the least sum over the rounds of tiles
-// that the CTA pairs make wins.
-int choose_nt(const MatmulArgs &a)
+// Rows of x a tile, and pairs that split K.  A tile's MMAs take about 2 nt cycles for each 64 columns, but never less than
+// a stage takes to be copied, expanded and handed on (kFloor), and a tile has a fixed cost (kFixed); a split adds the
+// exchange of the sums.  The choice with the least sum over the rounds of tiles that the pairs make wins.
+void choose(const MatmulArgs &a, int bits, int *nt_out, int *ranks_out)
 {
-    constexpr double kFloor = 220, kFixed = 3000;
+    const double kFloor = bits == 16 ? 260 : 340, kFixed = 3000;
     const int pairs = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1;
     const int mt = (a.mb + 7) / 8;
-    int best = 16;
     double cost = 0;
-    for (int nt = 16; nt <= 256; nt += 16) {
-        double tiles = static_cast<double>((a.rows + nt - 1) / nt);
-        if (a.offsets) {  // every expert with rows ends in a partial tile: half a tile each
-            const double live = a.experts < a.rows ? a.experts : static_cast<double>(a.rows);
-            tiles = static_cast<double>(a.rows) / nt + 0.5 * live;
-            if (tiles < live) tiles = live;
-        }
-        const double waves = std::ceil(tiles * mt / pairs);
-        const double c = waves * (a.kb * (2.0 * nt > kFloor ? 2.0 * nt : kFloor) + kFixed);
-        if (nt == 16 || c < cost) {
-            cost = c;
-            best = nt;
+    *nt_out = 0;
+    for (int ranks = 1; ranks <= 4; ranks *= 2) {
+        if (ranks > 1 && (a.offsets || a.kb < 4 * ranks)) break;
+        for (int nt = 16; nt <= 256; nt += 16) {
+            double tiles = static_cast<double>((a.rows + nt - 1) / nt);
+            if (a.offsets) {  // every expert with rows ends in a partial tile: half a tile each
+                const double live = a.experts < a.rows ? a.experts : static_cast<double>(a.rows);
+                tiles = static_cast<double>(a.rows) / nt + 0.5 * live;
+                if (tiles < live) tiles = live;
+            }
+            // clusters of eight CTAs leave some SMs of a GPC unused
+            if (ranks > 1 && (tiles * mt * ranks > (ranks == 4 ? 0.8 : 0.95) * pairs || (ranks - 1) * nt * 512 > 160 * 1024)) continue;
+            const double waves = ranks > 1 ? 1 : std::ceil(tiles * mt / pairs);
+            const double per_kb = 2.0 * nt > kFloor ? 2.0 * nt : kFloor;
+            const double c = waves * ((a.kb + ranks - 1) / ranks * per_kb + kFixed) + (ranks > 1 ? 3000 + 20.0 * nt * (ranks - 1) : 0);
+            if (*nt_out == 0 || c < cost) {
+                cost = c;
+                *nt_out = nt;
+                *ranks_out = ranks;
+            }
         }
     }
-    return best;
 }
 
 }  // namespace
@@ -565,8 +654,9 @@ cudaError_t launch_matmul_tc(const MatmulArgs &a, int dtype, int bits, cudaStrea
     int *status = device_status_ptr();
     const EncodeTiled encode = encode_tiled();
     if (!status || !encode) return cudaErrorNotSupported;
-    const int nt = choose_nt(a);
-    const TcShape s = shape_of(a, bits, nt);
+    int nt = 0, ranks = 1;
+    choose(a, bits, &nt, &ranks);
+    const TcShape s = shape_of(a, bits, nt, ranks);
     int64_t u = (a.rows + nt - 1) / nt;
     if (a.offsets) u += a.experts < a.rows ? a.experts : a.rows;
     const int64_t tiles = u * s.mt;  // at most; experts' tiles are counted by the kernel
@@ -574,7 +664,7 @@ cudaError_t launch_matmul_tc(const MatmulArgs &a, int dtype, int bits, cudaStrea
     CUtensorMap map;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.k), static_cast<cuuint64_t>(a.x_rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.ldx) * 2};
-    const cuuint32_t box[2] = {64, a.gather ? 1u : static_cast<cuuint32_t>(nt / 2)}, unit[2] = {1, 1};
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(nt / 2)}, unit[2] = {1, 1};
     if (encode(&map, dtype == QNN_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
                const_cast<void *>(a.x), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
