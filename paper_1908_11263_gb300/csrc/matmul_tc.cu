@@ -33,6 +33,7 @@ constexpr uint32_t kBarBytes = 8 * (3 * kMaxStages + 4) + 16;
 struct TcShape {
     int nt, mt, stages;       // rows of x a tile, tiles along the image rows, pipeline stages
     int ranks;                // pairs of a cluster that split K
+    int group;                // tiles along the image rows that run side by side
     uint32_t cols;            // tensor-memory columns (power of two)
     uint32_t off_x, off_raw, off_bar, off_tab, smem;
 };
@@ -228,13 +229,15 @@ struct Tile {
     int64_t first;
 };
 
-// Tile `id`: tiles along the image rows first, then along the rows of x (of the experts one after another; `tab` holds
-// the tiles before each expert).
-__device__ __forceinline__ Tile tile_at(const MatmulArgs &a, const TcShape &s, const int *tab, int id)
+// Tile `id` of `us` tiles along the rows of x (of the experts one after another; `tab` holds the tiles before each
+// expert): `group` tiles along the image rows, then along the rows of x, then the next group of image rows.  The pairs
+// then work on about as many bytes of weights as of x at a time, and both stay in L2 while they are shared.
+__device__ __forceinline__ Tile tile_at(const MatmulArgs &a, const TcShape &s, const int *tab, int us, int id)
 {
     Tile t;
-    t.mtile = id % s.mt;
-    const int u = id / s.mt;
+    const int block = id / (s.group * us), m0 = block * s.group, in = id - m0 * us;
+    const int wide = min(s.group, s.mt - m0), u = in / wide;
+    t.mtile = m0 + in - u * wide;
     t.expert = 0;
     if (a.offsets) {
         const int lo = find_expert(tab, a.experts, u);
@@ -274,8 +277,8 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < s.stages; ++i) {
-            mbar_init(full + i, 1);
-            mbar_init(ready + i, (kPacked ? 8 : 2) + (a.gather ? 4 : 0));
+            mbar_init(full + i, a.gather ? 1 + 64 : 1);
+            mbar_init(ready + i, kPacked ? 8 : 2);
             mbar_init(empty + i, 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -298,7 +301,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = *slot;
-    const int tiles = (a.offsets ? tab[a.experts] : static_cast<int>((a.rows + s.nt - 1) / s.nt)) * s.mt;
+    const int us = a.offsets ? tab[a.experts] : static_cast<int>((a.rows + s.nt - 1) / s.nt), tiles = us * s.mt;
 
     if (a.zero_tail)  // rows that no expert fills
         for (int64_t r = a.offsets[a.experts] + blockIdx.x; r < a.rows; r += gridDim.x)
@@ -318,7 +321,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         // ------------------------------------------------ loads
         int uses = 0;
         for (int id = pair; id < tiles && ok; id += pairs) {
-            const Tile t = tile_at(a, s, tab, id);
+            const Tile t = tile_at(a, s, tab, us, id);
             const int mb = min((t.mtile * 2 + rank) * 4 + (lane & 3), a.mb - 1);  // rows past the image are not stored
             const uint8_t *src = a.image + (static_cast<size_t>(t.expert) * a.mb + mb) * a.kb * kBlock;
             for (int kb = kb0; kb < kb1; ++kb) {
@@ -377,23 +380,15 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         }
     } else if (loader == 0 || loader == 1) {
         // ------------------------------------------------ rows of x that the expert picks
-        constexpr int kDeep = 3;  // stages in flight; below the number of stages, so that every stage is handed on
         const int per = s.nt / 16, r0 = loader * (s.nt / 4) + (lane >> 3);  // this lane copies rows r0 + 4 i, i < per
         const int c = lane & 7;
-        int old = 0, issued = 0;  // stage to hand on next
-        auto hand_on = [&]() {
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_at(ready + old, leader);
-            if (++old == s.stages) old = 0;
-        };
         for (int id = pair; id < tiles && ok; id += pairs) {
-            const Tile t = tile_at(a, s, tab, id);
-            int rows[16];
+            const Tile t = tile_at(a, s, tab, us, id);
+            const T *src[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int r = rank * (s.nt / 2) + r0 + 4 * i;  // rows past the count repeat the first; they are not stored
-                rows[i] = i < per ? a.order[t.first + (r < t.count ? r : 0)] / a.top : 0;
+                src[i] = static_cast<const T *>(a.x) + (i < per ? a.order[t.first + (r < t.count ? r : 0)] / a.top : 0) * a.ldx;
             }
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait_warp(empty + st, phase ^ 1, status)) {
@@ -402,21 +397,21 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                 }
                 const int k = kb * 64 + c * 8;
                 const uint32_t bytes = max(0, min(16, 2 * (a.k - k)));
+                const int64_t at = bytes ? k : 0;
+                // rows four apart differ in bit 2 of the swizzle
                 const uint32_t dst = smem_addr(sm_x + st * x_bytes) + r0 * 128;
-                const T *x = static_cast<const T *>(a.x) + (bytes ? k : 0);
+                const uint32_t even = dst + (c ^ (r0 & 7)) * 16, odd = dst + 512 + (c ^ ((r0 + 4) & 7)) * 16;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (i < per) cp_async16(dst + i * 512 + (c ^ ((r0 + 4 * i) & 7)) * 16, x + rows[i] * a.ldx, bytes);
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (++issued > kDeep) {
-                    asm volatile("cp.async.wait_group %0;" ::"n"(kDeep) : "memory");
-                    hand_on();
+                for (int i = 0; i < 16; i += 2) {
+                    if (i < per) cp_async16(even + i * 512, src[i] + at, bytes);
+                    if (i + 1 < per) cp_async16(odd + i * 512, src[i + 1] + at, bytes);
                 }
+                // this lane's copies arrive on the stage when they have landed; whoever hands the stage on fences them
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(full + st)) : "memory");
                 advance();
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        for (int i = 0; i < min(issued, kDeep); ++i) hand_on();
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == 2 && !kPacked) {
         // ------------------------------------------------ complete stages of 16-bit weights
         for (int id = pair; id < tiles && ok; id += pairs)
@@ -425,6 +420,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                     ok = false;
                     break;
                 }
+                if (a.gather) fence_proxy_async_smem();  // cp.async writes as the threads do; the MMAs read through the async proxy
                 if (lane == 0) mbar_arrive_at(ready + st, leader);
                 __syncwarp();
                 advance();
@@ -435,7 +431,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         int it = 0;
         for (int id = pair; id < tiles && ok; id += pairs, ++it) {
             const int buf = it & 1;
-            const Tile t = tile_at(a, s, tab, id);
+            const Tile t = tile_at(a, s, tab, us, id);
             const int row = t.mtile * 256 + rank * 128 + quarter * 32 + lane;  // image row
             const int ch = a.gated ? (row >> 4) * 8 + (row & 7) : row;
             const bool valid = ch < a.m;
@@ -506,7 +502,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         const bool epilogue = warp >= 4 && warp < 12;
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t src = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-        const Tile t = tile_at(a, s, tab, pair);
+        const Tile t = tile_at(a, s, tab, us, pair);
         if (epilogue && split > 0)
             for (int c = 16 * half; c < t.count; c += 32) {
                 uint32_t acc[16];
@@ -568,6 +564,11 @@ TcShape shape_of(const MatmulArgs &a, int bits, int nt, int ranks)
     s.nt = nt;
     s.ranks = ranks;
     s.mt = (a.mb + 7) / 8;
+    // g tiles of weights (256 rows of `bits`) beside 76 / g tiles of x (nt rows of 16 bits): the fewest bytes at
+    // g = sqrt(76 * 16 nt / (256 bits))
+    s.group = static_cast<int>(std::sqrt(4.75 * nt / bits) + 0.5);
+    if (s.group < 1) s.group = 1;
+    if (s.group > s.mt) s.group = s.mt;
     const uint32_t raw = bits == 16 ? 0 : 4 * (32 * 64 * bits / 8), x = nt / 2 * 128, stage = kABytes + x + raw;
     const uint32_t tab = (4 * (a.experts + 1) + 15) / 16 * 16;
     const uint32_t room = 227 * 1024 - kBarBytes - tab;
