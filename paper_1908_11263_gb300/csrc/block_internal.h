@@ -29,8 +29,10 @@ cudaError_t launch_matmul_prep(const qnn_matmul_desc &d, const void *w, const fl
 cudaError_t launch_combine(int dtype, const float *z, int64_t ldz, const float *weights, const int32_t *position,
                            int64_t tokens, int top, int m, const void *residual, int64_t ldres, void *y, int64_t ldy,
                            cudaStream_t st);
-// rows of 16-bit values to rows ldd apart (ldd a multiple of 8), for the loads that need 16-byte aligned rows
-cudaError_t launch_align_rows(const void *src, int64_t lds, void *dst, int64_t ldd, int64_t rows, int cols, cudaStream_t st);
+// rows of 16-bit values to rows ldd apart (a multiple of 8), in order or as a plan has them: for the tiled loads, which
+// take 16-byte aligned rows that lie one after another
+cudaError_t launch_take_rows(const void *src, int64_t lds, const int32_t *order, int top, void *dst, int64_t ldd, int64_t rows,
+                             int cols, cudaStream_t st);
 // ---- tcgen05 -- matmul_tc.cu (rows of x 16-byte aligned)
 cudaError_t launch_matmul_tc(const MatmulArgs &a, int dtype, int bits, cudaStream_t st);
 // ---- few rows: streamed weights -- matmul_stream.cu

@@ -57,21 +57,24 @@ bool on_tensor_cores(int64_t rows, int experts)
 int64_t align8(int64_t v) { return (v + 7) / 8 * 8; }
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Bytes for x with 16-byte aligned rows, where the tensor-core kernel needs them and x has none.
-size_t staging_bytes(const qnn_matmul_desc &d, int64_t rows, int experts, int64_t x_rows, const void *x, int64_t ldx)
+// Bytes for the rows of x as the tensor-core kernel takes them, where x has not got them so: `rows` rows, in the order
+// of the plan for a dispatch, 16-byte aligned.
+size_t staging_bytes(const qnn_matmul_desc &d, int64_t rows, int experts, bool gather, const void *x, int64_t ldx)
 {
-    if (!on_tensor_cores(rows, experts) || (aligned(x, 16) && ldx % 8 == 0)) return 0;
-    return static_cast<size_t>(x_rows) * align8(d.k) * 2;
+    if (!on_tensor_cores(rows, experts) || (!gather && aligned(x, 16) && ldx % 8 == 0)) return 0;
+    return static_cast<size_t>(rows) * align8(d.k) * 2;
 }
 
 cudaError_t run_product(MatmulArgs a, const qnn_matmul_desc &d, void *staging, cudaStream_t st)
 {
     if (!on_tensor_cores(a.rows, a.offsets ? a.experts : 0)) return launch_matmul_stream(a, d.dtype, d.bits, st);
-    if (!a.x_vec) {
-        const cudaError_t e = launch_align_rows(a.x, a.ldx, staging, align8(d.k), a.x_rows, d.k, st);
+    if (a.gather || !a.x_vec) {
+        const cudaError_t e = launch_take_rows(a.x, a.ldx, a.gather ? a.order : nullptr, a.top, staging, align8(d.k), a.rows, d.k, st);
         if (e != cudaSuccess) return e;
         a.x = staging;
         a.ldx = align8(d.k);
+        a.x_rows = a.rows;
+        a.gather = 0;
     }
     return launch_matmul_tc(a, d.dtype, d.bits, st);
 }
@@ -185,7 +188,7 @@ qnn_status qnn_matmul_workspace_size(const qnn_matmul_desc *d, int64_t t, const 
     if (st != QNN_OK) return st;
     if (t < 0 || ldx < d->k) return QNN_EINVAL;
     if (t > kMaxRows) return QNN_EUNSUPPORTED;
-    *bytes = staging_bytes(*d, t, 0, t, x, ldx);
+    *bytes = staging_bytes(*d, t, 0, false, x, ldx);
     return QNN_OK;
 }
 
@@ -215,7 +218,7 @@ qnn_status qnn_experts_workspace_size(const qnn_matmul_desc *d, int64_t tokens, 
     if (st != QNN_OK) return st;
     if (ldx < d->k) return QNN_EINVAL;
     const int64_t slots = tokens * top;
-    *bytes = staging_bytes(*d, slots, d->experts, combine ? slots : tokens, x, ldx);
+    *bytes = staging_bytes(*d, slots, d->experts, !combine, x, ldx);
     if (combine) *bytes += align256(static_cast<size_t>(slots) * combine_ld(*d) * sizeof(float));
     return QNN_OK;
 }

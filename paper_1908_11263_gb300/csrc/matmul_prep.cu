@@ -140,20 +140,44 @@ __global__ void combine_kernel(const CombineArgs a)
     }
 }
 
-__global__ void align_rows_kernel(const uint16_t *src, int64_t lds, uint16_t *dst, int64_t ldd, int cols)
+// Row i of dst: row i of src, or row order[i] / top (no row where order[i] is negative).  VEC: rows are 16-byte aligned
+// and whole vectors.
+template <bool VEC>
+__global__ void take_rows_kernel(const uint16_t *src, int64_t lds, const int32_t *order, int top, uint16_t *dst, int64_t ldd,
+                                 int64_t rows, int cols)
 {
-    const int64_t row = blockIdx.x;
     pdl_begin();
-    for (int c = threadIdx.x; c < cols; c += blockDim.x) dst[row * ldd + c] = src[row * lds + c];
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * blockDim.y + threadIdx.y; row < rows;
+         row += static_cast<int64_t>(gridDim.x) * blockDim.y) {
+        int64_t from = row;
+        if (order) {
+            const int slot = order[row];
+            if (slot < 0) continue;
+            from = slot / top;
+        }
+        const uint16_t *p = src + from * lds;
+        uint16_t *q = dst + row * ldd;
+        if constexpr (VEC) {
+            for (int c = threadIdx.x * 8; c < cols; c += blockDim.x * 8)
+                *reinterpret_cast<uint4 *>(q + c) = *reinterpret_cast<const uint4 *>(p + c);
+        } else {
+            for (int c = threadIdx.x; c < cols; c += blockDim.x) q[c] = p[c];
+        }
+    }
 }
 
 }  // namespace
 
-cudaError_t launch_align_rows(const void *src, int64_t lds, void *dst, int64_t ldd, int64_t rows, int cols, cudaStream_t st)
+cudaError_t launch_take_rows(const void *src, int64_t lds, const int32_t *order, int top, void *dst, int64_t ldd, int64_t rows,
+                             int cols, cudaStream_t st)
 {
     if (rows == 0) return cudaSuccess;
-    return launch_pdl(align_rows_kernel, dim3(static_cast<unsigned>(rows)), 256, 0, st, 1, static_cast<const uint16_t *>(src), lds,
-                      static_cast<uint16_t *>(dst), ldd, cols);
+    const bool vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && lds % 8 == 0 && cols % 8 == 0;
+    const unsigned grid = static_cast<unsigned>(rows < 65535 ? rows : 65535);
+    return vec ? launch_pdl(take_rows_kernel<true>, dim3(grid), 128, 0, st, 1, static_cast<const uint16_t *>(src), lds, order, top,
+                            static_cast<uint16_t *>(dst), ldd, rows, cols)
+               : launch_pdl(take_rows_kernel<false>, dim3(grid), 128, 0, st, 1, static_cast<const uint16_t *>(src), lds, order, top,
+                            static_cast<uint16_t *>(dst), ldd, rows, cols);
 }
 
 cudaError_t launch_matmul_prep(const qnn_matmul_desc &d, const void *w, const float *scale, const float *bias,

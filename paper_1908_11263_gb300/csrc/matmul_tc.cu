@@ -11,9 +11,9 @@
 //
 // Warps: 0 loads (x by tiled TMA, weight blocks by bulk copies), 1 issues the MMAs (first CTA of the pair), 2 hands
 // complete stages of 16-bit weights on, 3 owns the tensor memory, 4-11 run the epilogue, 12-19 expand packed codes into
-// the A operand, two groups on alternate stages.  Rows that an expert picks from x are copied by two more warps (2 and 3
-// of a packed product, 12 and 13 otherwise) with cp.async: four-row TMA gathers took about 80 cycles each, five times
-// what the MMAs of a stage do.
+// the A operand, two groups on alternate stages.  Rows that an expert picks from x lie one after another before the
+// launch: picking them inside it held the MMAs up (692 us with four-row TMA gathers, which take some 80 cycles each, 371
+// with cp.async by two warps, for a product that takes 171 on rows in order and a copy that takes 30).
 // Every wait is bounded (mbar_wait_warp); a wait that gives up ends its role, and the kernel, with the status word set.
 #include <cuda.h>
 
@@ -69,12 +69,6 @@ __device__ __forceinline__ void st_cluster(uint32_t at, int rank, float v)
     asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %0, %1;\n\tst.shared::cluster.f32 [r], %2;\n\t}" ::"r"(at),
                  "r"(rank), "f"(v)
                  : "memory");
-}
-
-// The first `bytes` of the 16, zeros after them.
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
 __device__ __forceinline__ void mma2_f16_warp(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
@@ -253,7 +247,7 @@ __device__ __forceinline__ Tile tile_at(const MatmulArgs &a, const TcShape &s, c
 }
 
 template <int BITS>
-constexpr int kTcThreads = BITS == 16 ? 448 : 640;
+constexpr int kTcThreads = BITS == 16 ? 384 : 640;
 
 template <typename T, int BITS>
 __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
@@ -277,7 +271,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < s.stages; ++i) {
-            mbar_init(full + i, a.gather ? 1 + 64 : 1);
+            mbar_init(full + i, 1);
             mbar_init(ready + i, kPacked ? 8 : 2);
             mbar_init(empty + i, 1);
         }
@@ -307,7 +301,6 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         for (int64_t r = a.offsets[a.experts] + blockIdx.x; r < a.rows; r += gridDim.x)
             for (int c = threadIdx.x; c < a.m; c += blockDim.x) static_cast<T *>(a.y)[r * a.ldy + c] = from_f32<T>(0.f);
 
-    const int loader = !a.gather ? -1 : kPacked ? warp - 2 : warp - 12;  // 0 or 1: copies rows of x
     bool ok = true;
     int st = 0;          // stage, and the parity of its barriers' current phase
     uint32_t phase = 0;
@@ -329,12 +322,12 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                     ok = false;
                     break;
                 }
-                if (lane == 0) mbar_arrive_expect_tx(full + st, (a.gather ? 0 : x_bytes) + 4 * kBlock);
+                if (lane == 0) mbar_arrive_expect_tx(full + st, x_bytes + 4 * kBlock);
                 __syncwarp();
                 uint8_t *dst = kPacked ? sm_raw + st * 4 * kBlock : sm_a + st * kABytes;
                 if (lane < 4)
                     bulk_g2s(dst + lane * kBlock, src + static_cast<size_t>(kb) * kBlock, kBlock, full + st);
-                else if (lane == 4 && !a.gather)
+                else if (lane == 4)
                     tma_tile(sm_x + st * x_bytes, &xmap, kb * 64, static_cast<int>(t.first) + rank * (s.nt / 2), full + st);
                 __syncwarp();
                 ++uses;
@@ -378,40 +371,6 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             }
             if (ok) mma2_commit_warp(acc_full + buf, both);
         }
-    } else if (loader == 0 || loader == 1) {
-        // ------------------------------------------------ rows of x that the expert picks
-        const int per = s.nt / 16, r0 = loader * (s.nt / 4) + (lane >> 3);  // this lane copies rows r0 + 4 i, i < per
-        const int c = lane & 7;
-        for (int id = pair; id < tiles && ok; id += pairs) {
-            const Tile t = tile_at(a, s, tab, us, id);
-            const T *src[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = rank * (s.nt / 2) + r0 + 4 * i;  // rows past the count repeat the first; they are not stored
-                src[i] = static_cast<const T *>(a.x) + (i < per ? a.order[t.first + (r < t.count ? r : 0)] / a.top : 0) * a.ldx;
-            }
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!mbar_wait_warp(empty + st, phase ^ 1, status)) {
-                    ok = false;
-                    break;
-                }
-                const int k = kb * 64 + c * 8;
-                const uint32_t bytes = max(0, min(16, 2 * (a.k - k)));
-                const int64_t at = bytes ? k : 0;
-                // rows four apart differ in bit 2 of the swizzle
-                const uint32_t dst = smem_addr(sm_x + st * x_bytes) + r0 * 128;
-                const uint32_t even = dst + (c ^ (r0 & 7)) * 16, odd = dst + 512 + (c ^ ((r0 + 4) & 7)) * 16;
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    if (i < per) cp_async16(even + i * 512, src[i] + at, bytes);
-                    if (i + 1 < per) cp_async16(odd + i * 512, src[i + 1] + at, bytes);
-                }
-                // this lane's copies arrive on the stage when they have landed; whoever hands the stage on fences them
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(full + st)) : "memory");
-                advance();
-            }
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == 2 && !kPacked) {
         // ------------------------------------------------ complete stages of 16-bit weights
         for (int id = pair; id < tiles && ok; id += pairs)
@@ -420,7 +379,6 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                     ok = false;
                     break;
                 }
-                if (a.gather) fence_proxy_async_smem();  // cp.async writes as the threads do; the MMAs read through the async proxy
                 if (lane == 0) mbar_arrive_at(ready + st, leader);
                 __syncwarp();
                 advance();
