@@ -109,7 +109,7 @@ struct CombineArgs {
     const void *residual;
     void *y;
     int64_t ldz, ldres, ldy, tokens;
-    int m, top;
+    int m, top, vec;  // vec: four neighbours of y and the residual at once
 };
 
 template <typename T>
@@ -119,15 +119,35 @@ __global__ void combine_kernel(const CombineArgs a)
     pdl_begin();
     for (int c = (blockIdx.y * blockDim.x + threadIdx.x) * 4; c < a.m; c += gridDim.y * blockDim.x * 4) {
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int j = 0; j < a.top; ++j) {
-            const int p = a.position[t * a.top + j];
-            if (p < 0) continue;
-            const float w = a.weights[t * a.top + j];
-            const float4 v = *reinterpret_cast<const float4 *>(a.z + p * a.ldz + c);
-            s.x = fmaf(w, v.x, s.x);
-            s.y = fmaf(w, v.y, s.y);
-            s.z = fmaf(w, v.z, s.z);
-            s.w = fmaf(w, v.w, s.w);
+        for (int j0 = 0; j0 < a.top; j0 += 4) {  // four rows in flight
+            float4 v[4];
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int p = j0 + i < a.top ? a.position[t * a.top + j0 + i] : -1;
+                w[i] = 0.f;
+                v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (p >= 0) {
+                    w[i] = a.weights[t * a.top + j0 + i];
+                    v[i] = __ldcs(reinterpret_cast<const float4 *>(a.z + p * a.ldz + c));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s.x = fmaf(w[i], v[i].x, s.x);
+                s.y = fmaf(w[i], v[i].y, s.y);
+                s.z = fmaf(w[i], v[i].z, s.z);
+                s.w = fmaf(w[i], v[i].w, s.w);
+            }
+        }
+        if (c + 4 <= a.m && a.vec) {
+            if (a.residual) {
+                const uint2 r = *reinterpret_cast<const uint2 *>(static_cast<const T *>(a.residual) + t * a.ldres + c);
+                const float2 lo = unpack2<T>(r.x), hi = unpack2<T>(r.y);
+                s.x += lo.x; s.y += lo.y; s.z += hi.x; s.w += hi.y;
+            }
+            *reinterpret_cast<uint2 *>(static_cast<T *>(a.y) + t * a.ldy + c) = make_uint2(pack2<T>(s.x, s.y), pack2<T>(s.z, s.w));
+            continue;
         }
         const float q[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
@@ -204,7 +224,9 @@ cudaError_t launch_combine(int dtype, const float *z, int64_t ldz, const float *
                            cudaStream_t st)
 {
     if (tokens == 0) return cudaSuccess;
-    const CombineArgs a = {z, weights, position, residual, y, ldz, ldres, ldy, tokens, m, top};
+    const int vec = reinterpret_cast<uintptr_t>(y) % 8 == 0 && ldy % 4 == 0 &&
+                    (!residual || (reinterpret_cast<uintptr_t>(residual) % 8 == 0 && ldres % 4 == 0));
+    const CombineArgs a = {z, weights, position, residual, y, ldz, ldres, ldy, tokens, m, top, vec};
     const dim3 grid(static_cast<unsigned>(tokens), (m + 1023) / 1024);
     return dtype == QNN_F16 ? launch_pdl(combine_kernel<__half>, grid, 256, 0, st, 1, a)
                             : launch_pdl(combine_kernel<__nv_bfloat16>, grid, 256, 0, st, 1, a);

@@ -2,7 +2,9 @@
 //
 // A unit of work is 32 image rows against a tile of NT rows of x (8, 16 or 32).  Resident blocks share the units evenly,
 // each a contiguous run of them (rows first, then tiles, experts one after another; the number of live tiles is known
-// only on the device).  The warps of a block split K, and their partial sums are added in shared memory in a fixed order.
+// only on the device).  The warps of a block split K, and their partial sums are added in shared memory in a fixed order;
+// where K is short, sets of four or two warps take units of their own, so that a warp has several blocks of a unit between
+// its ends.
 // Every warp copies its own blocks of the image (cp.async, whole lines) into a ring of its own, several blocks ahead and
 // across the ends of units: no registers hold loads in flight and no barrier of the block stands between a copy and its
 // use.  A lane's vector of packed codes is its A fragment; 32 bytes of a row of x are its B fragment.  The product is
@@ -107,7 +109,7 @@ struct StreamTile {
 };
 
 template <typename T, int BITS, int NT>
-__global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) matmul_stream_kernel(const MatmulArgs a, const int ranks)
+__global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) matmul_stream_kernel(const MatmulArgs a, const int ranks, const int wpu)
 {
     using R = Ring<BITS, NT>;
     constexpr int kN = NT / 8;
@@ -118,7 +120,11 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
     Part *parts = reinterpret_cast<Part *>(smem + kStreamWarps * R::kWarpBytes);
     int *tab = reinterpret_cast<int *>(smem + kStreamWarps * R::kWarpBytes + R::kPartBytes);  // tiles before each expert
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int rank = blockIdx.x % ranks, share = blockIdx.x / ranks, shares = gridDim.x / ranks;
+    // sets of `wpu` warps (all eight where a cluster splits K)
+    const int sets = kStreamWarps / wpu, set = warp / wpu, in_set = warp - set * wpu, set_threads = wpu * 32;
+    const int tid = threadIdx.x - set * set_threads;
+    const int rank = blockIdx.x % ranks, share = blockIdx.x / ranks * sets + set, shares = gridDim.x / ranks * sets;
+    auto set_barrier = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(set + 1), "r"(set_threads) : "memory"); };
 
     if (ranks > 1) cluster_arrive();  // (this block has started)
     pdl_begin();
@@ -150,7 +156,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
     };
 
     // this warp's share of K, in slots: columns (kb0 + i * step) * 64 ..., i < per
-    const int kb0 = (rank * kStreamWarps + warp) * R::kSub, step = ranks * kStreamWarps * R::kSub;
+    const int kb0 = (rank * wpu + in_set) * R::kSub, step = ranks * wpu * R::kSub;
     const int per = kb0 < a.kb ? (a.kb - kb0 + step - 1) / step : 0;
     const uint32_t wstep = step * kBlock;
     const uint32_t ring = smem_addr(smem) + warp * R::kWarpBytes;
@@ -160,6 +166,8 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
     int ck = a.kb, ctile = -1, ccount = 0;    // next column block of the unit before it, its tile, the tile's rows
     const uint8_t *wtile = nullptr, *wsrc = nullptr;
     const T *xrow[2 * kN];
+    // this lane's place among a block's rows of x: row lane / 8 (and every fourth after it), swizzled chunk lane % 8
+    const uint32_t xlane = (lane >> 3) * 128 + ((lane & 7) ^ (lane >> 3)) * 16;
     auto copy_next = [&](uint32_t slot) {
         if (ck >= a.kb) {
             const int tile = cu / a.mb, mb = cu - tile * a.mb;
@@ -180,31 +188,42 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
             ck = kb0;
             wsrc = wtile + (static_cast<size_t>(mb) * a.kb + kb0) * kBlock;
         }
+        // slot: the blocks' weights one after another, then their x
+        const uint32_t wdst = slot + lane * 16, xdst = slot + R::kSub * R::kWBytes + xlane;
+        if ((ck + R::kSub) * 64 <= a.k && a.x_vec) {  // whole blocks: the common case, few instructions
 #pragma unroll
-        for (int s = 0; s < R::kSub; ++s) {
-            if (ck + s >= a.kb) break;
-            const uint32_t dst = slot + s * (R::kWBytes + R::kXBytes);
-#pragma unroll
-            for (int i = 0; i < R::kWBytes / 512; ++i) cp_async16(dst + i * 512 + lane * 16, wsrc + s * kBlock + i * 512);
-            const int k0 = (ck + s) * 64;
-            const int left = 2 * (a.k - k0 - (lane & 7) * 8);  // bytes of the row from this lane's chunk on
+            for (int i = 0; i < R::kSub * R::kWBytes / 512; ++i) cp_async16(wdst + i * 512, wsrc + i * 512);
 #pragma unroll
             for (int i = 0; i < 2 * kN; ++i) {
                 if (i * 4 >= ccount) break;
-                const T *p = xrow[i] + k0;
-                const int r = i * 4 + (lane >> 3);
-                const uint32_t to = dst + R::kWBytes + r * 128 + ((lane & 7) ^ (r & 7)) * 16;
-                if (a.x_vec) {
-                    if (k0 + 64 <= a.k)
-                        cp_async16(to, p);
-                    else
-                        cp_async16_part(to, left > 0 ? p : static_cast<const T *>(a.x), max(0, min(16, left)));
-                } else {  // rows that are not 16-byte aligned, two bytes at a time
-                    const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
+                const T *p = xrow[i] + ck * 64;
+                // rows four apart differ in bit 2 of the swizzle
+                const uint32_t to = (i & 1 ? xdst ^ 64 : xdst) + i * 512;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint16_t v = 2 * e < left ? q[e] : 0;
-                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + e * 2), "h"(v) : "memory");
+                for (int s = 0; s < R::kSub; ++s) cp_async16(to + s * R::kXBytes, p + s * 64);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < R::kSub; ++s) {
+                if (ck + s >= a.kb) break;
+#pragma unroll
+                for (int i = 0; i < R::kWBytes / 512; ++i) cp_async16(wdst + s * kBlock + i * 512, wsrc + s * kBlock + i * 512);
+                const int k0 = (ck + s) * 64;
+                const int left = 2 * (a.k - k0 - (lane & 7) * 8);  // bytes of the row from this lane's chunk on
+#pragma unroll
+                for (int i = 0; i < 2 * kN; ++i) {
+                    if (i * 4 >= ccount) break;
+                    const T *p = xrow[i] + k0;
+                    const uint32_t to = (i & 1 ? xdst ^ 64 : xdst) + i * 512 + s * R::kXBytes;
+                    if (a.x_vec) {
+                        cp_async16_part(to, left > 0 ? p : static_cast<const T *>(a.x), max(0, min(16, left)));
+                    } else {  // rows that are not 16-byte aligned, two bytes at a time
+                        const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint16_t v = 2 * e < left ? q[e] : 0;
+                            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + e * 2), "h"(v) : "memory");
+                        }
                     }
                 }
             }
@@ -218,7 +237,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
     StreamTile cur = {0, 0, 0};
     int cur_tile = -1;
     const int chans = a.gated ? 16 : 32, shift = a.gated ? 4 : 5;
-    const int my_c = threadIdx.x & (chans - 1), my_r = a.gated ? (my_c >> 3) * 16 + (my_c & 7) : my_c;
+    const int my_c = tid & (chans - 1), my_r = a.gated ? (my_c >> 3) * 16 + (my_c & 7) : my_c;
     float2 q0, q1;  // scale and bias of this thread's channel (gate and up), loaded while the unit's blocks arrive
     int cur_mb = 0;
     auto begin_unit = [&](int unit) {
@@ -245,12 +264,14 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
                     part[warp * 32 + j * 16 + g + (i >> 1) * 8][n * 8 + 2 * t + (i & 1)] = s;
                     acc[0][j][n][i] = acc[kChains - 1][j][n][i] = 0.f;
                 }
-        __syncthreads();
-        // row r of the image, row n of x, added over the warps
+        set_barrier();
+        // row r of the image, row n of x, added over the set's warps (or over the blocks of a cluster)
         auto sum = [&](const Part &part, int r, int n) {
-            float s = 0.f;
-#pragma unroll
-            for (int p = 0; p < kStreamWarps; ++p) s += part[p * 32 + r][n];
+            const float *p = &part[set * wpu * 32 + r][n];
+            constexpr int kStep = 32 * (NT + 1);
+            float s = p[0] + p[kStep];
+            if (wpu > 2) s += p[2 * kStep] + p[3 * kStep];
+            if (wpu > 4) s += (p[4 * kStep] + p[5 * kStep]) + (p[6 * kStep] + p[7 * kStep]);
             return s;
         };
         const Part *from = &part;
@@ -272,7 +293,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
         }
         const int64_t col = static_cast<int64_t>(cur_mb) * chans + my_c;
         if (col < a.m)
-            for (int n = threadIdx.x >> shift; n < cur.count; n += (kStreamWarps * 32) >> shift) {
+            for (int n = tid >> shift; n < cur.count; n += set_threads >> shift) {
                 float s = activate(fmaf(sum(*from, my_r, n), q0.x, q0.y), a.act);
                 if (a.gated) s *= fmaf(sum(*from, my_r + 8, n), q1.x, q1.y);
                 finish<T>(a, cur.first + n, col, s);
@@ -298,7 +319,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
 #pragma unroll
         for (int s = 0; s < R::kSub; ++s) {
             if (kb0 + in_unit * step + s >= a.kb) break;
-            const uint32_t at = base + s * (R::kWBytes + R::kXBytes);
+            const uint32_t at = base + s * R::kWBytes, xat = base + R::kSub * R::kWBytes + s * R::kXBytes;
             uint32_t w[BITS * 2], x[kN][8];
 #pragma unroll
             for (int i = 0; i < BITS / 2; ++i) {
@@ -310,7 +331,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Ring<BITS, NT>::kPerSm) mat
             for (int n = 0; n < kN; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const uint4 q = lds16(at + R::kWBytes + (n * 8 + g) * 128 + ((2 * t + i) ^ g) * 16);
+                    const uint4 q = lds16(xat + (n * 8 + g) * 128 + ((2 * t + i) ^ g) * 16);
                     x[n][4 * i] = q.x; x[n][4 * i + 1] = q.y; x[n][4 * i + 2] = q.z; x[n][4 * i + 3] = q.w;
                 }
 #pragma unroll
@@ -357,9 +378,14 @@ cudaError_t launch_one(const MatmulArgs &a, int64_t tiles, cudaStream_t st)
     const int64_t slots = R::kPerSm * device_sm_count(), units = tiles * a.mb;
     int ranks = 1;
     while (!a.offsets && ranks < 8 && 2 * ranks * units <= slots && a.kb >= 2 * ranks * kStreamWarps * R::kSub) ranks *= 2;
-    const int64_t shares = ranks > 1 ? units : std::min(slots, units);
+    // Warps to a unit: fewer while a warp has less than eight blocks of it.  (30 experts of 2 * 1024 rows
+    // and 2048 columns, INT-4: 27.7 us with four warps a unit, 28.7 with eight.)
+    int wpu = kStreamWarps;
+    while (ranks == 1 && wpu > 2 && a.kb < 8 * wpu && 2 * units > slots * (kStreamWarps / wpu)) wpu /= 2;
+    const int64_t sets = kStreamWarps / wpu;
+    const int64_t shares = ranks > 1 ? units : std::min(slots, (units + sets - 1) / sets);
     return launch_pdl(matmul_stream_kernel<T, BITS, NT>, dim3(static_cast<unsigned>(shares * ranks)), kStreamWarps * 32, R::kSmem, st,
-                      ranks, a, ranks);
+                      ranks, a, ranks, wpu);
 }
 
 template <typename T, int BITS>

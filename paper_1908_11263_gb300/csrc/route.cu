@@ -1,9 +1,11 @@
 // qnn_route_topk() and qnn_expert_plan(): which experts a token goes to, and the tokens each expert gets.
 //
-// route_topk_kernel: one warp owns one token; lane l holds experts l, l + 32, ...  Scores are compared as 32-bit keys
-// whose unsigned order is the order of the floats, so the warp's best expert is one integer maximum over the lanes and
-// the lowest index among equals one integer minimum: ties go to the lowest index by construction.  The choice uses the
-// score itself (the logit where softmax scores carry no bias: the same order without rounding).
+// route_topk_kernel: one warp owns one token; lane l holds NV neighbouring experts from l * NV on.  Scores are compared as
+// 32-bit keys whose unsigned order is the order of the floats, so the warp's best expert is one integer maximum over the
+// lanes and the lowest index among equals one integer minimum: ties go to the lowest index by construction.  The choice
+// uses the score itself (the logit where softmax scores carry no bias: the same order without rounding).  Groups that are
+// whole lanes, a power of two of them, find their two best with a few shuffles; other splits go through shared memory.
+// The kernel is bound by its instructions, not by the logits' bytes.
 //
 // expert plan: a stable counting sort of the slots (token * top + choice) by expert.  Ranks come from ordered per-warp
 // counts, never from the order in which atomics land, so the plan is the same on every run.
@@ -24,6 +26,7 @@ struct RouteArgs {
     int64_t t, ld;
     int e, k, sigmoid, groups, top_groups, two, renorm;
     int group_size;
+    int vec;               // rows are aligned for 16-byte loads
     uint32_t group_magic;  // expert / group_size = (expert * magic) >> 20 for experts below 1024
     float scale;
 };
@@ -45,6 +48,26 @@ __device__ __forceinline__ float score_of(float v, int sigmoid, float top)
     return sigmoid ? 1.f / __fadd_rn(1.f, expf(-v)) : exp_from(v, top);
 }
 
+// NV (a multiple of four) neighbouring logits.
+template <typename T, int NV>
+__device__ __forceinline__ void load_run(const T *p, float (&x)[NV])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i + 4 <= NV; i += 4) {
+            const float4 q = *reinterpret_cast<const float4 *>(p + i);
+            x[i] = q.x; x[i + 1] = q.y; x[i + 2] = q.z; x[i + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i + 4 <= NV; i += 4) {
+            const uint2 q = *reinterpret_cast<const uint2 *>(p + i);
+            const float2 f = unpack2<T>(q.x), h = unpack2<T>(q.y);
+            x[i] = f.x; x[i + 1] = f.y; x[i + 2] = h.x; x[i + 3] = h.y;
+        }
+    }
+}
+
 template <typename T, int NV>
 __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const RouteArgs a)
 {
@@ -54,12 +77,14 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
     pdl_begin();
     if (token >= a.t) return;
     const T *row = static_cast<const T *>(a.logits) + token * a.ld;
+    const int e0 = lane * NV;  // this lane's first expert
 
     float x[NV];
+    if (NV >= 4 && a.vec && e0 + NV <= a.e) {
+        load_run<T, NV>(row + e0, x);
+    } else {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int e = i * 32 + lane;
-        x[i] = e < a.e ? to_f32<T>(row[e]) : -INFINITY;
+        for (int i = 0; i < NV; ++i) x[i] = e0 + i < a.e ? to_f32<T>(row[e0 + i]) : -INFINITY;
     }
     float top = 0.f, total = 1.f;
     if (!a.sigmoid) {
@@ -78,70 +103,111 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
         }
     }
     // what the choice goes by
+    const bool scored = a.sigmoid || a.bias;
     uint32_t key[NV];
-    float *sc = sm_scores + (threadIdx.x >> 5) * a.e;
+    float of[NV];  // what groups go by
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int e = i * 32 + lane;
         float c = x[i];
-        if (c > -INFINITY && (a.sigmoid || a.bias)) {
+        if (scored) {
             c = score_of(x[i], a.sigmoid, top);
             if (!a.sigmoid) c /= total;
-            if (a.bias) c += a.bias[e];
+            if (a.bias && e0 + i < a.e) c += a.bias[e0 + i];
         }
-        key[i] = order_key(c);
-        if (a.groups > 1 && e < a.e) {
-            if (!a.sigmoid && !a.bias && a.two && key[i]) c = score_of(x[i], 0, top);  // sums need the scores themselves
-            sc[e] = key[i] ? c : -INFINITY;
+        key[i] = x[i] > -INFINITY ? order_key(c) : 0u;
+        if (a.groups > 1) {
+            // sums need the scores themselves
+            of[i] = key[i] == 0u ? -INFINITY : !scored && a.two ? score_of(x[i], 0, top) : c;
         }
     }
     if (a.groups > 1) {
-        __syncwarp();
-        // lane g scores group g: its best expert, or the sum of its two best
-        float best = -INFINITY;
-        if (lane < a.groups) {
-            float second = -INFINITY;
-            int j = lane % a.group_size;  // a start of its own a lane: fewer bank conflicts
-            for (int n = 0; n < a.group_size; ++n) {
-                const float v = sc[lane * a.group_size + j];
-                second = fmaxf(second, fminf(best, v));
-                best = fmaxf(best, v);
-                j = j + 1 == a.group_size ? 0 : j + 1;
+        uint32_t mine = 0u;  // key of this lane's group; the group's first lane speaks for it
+        int group;
+        const int width = a.group_size / NV;  // lanes a group
+        const bool lanes = a.group_size % NV == 0 && (width & (width - 1)) == 0;
+        if (lanes) {
+            float best = of[0], second = -INFINITY;
+#pragma unroll
+            for (int i = 1; i < NV; ++i) {
+                second = fmaxf(second, fminf(best, of[i]));
+                best = fmaxf(best, of[i]);
+            }
+            for (int o = 1; o < width; o <<= 1) {
+                const float b = __shfl_xor_sync(kFull, best, o), s = __shfl_xor_sync(kFull, second, o);
+                second = fmaxf(fmaxf(second, s), fminf(best, b));
+                best = fmaxf(best, b);
             }
             if (a.two && second > -INFINITY) best += second;
-        }
-        const uint32_t mine = lane < a.groups ? order_key(best) : 0u;
-        int rank = 0;
-        for (int g = 0; g < a.groups; ++g) {
-            const uint32_t o = __shfl_sync(kFull, mine, g);
-            rank += o > mine || (o == mine && g < lane);
-        }
-        const uint32_t keep = __ballot_sync(kFull, lane < a.groups && rank < a.top_groups);
+            group = lane / width;
+            mine = group < a.groups ? order_key(best) : 0u;
+        } else {
+            float *sc = sm_scores + (threadIdx.x >> 5) * a.e;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t e = i * 32 + lane;
-            const uint32_t g = (e * a.group_magic) >> 20;
-            if (e >= static_cast<uint32_t>(a.e) || !((keep >> (g & 31)) & 1)) key[i] = 0u;
+            for (int i = 0; i < NV; ++i)
+                if (e0 + i < a.e) sc[e0 + i] = of[i];
+            __syncwarp();
+            group = lane;
+            if (lane < a.groups) {
+                float best = -INFINITY, second = -INFINITY;
+                int j = lane % a.group_size;  // a start of its own a lane: fewer bank conflicts
+                for (int n = 0; n < a.group_size; ++n) {
+                    const float v = sc[lane * a.group_size + j];
+                    second = fmaxf(second, fminf(best, v));
+                    best = fmaxf(best, v);
+                    j = j + 1 == a.group_size ? 0 : j + 1;
+                }
+                if (a.two && second > -INFINITY) best += second;
+                mine = order_key(best);
+            }
+        }
+        uint32_t keep = 0u;
+        for (int n = 0; n < a.top_groups; ++n) {
+            const uint32_t top_key = __reduce_max_sync(kFull, mine);
+            if (top_key == 0u) break;
+            const uint32_t g = __reduce_min_sync(kFull, mine == top_key ? static_cast<uint32_t>(group) : kFull);
+            keep |= 1u << g;
+            if (static_cast<uint32_t>(group) == g) mine = 0u;
+        }
+        if (lanes) {
+            if (!((keep >> (group & 31)) & 1) || group >= a.groups)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) key[i] = 0u;
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t g = (static_cast<uint32_t>(e0 + i) * a.group_magic) >> 20;
+                if (!((keep >> (g & 31)) & 1)) key[i] = 0u;
+            }
         }
     }
     // the k best, one warp maximum each; lane j keeps choice j
     int id = -1;
-    for (int j = 0; j < a.k; ++j) {
-        uint32_t best = key[0];
-        int at = 0;
+    uint32_t best = 0u;  // this lane's best key left, and its place
+    int at = 0;
+    auto rank_lane = [&]() {
+        best = key[0];
+        at = 0;
 #pragma unroll
         for (int i = 1; i < NV; ++i)
             if (key[i] > best) {
                 best = key[i];
                 at = i;
             }
+    };
+    rank_lane();
+    for (int j = 0; j < a.k; ++j) {
         const uint32_t top_key = __reduce_max_sync(kFull, best);
         if (top_key == 0u) break;
-        const uint32_t e = __reduce_min_sync(kFull, best == top_key ? static_cast<uint32_t>(at * 32 + lane) : kFull);
-        if (lane == j) id = static_cast<int>(e);
+        // lanes hold neighbours in order, so the lowest lane has the lowest index
+        const int owner = __ffs(__ballot_sync(kFull, best == top_key)) - 1;
+        const int e = __shfl_sync(kFull, e0 + at, owner);
+        if (lane == j) id = e;
+        if (lane == owner) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (e == static_cast<uint32_t>(i * 32 + lane)) key[i] = 0u;
+            for (int i = 0; i < NV; ++i)
+                if (at == i) key[i] = 0u;
+            rank_lane();
+        }
     }
     float w = 0.f;
     if (id >= 0) {
@@ -194,17 +260,17 @@ __global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const int32_t 
         if (e >= 0) atomicAdd(&sm_plan[e], 1);
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < experts; e += kPlanThreads) counts[static_cast<int64_t>(blockIdx.x) * experts + e] = sm_plan[e];
+    for (int e = threadIdx.x; e < experts; e += kPlanThreads) counts[e * gridDim.x + blockIdx.x] = sm_plan[e];
 }
 
-// counts: per-block counts of plan_count_kernel, or NULL when one block holds all slots.
+// counts: plan_count_kernel's [expert][block], or NULL when one block holds all slots.
 __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t *ids, int64_t slots, int64_t chunk,
                                                                   int experts, const int32_t *counts, int32_t *offsets,
                                                                   int32_t *order, int32_t *position)
 {
-    extern __shared__ int32_t sm_plan[];  // [warps][experts] counts, then [experts] starts
+    extern __shared__ int32_t sm_plan[];  // [warps][experts] counts, then [experts] starts and totals
     __shared__ int32_t part[32];
-    int32_t *start = sm_plan + kPlanWarps * experts;
+    int32_t *start = sm_plan + kPlanWarps * experts, *totals = start + experts;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int i = threadIdx.x; i < kPlanWarps * experts; i += kPlanThreads) sm_plan[i] = 0;
     __syncthreads();
@@ -218,7 +284,29 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
         if (e >= 0) atomicAdd(&mine[e], 1);
     }
     __syncthreads();
-    // exclusive counts over the warps; totals over all blocks, and over the blocks before this one
+    if (counts) {
+        // a warp an expert: its slots over all blocks (at most 128), and over the blocks before this one
+        const int blocks = gridDim.x;
+#pragma unroll 4
+        for (int e = warp; e < experts; e += kPlanWarps) {
+            int all = 0, before = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int b = i * 32 + lane;
+                const int c = b < blocks ? counts[e * blocks + b] : 0;
+                all += c;
+                before += b < static_cast<int>(blockIdx.x) ? c : 0;
+            }
+            all = __reduce_add_sync(kFull, all);
+            before = __reduce_add_sync(kFull, before);
+            if (lane == 0) {
+                totals[e] = all;
+                start[e] = before;
+            }
+        }
+        __syncthreads();
+    }
+    // exclusive counts over the warps; exclusive scan of the totals over the experts
     int32_t running = 0;
     for (int base = 0; base < experts; base += kPlanThreads) {
         const int e = base + threadIdx.x;
@@ -230,17 +318,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
                 sm_plan[w * experts + e] = own;
                 own += c;
             }
-            total = own;
-            if (counts) {
-                total = 0;
-                for (int b = 0; b < static_cast<int>(gridDim.x); ++b) {
-                    const int32_t c = counts[static_cast<int64_t>(b) * experts + e];
-                    before += b < static_cast<int>(blockIdx.x) ? c : 0;
-                    total += c;
-                }
-            }
+            total = counts ? totals[e] : own;
+            before = counts ? start[e] : 0;
         }
-        // exclusive scan of the totals over the experts
         int32_t inc = total;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -312,6 +392,8 @@ cudaError_t launch_route_topk(const qnn_route_desc &d, const void *logits, const
     a.top_groups = d.top_groups; a.two = d.group_score == QNN_GROUP_TOP2; a.renorm = d.renormalise; a.scale = d.scale;
     a.group_size = d.experts / d.groups;
     a.group_magic = ((1u << 20) + a.group_size - 1) / a.group_size;
+    const int64_t row_bytes = d.ld * (d.dtype == QNN_F32 ? 4 : 2);
+    a.vec = reinterpret_cast<uintptr_t>(logits) % 16 == 0 && row_bytes % 16 == 0;
     if (d.dtype == QNN_F32) return launch_route_type<float>(a, stream);
     if (d.dtype == QNN_F16) return launch_route_type<__half>(a, stream);
     return launch_route_type<__nv_bfloat16>(a, stream);
@@ -330,7 +412,7 @@ cudaError_t launch_expert_plan(const int32_t *ids, int64_t slots, int experts, i
     int64_t chunk;
     const int nb = plan_blocks(slots, &chunk);
     int32_t *counts = nb > 1 ? static_cast<int32_t *>(workspace) : nullptr;
-    const size_t smem = sizeof(int32_t) * (kPlanWarps + 1) * experts;
+    const size_t smem = sizeof(int32_t) * (kPlanWarps + 2) * experts;
     if (smem > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    static_cast<int>(smem));
