@@ -26,7 +26,7 @@ struct RouteArgs {
     int64_t t, ld;
     int e, k, sigmoid, groups, top_groups, two, renorm;
     int group_size;
-    int vec;               // rows are aligned for 16-byte loads
+    int vec, bias_vec;     // rows of logits, and the bias, are aligned for 16-byte loads
     uint32_t group_magic;  // expert / group_size = (expert * magic) >> 20 for experts below 1024
     float scale;
 };
@@ -39,15 +39,21 @@ __device__ __forceinline__ uint32_t order_key(float v)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ float exp_from(float v, float top) { return top == INFINITY ? (v == INFINITY ? 1.f : 0.f) : expf(v - top); }
+// exp(v - top); where the largest logit is infinite, the infinite ones share the weight
+__device__ __forceinline__ float exp_from(float v, float top)
+{
+    const float e = expf(v - (top == INFINITY ? 0.f : top));
+    return top == INFINITY ? (v == INFINITY ? 1.f : 0.f) : e;
+}
+
+// The sum is rounded by itself, so that a score is the same wherever it is computed.
+__device__ __forceinline__ float sigmoid_of(float v) { return __frcp_rn(__fadd_rn(1.f, expf(-v))); }
 
 __device__ __forceinline__ float score_of(float v, int sigmoid, float top)
 {
-    if (!(v > -INFINITY)) return 0.f;
-    // the sum rounded by itself, so that a score is the same wherever it is computed
-    return sigmoid ? 1.f / __fadd_rn(1.f, expf(-v)) : exp_from(v, top);
+    if (sigmoid) return v > -INFINITY ? sigmoid_of(v) : 0.f;
+    return v > -INFINITY ? exp_from(v, top) : 0.f;
 }
-
 // NV (a multiple of four) neighbouring logits.
 template <typename T, int NV>
 __device__ __forceinline__ void load_run(const T *p, float (&x)[NV])
@@ -71,6 +77,7 @@ __device__ __forceinline__ void load_run(const T *p, float (&x)[NV])
 template <typename T, int NV>
 __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const RouteArgs a)
 {
+    __shared__ uint2 candidates[kRouteWarps][64];  // key and expert
     extern __shared__ float sm_scores[];  // one row of group_size * groups scores a warp (grouped calls only)
     const int lane = threadIdx.x & 31;
     const int64_t token = static_cast<int64_t>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5);
@@ -105,20 +112,35 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
     // what the choice goes by
     const bool scored = a.sigmoid || a.bias;
     uint32_t key[NV];
-    float of[NV];  // what groups go by
+    float of[NV], bias[NV];  // what groups go by
+    if (NV >= 4 && a.bias && a.bias_vec && e0 + NV <= a.e) {
+        load_run<float, NV>(a.bias + e0, bias);
+    } else {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        float c = x[i];
-        if (scored) {
-            c = score_of(x[i], a.sigmoid, top);
-            if (!a.sigmoid) c /= total;
-            if (a.bias && e0 + i < a.e) c += a.bias[e0 + i];
+        for (int i = 0; i < NV; ++i) bias[i] = a.bias && e0 + i < a.e ? a.bias[e0 + i] : 0.f;
+    }
+    // Straight-line loops, the mode outside: a closed expert's logit counts as 0 here (its key is 0 below), which also keeps
+    // the exponential and the reciprocal off their slow paths for infinities.
+    float c[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) c[i] = x[i];
+    if (a.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) c[i] = __fadd_rn(sigmoid_of(x[i] > -INFINITY ? x[i] : 0.f), bias[i]);
+    } else if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) c[i] = score_of(x[i], 0, top) / total + bias[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) key[i] = x[i] > -INFINITY ? order_key(c[i]) : 0u;
+    if (a.groups > 1) {
+        // sums need the scores themselves
+        if (!scored && a.two) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) c[i] = score_of(x[i], 0, top);
         }
-        key[i] = x[i] > -INFINITY ? order_key(c) : 0u;
-        if (a.groups > 1) {
-            // sums need the scores themselves
-            of[i] = key[i] == 0u ? -INFINITY : !scored && a.two ? score_of(x[i], 0, top) : c;
-        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) of[i] = key[i] == 0u ? -INFINITY : c[i];
     }
     if (a.groups > 1) {
         uint32_t mine = 0u;  // key of this lane's group; the group's first lane speaks for it
@@ -180,33 +202,71 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
             }
         }
     }
-    // the k best, one warp maximum each; lane j keeps choice j
+    // The k best, one warp maximum each; lane j keeps choice j.  Few keys can be among them: at least k are as large as the
+    // k-th largest of the lanes' maxima, so only keys from there on are candidates, about a dozen of 256.  They are moved
+    // together, at most two to a lane, which makes a step a few instructions instead of a search through NV keys.
     int id = -1;
-    uint32_t best = 0u;  // this lane's best key left, and its place
-    int at = 0;
-    auto rank_lane = [&]() {
-        best = key[0];
-        at = 0;
+    uint32_t best = key[0];
 #pragma unroll
-        for (int i = 1; i < NV; ++i)
-            if (key[i] > best) {
-                best = key[i];
-                at = i;
-            }
-    };
-    rank_lane();
+    for (int i = 1; i < NV; ++i) best = max(best, key[i]);
+    uint32_t least = best, floor_key = 1u;  // the k-th largest maximum; 1 (any open expert) where there are fewer
     for (int j = 0; j < a.k; ++j) {
-        const uint32_t top_key = __reduce_max_sync(kFull, best);
-        if (top_key == 0u) break;
-        // lanes hold neighbours in order, so the lowest lane has the lowest index
-        const int owner = __ffs(__ballot_sync(kFull, best == top_key)) - 1;
-        const int e = __shfl_sync(kFull, e0 + at, owner);
-        if (lane == j) id = e;
-        if (lane == owner) {
+        const uint32_t top_key = __reduce_max_sync(kFull, least);
+        if (top_key == 0u) {
+            floor_key = 1u;
+            break;
+        }
+        floor_key = top_key;
+        // one lane a step: equal maxima count one by one
+        const uint32_t who = __ballot_sync(kFull, least == top_key);
+        if (lane == __ffs(who) - 1) least = 0u;
+    }
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) count += key[i] >= floor_key;
+    int before = count;  // lanes in order, so candidates lie in the order of their experts
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(kFull, before, o);
+        if (lane >= o) before += v;
+    }
+    const int all = __shfl_sync(kFull, before, 31);
+    if (all <= 64) {
+        uint2 *mine = candidates[threadIdx.x >> 5];
+        int at = before - count;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (key[i] >= floor_key) mine[at++] = make_uint2(key[i], e0 + i);
+        __syncwarp();
+        uint2 c0 = lane < all ? mine[lane] : make_uint2(0u, kFull), c1 = lane + 32 < all ? mine[lane + 32] : make_uint2(0u, kFull);
+        for (int j = 0; j < a.k; ++j) {
+            const uint32_t top_key = __reduce_max_sync(kFull, max(c0.x, c1.x));
+            if (top_key == 0u) break;
+            // the lower expert of the two where both are equal: c0 comes first
+            const uint32_t e = __reduce_min_sync(kFull, c0.x == top_key ? c0.y : c1.x == top_key ? c1.y : kFull);
+            if (lane == j) id = static_cast<int>(e);
+            if (c0.y == e) c0.x = 0u;
+            if (c1.y == e) c1.x = 0u;
+        }
+    } else {  // many equal scores
+        for (int j = 0; j < a.k; ++j) {
+            uint32_t lane_best = key[0];
+            int at = 0;
+#pragma unroll
+            for (int i = 1; i < NV; ++i)
+                if (key[i] > lane_best) {
+                    lane_best = key[i];
+                    at = i;
+                }
+            const uint32_t top_key = __reduce_max_sync(kFull, lane_best);
+            if (top_key == 0u) break;
+            // lanes hold neighbours in order, so the lowest lane has the lowest index
+            const int owner = __ffs(__ballot_sync(kFull, lane_best == top_key)) - 1;
+            const int e = __shfl_sync(kFull, e0 + at, owner);
+            if (lane == j) id = e;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (at == i) key[i] = 0u;
-            rank_lane();
+                if (e == e0 + i) key[i] = 0u;
         }
     }
     float w = 0.f;
@@ -286,9 +346,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
     __syncthreads();
     if (counts) {
         // a warp an expert: its slots over all blocks (at most 128), and over the blocks before this one
-        const int blocks = gridDim.x;
+        const int blocks = gridDim.x, rounds = (experts + kPlanWarps - 1) / kPlanWarps;
 #pragma unroll 4
-        for (int e = warp; e < experts; e += kPlanWarps) {
+        for (int n = 0; n < rounds; ++n) {
+            // every block starts at another expert: all of them at the same rows at once would queue at one L2 slice
+            const int e = (n + static_cast<int>(blockIdx.x)) % rounds * kPlanWarps + warp;
+            if (e >= experts) continue;
             int all = 0, before = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -394,6 +457,7 @@ cudaError_t launch_route_topk(const qnn_route_desc &d, const void *logits, const
     a.group_magic = ((1u << 20) + a.group_size - 1) / a.group_size;
     const int64_t row_bytes = d.ld * (d.dtype == QNN_F32 ? 4 : 2);
     a.vec = reinterpret_cast<uintptr_t>(logits) % 16 == 0 && row_bytes % 16 == 0;
+    a.bias_vec = reinterpret_cast<uintptr_t>(bias) % 16 == 0;
     if (d.dtype == QNN_F32) return launch_route_type<float>(a, stream);
     if (d.dtype == QNN_F16) return launch_route_type<__half>(a, stream);
     return launch_route_type<__nv_bfloat16>(a, stream);
