@@ -46,12 +46,13 @@ qnn_status check_image(const qnn_matmul_desc &d, const void *image, size_t bytes
     return aligned(image, 256) ? QNN_OK : QNN_EALIGN;
 }
 
-// The tensor-core kernel takes over where a matrix meets more rows of x than this (on average, for experts).
-constexpr int64_t kStreamRows = 32, kStreamExpertRows = 16;
-
-bool on_tensor_cores(int64_t rows, int experts)
+// The tensor-core kernel takes over where a matrix meets more rows of x than this, on average for experts.  Measured on
+// both sides (us, streaming / tensor cores): 32 rows of 4096 x 4096 INT-4 9.4 / 17.6, 16-bit 10.7 / 16.0; 64 experts of
+// 2 * 1024 x 2048, INT-4 with 16 rows an expert 82 / 106, 16-bit with 4 rows 77 / 76, with 6 rows 101 / 85, with 8 rows
+// 109 / 83 (the stream reads 16-bit weights again for every 8 or 16 rows; of packed ones it mostly expands the codes).
+bool on_tensor_cores(int64_t rows, int experts, int bits)
 {
-    return experts ? rows > kStreamExpertRows * experts : rows > kStreamRows;
+    return rows > (experts ? static_cast<int64_t>(bits == 16 ? 6 : 16) * experts : 32);
 }
 
 int64_t align8(int64_t v) { return (v + 7) / 8 * 8; }
@@ -61,13 +62,13 @@ size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 // of the plan for a dispatch, 16-byte aligned.
 size_t staging_bytes(const qnn_matmul_desc &d, int64_t rows, int experts, bool gather, const void *x, int64_t ldx)
 {
-    if (!on_tensor_cores(rows, experts) || (!gather && aligned(x, 16) && ldx % 8 == 0)) return 0;
+    if (!on_tensor_cores(rows, experts, d.bits) || (!gather && aligned(x, 16) && ldx % 8 == 0)) return 0;
     return static_cast<size_t>(rows) * align8(d.k) * 2;
 }
 
 cudaError_t run_product(MatmulArgs a, const qnn_matmul_desc &d, void *staging, cudaStream_t st)
 {
-    if (!on_tensor_cores(a.rows, a.offsets ? a.experts : 0)) return launch_matmul_stream(a, d.dtype, d.bits, st);
+    if (!on_tensor_cores(a.rows, a.offsets ? a.experts : 0, d.bits)) return launch_matmul_stream(a, d.dtype, d.bits, st);
     if (a.gather || !a.x_vec) {
         const cudaError_t e = launch_take_rows(a.x, a.ldx, a.gather ? a.order : nullptr, a.top, staging, align8(d.k), a.rows, d.k, st);
         if (e != cudaSuccess) return e;

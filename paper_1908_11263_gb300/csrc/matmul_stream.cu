@@ -371,7 +371,7 @@ template <typename T, int BITS, int NT>
 cudaError_t launch_one(const MatmulArgs &a, int64_t tiles, cudaStream_t st)
 {
     using R = Ring<BITS, NT>;
-    const cudaError_t e = cudaFuncSetAttribute(matmul_stream_kernel<T, BITS, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, R::kSmem);
+    const cudaError_t e = raise_smem<matmul_stream_kernel<T, BITS, NT>>(R::kSmem);
     if (e != cudaSuccess) return e;
     // A block for every slot of the GPU, or for every unit; K split over clusters while those fill half of the slots at most
     // and every warp keeps a slot of K.

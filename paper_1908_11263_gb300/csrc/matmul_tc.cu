@@ -544,19 +544,8 @@ TcShape shape_of(const MatmulArgs &a, int bits, int nt, int ranks)
 template <typename T, int BITS>
 cudaError_t launch_tc(const CUtensorMap &map, const MatmulArgs &a, const TcShape &s, int64_t tiles, int *status, cudaStream_t st)
 {
-    static std::mutex mu;
-    static unsigned raised = 0;  // devices whose shared-memory limit is raised
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    const cudaError_t e = raise_smem<matmul_tc_kernel<T, BITS>>(227 * 1024);
     if (e != cudaSuccess) return e;
-    {
-        std::lock_guard<std::mutex> lock(mu);
-        if (dev >= 32 || !(raised >> dev & 1)) {
-            e = cudaFuncSetAttribute(matmul_tc_kernel<T, BITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-            if (e != cudaSuccess) return e;
-            if (dev < 32) raised |= 1u << dev;
-        }
-    }
     const int64_t pairs = device_sm_count() / 2;
     const unsigned grid = static_cast<unsigned>(s.ranks > 1 ? 2 * s.ranks * tiles : 2 * (tiles < pairs ? tiles : pairs));
     return launch_pdl(matmul_tc_kernel<T, BITS>, dim3(grid), kTcThreads<BITS>, s.smem, st, 2 * s.ranks, map, a, s, status);

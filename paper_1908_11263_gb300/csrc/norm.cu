@@ -398,8 +398,7 @@ cudaError_t launch_stream(const NormArgs &a, int64_t t, cudaStream_t stream, boo
     // a few rows a block at least, or the ring does not pay for itself
     if (s.stages < 2 || t < 3ll * per_sm * sms) return cudaSuccess;
     const size_t smem = static_cast<size_t>(s.stages) * stage;
-    const cudaError_t e = cudaFuncSetAttribute(block_norm_stream_kernel<T, R, VEC>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(room));
+    const cudaError_t e = raise_smem<block_norm_stream_kernel<T, R, VEC>>(room);
     if (e != cudaSuccess) return e;
     *taken = true;
     return launch_pdl(block_norm_stream_kernel<T, R, VEC>, dim3(per_sm * sms), threads, smem, stream, 1, a, s, t, status);

@@ -478,8 +478,7 @@ cudaError_t launch_expert_plan(const int32_t *ids, int64_t slots, int experts, i
     int32_t *counts = nb > 1 ? static_cast<int32_t *>(workspace) : nullptr;
     const size_t smem = sizeof(int32_t) * (kPlanWarps + 2) * experts;
     if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   static_cast<int>(smem));
+        const cudaError_t e = raise_smem<plan_place_kernel>(sizeof(int32_t) * (kPlanWarps + 2) * 1024);
         if (e != cudaSuccess) return e;
     }
     if (counts) {

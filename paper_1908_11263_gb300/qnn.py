@@ -687,16 +687,15 @@ class ExpertPlan:
 
     @property
     def order(self):
-        return self._buffer[:self.tokens * self.top]
+        return self._buffer.narrow(0, 0, self.tokens * self.top)
 
     @property
     def position(self):
-        slots = self.tokens * self.top
-        return self._buffer[slots:2 * slots].view(self.tokens, self.top)
+        return self._buffer.as_strided((self.tokens, self.top), (self.top, 1), self.tokens * self.top)
 
     @property
     def offsets(self):
-        return self._buffer[2 * self.tokens * self.top:]
+        return self._buffer.narrow(0, 2 * self.tokens * self.top, self.experts + 1)
 
 
 def expert_plan(ids, experts, *, stream=None) -> ExpertPlan:
