@@ -118,14 +118,44 @@ __device__ __forceinline__ void expand16(const uint32_t *w, uint32_t (&v)[8])
 
 // ---------------------------------------------------------------- epilogue
 
-// v / (1 + exp(-v)) as 2^(-v log2 e) on the special-function unit: the product's rounding leaves a relative error below
-// |v| 2^-24 in the exponential, far under the 2^-11 of a 16-bit output.
-__device__ __forceinline__ float silu(float v)
+// 2^v and 1 / v on the special-function unit.
+__device__ __forceinline__ float fast_exp2(float v)
 {
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.4426950408889634f * v));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-    return v * r;
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v));
+    return e;
+}
+__device__ __forceinline__ float fast_rcp(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// v / (1 + 2^exponent).  Rounding the exponent leaves a relative error of about |exponent| 2^-24 in the power, far under
+// the 2^-11 of a 16-bit output.
+__device__ __forceinline__ float gated_by_sigmoid(float v, float exponent) { return v * fast_rcp(1.f + fast_exp2(exponent)); }
+
+__device__ __forceinline__ float silu(float v) { return gated_by_sigmoid(v, -1.4426950408889634f * v); }
+
+// v Phi(v) = max(v, 0) - |v| erfc(|v| / sqrt 2) / 2, erfc by formula 7.1.26 of Abramowitz and Stegun (error below 1.5e-7):
+// no cancellation for negative v, and a third of the instructions of the erf that is accurate to the last bit.
+__device__ __forceinline__ float gelu(float v)
+{
+    const float a = fabsf(v), t = fast_rcp(fmaf(0.3275911f * 0.70710678118654752f, a, 1.f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f) * t;
+    const float e = fast_exp2(-0.72134752044448170f * v * v);  // exp(-v^2 / 2)
+    const float h = 0.5f * a * p * e;
+    return (v > 0.f ? v : v == v ? 0.f : v) - (e > 0.f ? h : 0.f);  // e is 0 for an infinite v
+}
+
+// 0.5 v (1 + tanh(u)) = v / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3)
+__device__ __forceinline__ float gelu_tanh(float v)
+{
+    return gated_by_sigmoid(v, -2.f * 1.4426950408889634f * 0.79788456080286536f * v * fmaf(0.044715f * v, v, 1.f));
 }
 
 __device__ __forceinline__ float activate(float v, int act)
@@ -133,8 +163,8 @@ __device__ __forceinline__ float activate(float v, int act)
     switch (act) {
         case QNN_ACT_RELU: return v > 0.f ? v : v == v ? 0.f : v;
         case QNN_ACT_SILU: return silu(v);
-        case QNN_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
-        case QNN_ACT_GELU_TANH: return 0.5f * v * (1.f + tanhf(0.79788456080286536f * (v + 0.044715f * v * v * v)));
+        case QNN_ACT_GELU: return gelu(v);
+        case QNN_ACT_GELU_TANH: return gelu_tanh(v);
         default: return v;
     }
 }

@@ -167,54 +167,75 @@ __device__ __forceinline__ void load_rows(const T *r, int64_t step, T (&v)[N], i
     }
 }
 
-// Sixteen rows of x (columns of the accumulator) from `row` on, `n` of them in use, of one image row.  Without a gate a
-// lane finishes its own channel.  With one, a channel's gate and up rows are eight lanes apart: of each two rows of x the
-// gate lane finishes the first and the up lane the second.
-// `others` sums of other pairs (one float a lane and column, `step` floats apart) are added first.
+// One lane's part of a tile's epilogue: sixteen rows of x (columns of the accumulator) at a time of one image row.  Without
+// a gate a lane finishes its own channel.  With one, a channel's gate and up rows are eight lanes apart: of each two rows
+// of x the gate lane finishes the first and the up lane the second.
+// The residual of a chunk is loaded before the sums are waited for, that of the next chunk before this one is stored.
 template <typename T, bool GATED>
-__device__ __forceinline__ void finish16(const MatmulArgs &a, uint32_t src, float2 p, int64_t row, int n, int64_t ch,
-                                         bool valid, const float *extra, int others, int step)
-{
-    constexpr int kN = GATED ? 8 : 16;
-    const bool up = GATED && (threadIdx.x & 8);
-    const int64_t rows = GATED ? 2 : 1;
-    if (up) ++row;
-    const int mine = !valid ? 0 : GATED ? (n + (up ? 0 : 1)) / 2 : n;  // rows that this lane finishes
+struct Epilogue {
+    static constexpr int kN = GATED ? 8 : 16, kRows = GATED ? 2 : 1;
+    const MatmulArgs &a;
+    float2 p;          // scale and bias
+    int64_t row, ch;   // first row of the tile (of this lane's rows), channel
+    int count;         // rows of the tile; none where the lane has no channel
+    bool up;
     T res[kN];
-    if (a.residual) load_rows(static_cast<const T *>(a.residual) + row * a.ldres + ch, rows * a.ldres, res, mine);
-    uint32_t acc[16];
-    __syncwarp();
-    tmem_ld16(src, acc);
-    tmem_wait_ld();
-    for (int o = 0; o < others; ++o)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) + extra[o * step + i * 128]);
-    float v[kN];
-    if constexpr (GATED) {
-        float u[kN];
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const float v0 = fmaf(__uint_as_float(acc[2 * i]), p.x, p.y), v1 = fmaf(__uint_as_float(acc[2 * i + 1]), p.x, p.y);
-            const float other = __shfl_xor_sync(0xffffffffu, up ? v0 : v1, 8);
-            v[i] = up ? other : v0;
-            u[i] = up ? v1 : other;
-        }
-        activate_all(v, a.act);
-#pragma unroll
-        for (int i = 0; i < kN; ++i) v[i] *= u[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < kN; ++i) v[i] = fmaf(__uint_as_float(acc[i]), p.x, p.y);
-        activate_all(v, a.act);
+
+    __device__ __forceinline__ Epilogue(const MatmulArgs &args, float2 params, int64_t first, int rows, int64_t channel)
+        : a(args), p(params), row(first), ch(channel), count(channel < args.m ? rows : 0), up(GATED && (threadIdx.x & 8))
+    {
+        if (up) ++row;
     }
-    if (a.residual)
+    // rows from column c on that this lane finishes
+    __device__ __forceinline__ int mine(int c) const { return GATED ? (count - c + (up ? 0 : 1)) >> 1 : count - c; }
+
+    __device__ __forceinline__ void fetch(int c)
+    {
+        if (a.residual)
+            load_rows(static_cast<const T *>(a.residual) + (row + c) * a.ldres + ch, kRows * a.ldres, res, count ? mine(c) : 0);
+    }
+
+    // Finishes columns c .. c + 15 and fetches the residual of the chunk at `next`.  `others` sums of other pairs (one float
+    // a lane and column, `step` floats apart) are added first.
+    __device__ __forceinline__ void chunk(uint32_t src, int c, int next, const float *extra, int others, int step)
+    {
+        uint32_t acc[16];
+        __syncwarp();
+        tmem_ld16(src + c, acc);
+        tmem_wait_ld();
+        for (int o = 0; o < others; ++o)
 #pragma unroll
-        for (int i = 0; i < kN; ++i) v[i] += to_f32<T>(res[i]);
-    if (a.out_f32)
-        store_rows(static_cast<float *>(a.y) + row * a.ldy + ch, rows * a.ldy, v, mine);
-    else
-        store_rows(static_cast<T *>(a.y) + row * a.ldy + ch, rows * a.ldy, v, mine);
-}
+            for (int i = 0; i < 16; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) + extra[o * step + (c + i) * 128]);
+        float v[kN];
+        if constexpr (GATED) {
+            float u[kN];
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                const float v0 = fmaf(__uint_as_float(acc[2 * i]), p.x, p.y), v1 = fmaf(__uint_as_float(acc[2 * i + 1]), p.x, p.y);
+                const float other = __shfl_xor_sync(0xffffffffu, up ? v0 : v1, 8);
+                v[i] = up ? other : v0;
+                u[i] = up ? v1 : other;
+            }
+            activate_all(v, a.act);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) v[i] *= u[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) v[i] = fmaf(__uint_as_float(acc[i]), p.x, p.y);
+            activate_all(v, a.act);
+        }
+        if (a.residual) {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) v[i] += to_f32<T>(res[i]);
+            if (next < count) fetch(next);
+        }
+        const int n = count ? mine(c) : 0;
+        if (a.out_f32)
+            store_rows(static_cast<float *>(a.y) + (row + c) * a.ldy + ch, kRows * a.ldy, v, n);
+        else
+            store_rows(static_cast<T *>(a.y) + (row + c) * a.ldy + ch, kRows * a.ldy, v, n);
+    }
+};
 
 // ---------------------------------------------------------------- tiles
 
@@ -392,8 +413,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             const Tile t = tile_at(a, s, tab, us, id);
             const int row = t.mtile * 256 + rank * 128 + quarter * 32 + lane;  // image row
             const int ch = a.gated ? (row >> 4) * 8 + (row & 7) : row;
-            const bool valid = ch < a.m;
             const float2 p = row < a.mb * 32 ? a.params[static_cast<int64_t>(t.expert) * a.mb * 32 + row] : make_float2(0.f, 0.f);
+            Epilogue<T, false> plain(a, p, t.first, t.count, ch);
+            Epilogue<T, true> gated(a, p, t.first, t.count, ch);
+            if (s.ranks == 1) {
+                if (a.gated) gated.fetch(16 * half);
+                else plain.fetch(16 * half);
+            }
             if (!mbar_wait_warp(acc_full + buf, (it >> 1) & 1, status)) {
                 ok = false;
                 break;
@@ -402,10 +428,8 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             if (s.ranks > 1) break;  // one tile a cluster: the sums of its pairs meet below
             const uint32_t src = tmem + buf * s.nt + (static_cast<uint32_t>(quarter * 32) << 16);
             for (int c = 16 * half; c < t.count; c += 32) {
-                if (a.gated)
-                    finish16<T, true>(a, src + c, p, t.first + c, t.count - c, ch, valid, nullptr, 0, 0);
-                else
-                    finish16<T, false>(a, src + c, p, t.first + c, t.count - c, ch, valid, nullptr, 0, 0);
+                if (a.gated) gated.chunk(src, c, c + 32, nullptr, 0, 0);
+                else plain.chunk(src, c, c + 32, nullptr, 0, 0);
             }
             __syncwarp();
             tc_fence_before();
@@ -476,12 +500,15 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             const int row = t.mtile * 256 + rank * 128 + quarter * 32 + lane;
             const int ch = a.gated ? (row >> 4) * 8 + (row & 7) : row;
             const float2 p = row < a.mb * 32 ? a.params[row] : make_float2(0.f, 0.f);
-            for (int c = 16 * half; c < t.count; c += 32) {
-                const float *extra = sums + c * 128 + quarter * 32 + lane;
-                if (a.gated)
-                    finish16<T, true>(a, src + c, p, t.first + c, t.count - c, ch, ch < a.m, extra, s.ranks - 1, s.nt * 128);
-                else
-                    finish16<T, false>(a, src + c, p, t.first + c, t.count - c, ch, ch < a.m, extra, s.ranks - 1, s.nt * 128);
+            const float *extra = sums + quarter * 32 + lane;
+            if (a.gated) {
+                Epilogue<T, true> e(a, p, t.first, t.count, ch);
+                e.fetch(16 * half);
+                for (int c = 16 * half; c < t.count; c += 32) e.chunk(src, c, c + 32, extra, s.ranks - 1, s.nt * 128);
+            } else {
+                Epilogue<T, false> e(a, p, t.first, t.count, ch);
+                e.fetch(16 * half);
+                for (int c = 16 * half; c < t.count; c += 32) e.chunk(src, c, c + 32, extra, s.ranks - 1, s.nt * 128);
             }
         }
         __syncwarp();
