@@ -9,7 +9,7 @@
 // Where the tiles fill half of the pairs at most, a cluster of several pairs takes one tile and splits its K; the other
 // pairs write their sums into the first pair's shared memory, which adds them in order.
 //
-// Warps: 0 loads (x by tiled TMA, weight blocks by bulk copies), 1 issues the MMAs (first CTA of the pair), 2 hands
+// Warps: 0 loads x and the weight blocks by tiled TMA, 1 issues the MMAs (first CTA of the pair), 2 hands
 // complete stages of 16-bit weights on, 3 owns the tensor memory, 4-11 run the epilogue, 12-19 expand packed codes into
 // the A operand, two groups on alternate stages.  Rows that an expert picks from x lie one after another before the
 // launch: picking them inside it held the MMAs up (692 us with four-row TMA gathers, which take some 80 cycles each, 371
@@ -71,6 +71,14 @@ __device__ __forceinline__ void st_cluster(uint32_t at, int rank, float v)
                  : "memory");
 }
 
+// mbar_wait_warp with one look before the clock is read: the roles below wait once a stage, mostly for a phase that is
+// complete or nearly so.
+__device__ __forceinline__ bool wait_stage(uint64_t *bar, uint32_t parity, int *status)
+{
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return mbar_wait_warp(bar, parity, status);
+}
+
 __device__ __forceinline__ void mma2_f16_warp(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
@@ -100,6 +108,17 @@ __device__ __forceinline__ void tma_tile(void *dst, const CUtensorMap *map, int 
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
             smem_addr(dst)),
         "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar))
+        : "memory");
+}
+
+// Four 32-row blocks of the image, the same 64 columns, with one instruction: issuing a copy takes a warp some hundred
+// cycles, and a copy for each block held a stage up to 600 cycles, whatever the MMAs took.
+__device__ __forceinline__ void tma_blocks(void *dst, const CUtensorMap *map, int kb, int mb, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %3, %4}], [%5];" ::"r"(
+            smem_addr(dst)),
+        "l"(map), "r"(0), "r"(kb), "r"(mb), "r"(smem_addr(bar))
         : "memory");
 }
 
@@ -272,7 +291,8 @@ constexpr int kTcThreads = BITS == 16 ? 384 : 640;
 
 template <typename T, int BITS>
 __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
-    matmul_tc_kernel(const __grid_constant__ CUtensorMap xmap, const MatmulArgs a, const TcShape s, int *status)
+    matmul_tc_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap, const MatmulArgs a,
+                     const TcShape s, int *status)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     constexpr bool kPacked = BITS != 16;
@@ -336,19 +356,17 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         int uses = 0;
         for (int id = pair; id < tiles && ok; id += pairs) {
             const Tile t = tile_at(a, s, tab, us, id);
-            const int mb = min((t.mtile * 2 + rank) * 4 + (lane & 3), a.mb - 1);  // rows past the image are not stored
-            const uint8_t *src = a.image + (static_cast<size_t>(t.expert) * a.mb + mb) * a.kb * kBlock;
+            const int mb = t.expert * a.mb + (t.mtile * 2 + rank) * 4;  // rows past the expert's are not stored
             for (int kb = kb0; kb < kb1; ++kb) {
-                if (!mbar_wait_warp(empty + st, phase ^ 1, status)) {
+                if (!wait_stage(empty + st, phase ^ 1, status)) {
                     ok = false;
                     break;
                 }
                 if (lane == 0) mbar_arrive_expect_tx(full + st, x_bytes + 4 * kBlock);
                 __syncwarp();
-                uint8_t *dst = kPacked ? sm_raw + st * 4 * kBlock : sm_a + st * kABytes;
-                if (lane < 4)
-                    bulk_g2s(dst + lane * kBlock, src + static_cast<size_t>(kb) * kBlock, kBlock, full + st);
-                else if (lane == 4)
+                if (lane == 0)
+                    tma_blocks(kPacked ? sm_raw + st * 4 * kBlock : sm_a + st * kABytes, &wmap, kb, mb, full + st);
+                else if (lane == 1)
                     tma_tile(sm_x + st * x_bytes, &xmap, kb * 64, static_cast<int>(t.first) + rank * (s.nt / 2), full + st);
                 __syncwarp();
                 ++uses;
@@ -361,7 +379,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                 st = s.stages - 1;
                 phase ^= 1;
             }
-            mbar_wait_warp(full + st, phase, status);
+            wait_stage(full + st, phase, status);
         }
     } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------ MMAs
@@ -371,14 +389,14 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         int it = 0;
         for (int id = pair; id < tiles && ok; id += pairs, ++it) {
             const int buf = it & 1;
-            if (!mbar_wait_warp(acc_empty + buf, ((it >> 1) & 1) ^ 1, status)) {
+            if (!wait_stage(acc_empty + buf, ((it >> 1) & 1) ^ 1, status)) {
                 ok = false;
                 break;
             }
             tc_fence_after();
             const uint32_t d = tmem + buf * s.nt;
             for (int kb = kb0; kb < kb1; ++kb) {
-                if (!mbar_wait_warp(ready + st, phase, status)) {
+                if (!wait_stage(ready + st, phase, status)) {
                     ok = false;
                     break;
                 }
@@ -396,7 +414,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
         // ------------------------------------------------ complete stages of 16-bit weights
         for (int id = pair; id < tiles && ok; id += pairs)
             for (int kb = kb0; kb < kb1; ++kb) {
-                if (!mbar_wait_warp(full + st, phase, status)) {
+                if (!wait_stage(full + st, phase, status)) {
                     ok = false;
                     break;
                 }
@@ -420,7 +438,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                 if (a.gated) gated.fetch(16 * half);
                 else plain.fetch(16 * half);
             }
-            if (!mbar_wait_warp(acc_full + buf, (it >> 1) & 1, status)) {
+            if (!wait_stage(acc_full + buf, (it >> 1) & 1, status)) {
                 ok = false;
                 break;
             }
@@ -448,7 +466,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                         advance();
                         continue;
                     }
-                    if (!mbar_wait_warp(full + st, phase, status)) {
+                    if (!wait_stage(full + st, phase, status)) {
                         ok = false;
                         break;
                     }
@@ -569,31 +587,31 @@ TcShape shape_of(const MatmulArgs &a, int bits, int nt, int ranks)
 }
 
 template <typename T, int BITS>
-cudaError_t launch_tc(const CUtensorMap &map, const MatmulArgs &a, const TcShape &s, int64_t tiles, int *status, cudaStream_t st)
+cudaError_t launch_tc(const CUtensorMap &map, const CUtensorMap &wmap, const MatmulArgs &a, const TcShape &s, int64_t tiles, int *status, cudaStream_t st)
 {
     const cudaError_t e = raise_smem<matmul_tc_kernel<T, BITS>>(227 * 1024);
     if (e != cudaSuccess) return e;
     const int64_t pairs = device_sm_count() / 2;
     const unsigned grid = static_cast<unsigned>(s.ranks > 1 ? 2 * s.ranks * tiles : 2 * (tiles < pairs ? tiles : pairs));
-    return launch_pdl(matmul_tc_kernel<T, BITS>, dim3(grid), kTcThreads<BITS>, s.smem, st, 2 * s.ranks, map, a, s, status);
+    return launch_pdl(matmul_tc_kernel<T, BITS>, dim3(grid), kTcThreads<BITS>, s.smem, st, 2 * s.ranks, map, wmap, a, s, status);
 }
 
 template <typename T>
-cudaError_t launch_bits(const CUtensorMap &map, const MatmulArgs &a, const TcShape &s, int bits, int64_t tiles, int *status,
+cudaError_t launch_bits(const CUtensorMap &map, const CUtensorMap &wmap, const MatmulArgs &a, const TcShape &s, int bits, int64_t tiles, int *status,
                         cudaStream_t st)
 {
-    if (bits == 16) return launch_tc<T, 16>(map, a, s, tiles, status, st);
-    if (bits == 8) return launch_tc<T, 8>(map, a, s, tiles, status, st);
-    if (bits == 4) return launch_tc<T, 4>(map, a, s, tiles, status, st);
-    return launch_tc<T, 2>(map, a, s, tiles, status, st);
+    if (bits == 16) return launch_tc<T, 16>(map, wmap, a, s, tiles, status, st);
+    if (bits == 8) return launch_tc<T, 8>(map, wmap, a, s, tiles, status, st);
+    if (bits == 4) return launch_tc<T, 4>(map, wmap, a, s, tiles, status, st);
+    return launch_tc<T, 2>(map, wmap, a, s, tiles, status, st);
 }
 
 // Rows of x a tile, and pairs that split K.  A tile's MMAs take about 2 nt cycles for each 64 columns, but never less than
 // a stage takes to be copied, expanded and handed on (kFloor), and a tile has a fixed cost (kFixed); a split adds the
 // exchange of the sums.  The choice with the least sum over the rounds of tiles that the pairs make wins.
-void choose(const MatmulArgs &a, int bits, int *nt_out, int *ranks_out)
+void choose(const MatmulArgs &a, int *nt_out, int *ranks_out)
 {
-    const double kFloor = bits == 16 ? 260 : 340, kFixed = 3000;
+    const double kFloor = 480, kFixed = 3000;
     const int pairs = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1;
     const int mt = (a.mb + 7) / 8;
     double cost = 0;
@@ -630,7 +648,7 @@ cudaError_t launch_matmul_tc(const MatmulArgs &a, int dtype, int bits, cudaStrea
     const EncodeTiled encode = encode_tiled();
     if (!status || !encode) return cudaErrorNotSupported;
     int nt = 0, ranks = 1;
-    choose(a, bits, &nt, &ranks);
+    choose(a, &nt, &ranks);
     const TcShape s = shape_of(a, bits, nt, ranks);
     int64_t u = (a.rows + nt - 1) / nt;
     if (a.offsets) u += a.experts < a.rows ? a.experts : a.rows;
@@ -644,8 +662,18 @@ cudaError_t launch_matmul_tc(const MatmulArgs &a, int dtype, int bits, cudaStrea
                const_cast<void *>(a.x), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return cudaErrorInvalidValue;
-    return dtype == QNN_F16 ? launch_bits<__half>(map, a, s, bits, tiles, status, st)
-                            : launch_bits<__nv_bfloat16>(map, a, s, bits, tiles, status, st);
+    // the image as words: 128 of them, the rest of a block, the blocks along K, the 32-row groups of all experts
+    CUtensorMap wmap;
+    const cuuint64_t block = 32 * 64 * bits / 8;
+    const cuuint64_t wdims[4] = {128, block / 512, static_cast<cuuint64_t>(a.kb), static_cast<cuuint64_t>(a.experts) * a.mb};
+    const cuuint64_t wstrides[3] = {512, block, block * a.kb};
+    const cuuint32_t wbox[4] = {128, static_cast<cuuint32_t>(block / 512), 1, 4}, wunit[4] = {1, 1, 1, 1};
+    if (encode(&wmap, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, const_cast<uint8_t *>(a.image), wdims, wstrides, wbox, wunit,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
+    return dtype == QNN_F16 ? launch_bits<__half>(map, wmap, a, s, bits, tiles, status, st)
+                            : launch_bits<__nv_bfloat16>(map, wmap, a, s, bits, tiles, status, st);
 }
 
 }  // namespace qnn
