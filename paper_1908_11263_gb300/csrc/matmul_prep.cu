@@ -160,28 +160,46 @@ __global__ void combine_kernel(const CombineArgs a)
     }
 }
 
-// Row i of dst: row i of src, or row order[i] / top (no row where order[i] is negative).  VEC: rows are 16-byte aligned
-// and whole vectors.
+// Row i of dst: row i of src, or row order[i] / top (no row where order[i] is negative).  A warp a row, eight 16-byte
+// loads of a lane in flight; VEC: rows are 16-byte aligned and whole vectors.
+constexpr int kTakeWarps = 8;
+
 template <bool VEC>
-__global__ void take_rows_kernel(const uint16_t *src, int64_t lds, const int32_t *order, int top, uint16_t *dst, int64_t ldd,
-                                 int64_t rows, int cols)
+__global__ void __launch_bounds__(kTakeWarps * 32) take_rows_kernel(const uint16_t *src, int64_t lds, const int32_t *order, int top,
+                                                                    uint16_t *dst, int64_t ldd, int64_t rows, int cols)
 {
     pdl_begin();
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * blockDim.y + threadIdx.y; row < rows;
-         row += static_cast<int64_t>(gridDim.x) * blockDim.y) {
-        int64_t from = row;
-        if (order) {
-            const int slot = order[row];
-            if (slot < 0) continue;
-            from = slot / top;
+    const int lane = threadIdx.x & 31;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kTakeWarps + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    int64_t from = row;
+    if (order) {
+        const int slot = order[row];
+        if (slot < 0) return;
+        from = slot / top;
+    }
+    const uint16_t *p = src + from * lds;
+    uint16_t *q = dst + row * ldd;
+    if constexpr (VEC) {
+        const int vecs = cols / 8;
+        for (int c = lane; c < vecs; c += 256) {
+            uint4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i * 32 < vecs) v[i] = reinterpret_cast<const uint4 *>(p)[c + i * 32];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i * 32 < vecs) reinterpret_cast<uint4 *>(q)[c + i * 32] = v[i];
         }
-        const uint16_t *p = src + from * lds;
-        uint16_t *q = dst + row * ldd;
-        if constexpr (VEC) {
-            for (int c = threadIdx.x * 8; c < cols; c += blockDim.x * 8)
-                *reinterpret_cast<uint4 *>(q + c) = *reinterpret_cast<const uint4 *>(p + c);
-        } else {
-            for (int c = threadIdx.x; c < cols; c += blockDim.x) q[c] = p[c];
+    } else {
+        for (int c = lane; c < cols; c += 256) {
+            uint16_t v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i * 32 < cols) v[i] = p[c + i * 32];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i * 32 < cols) q[c + i * 32] = v[i];
         }
     }
 }
@@ -193,10 +211,10 @@ cudaError_t launch_take_rows(const void *src, int64_t lds, const int32_t *order,
 {
     if (rows == 0) return cudaSuccess;
     const bool vec = reinterpret_cast<uintptr_t>(src) % 16 == 0 && lds % 8 == 0 && cols % 8 == 0;
-    const unsigned grid = static_cast<unsigned>(rows < 65535 ? rows : 65535);
-    return vec ? launch_pdl(take_rows_kernel<true>, dim3(grid), 128, 0, st, 1, static_cast<const uint16_t *>(src), lds, order, top,
+    const unsigned grid = static_cast<unsigned>((rows + kTakeWarps - 1) / kTakeWarps);
+    return vec ? launch_pdl(take_rows_kernel<true>, dim3(grid), kTakeWarps * 32, 0, st, 1, static_cast<const uint16_t *>(src), lds, order, top,
                             static_cast<uint16_t *>(dst), ldd, rows, cols)
-               : launch_pdl(take_rows_kernel<false>, dim3(grid), 128, 0, st, 1, static_cast<const uint16_t *>(src), lds, order, top,
+               : launch_pdl(take_rows_kernel<false>, dim3(grid), kTakeWarps * 32, 0, st, 1, static_cast<const uint16_t *>(src), lds, order, top,
                             static_cast<uint16_t *>(dst), ldd, rows, cols);
 }
 
