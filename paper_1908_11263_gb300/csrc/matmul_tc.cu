@@ -609,7 +609,7 @@ cudaError_t launch_bits(const CUtensorMap &map, const CUtensorMap &wmap, const M
 // Rows of x a tile, and pairs that split K.  A tile's MMAs take about 2 nt cycles for each 64 columns, but never less than
 // a stage takes to be copied, expanded and handed on (kFloor), and a tile has a fixed cost (kFixed); a split adds the
 // exchange of the sums.  The choice with the least sum over the rounds of tiles that the pairs make wins.
-void choose(const MatmulArgs &a, int *nt_out, int *ranks_out)
+void choose(const MatmulArgs &a, int bits, int *nt_out, int *ranks_out)
 {
     const double kFloor = 480, kFixed = 3000;
     const int pairs = device_sm_count() / 2 > 0 ? device_sm_count() / 2 : 1;
@@ -626,7 +626,9 @@ void choose(const MatmulArgs &a, int *nt_out, int *ranks_out)
                 if (tiles < live) tiles = live;
             }
             // clusters of eight CTAs leave some SMs of a GPC unused
-            if (ranks > 1 && (tiles * mt * ranks > (ranks == 4 ? 0.8 : 0.95) * pairs || (ranks - 1) * nt * 512 > 160 * 1024)) continue;
+            if (ranks > 1 && tiles * mt * ranks > (ranks == 4 ? 0.8 : 0.95) * pairs) continue;
+            // the other pairs' sums have to fit the stages
+            if (ranks > 1 && (ranks - 1) * nt * 512u > shape_of(a, bits, nt, ranks).off_bar) continue;
             const double waves = ranks > 1 ? 1 : std::ceil(tiles * mt / pairs);
             const double per_kb = 2.0 * nt > kFloor ? 2.0 * nt : kFloor;
             const double c = waves * ((a.kb + ranks - 1) / ranks * per_kb + kFixed) + (ranks > 1 ? 3000 + 20.0 * nt * (ranks - 1) : 0);
@@ -648,7 +650,7 @@ cudaError_t launch_matmul_tc(const MatmulArgs &a, int dtype, int bits, cudaStrea
     const EncodeTiled encode = encode_tiled();
     if (!status || !encode) return cudaErrorNotSupported;
     int nt = 0, ranks = 1;
-    choose(a, &nt, &ranks);
+    choose(a, bits, &nt, &ranks);
     const TcShape s = shape_of(a, bits, nt, ranks);
     int64_t u = (a.rows + nt - 1) / nt;
     if (a.offsets) u += a.experts < a.rows ? a.experts : a.rows;
