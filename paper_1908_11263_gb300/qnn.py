@@ -660,8 +660,9 @@ def route_topk(logits, k, *, score="softmax", bias=None, groups=1, top_groups=No
     p, ld = _rows(logits, logits.dtype, "logits")
     dev, (t, e) = logits.device, logits.shape
     pbias = _param(bias, torch.float32, "bias", (e,), dev)
-    weights = torch.empty((t, max(k, 0)), dtype=torch.float32, device=dev)
-    ids = torch.empty((t, max(k, 0)), dtype=torch.int32, device=dev)
+    shape = (t, k if k > 0 else 0)
+    weights = torch.empty(shape, dtype=torch.float32, device=dev)
+    ids = torch.empty(shape, dtype=torch.int32, device=dev)
     desc = RouteDesc(ctypes.sizeof(RouteDesc), code, e, k, _SCORES[score], groups, groups if top_groups is None else top_groups,
                      _GROUP_SCORES[group_score], int(bool(renormalise)), scale, t, ld)
     st = load().qnn_route_topk(ctypes.byref(desc), p, pbias, weights.data_ptr(), ids.data_ptr(),
@@ -687,7 +688,7 @@ class ExpertPlan:
 
     @property
     def order(self):
-        return self._buffer.narrow(0, 0, self.tokens * self.top)
+        return self._buffer.as_strided((self.tokens * self.top,), (1,), 0)
 
     @property
     def position(self):
@@ -695,7 +696,7 @@ class ExpertPlan:
 
     @property
     def offsets(self):
-        return self._buffer.narrow(0, 2 * self.tokens * self.top, self.experts + 1)
+        return self._buffer.as_strided((self.experts + 1,), (1,), 2 * self.tokens * self.top)
 
 
 def expert_plan(ids, experts, *, stream=None) -> ExpertPlan:
