@@ -480,8 +480,8 @@ enum {
 typedef struct {
     uint32_t struct_size;      /* = sizeof(qnn_matmul_desc) */
     int32_t experts;           /* matrices: 1 for qnn_matmul_run(), 1 .. 1024 for the experts' products */
-    int32_t m;                 /* output channels */
-    int32_t k;                 /* input channels, a multiple of 8/bits for packed weights */
+    int32_t m;                 /* output channels, at most 2^24 */
+    int32_t k;                 /* input channels, at most 2^24; a multiple of 8/bits for packed weights */
     int32_t bits;              /* 16, 8, 4 or 2 */
     int32_t dtype;             /* QNN_F16 or QNN_BF16: x, residual, outputs and 16-bit weights */
     int32_t gated;             /* 1: y = act(gate) * up */
@@ -506,7 +506,7 @@ qnn_status qnn_matmul_prepare(const qnn_matmul_desc *d, const void *w, const flo
  *   y = residual + act(v)             or  residual + act(v_gate) * v_up
  *
  * rounded once.  x [t][k], residual [t][m] or NULL, y [t][m] of type dtype, or
- * float when out_f32 is set.  y may be the residual itself (same pointer,
+ * float when out_f32 is set; t is at most 2^20.  y may be the residual itself (same pointer,
  * stride and type), no other overlap.  Workspace (256-byte aligned) as
  * qnn_matmul_workspace_size() says for the same d, t, x and ldx.
  */
@@ -516,7 +516,8 @@ qnn_status qnn_matmul_run(const qnn_matmul_desc *d, const void *image, size_t im
                           void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * The experts' products over a plan of qnn_expert_plan() (tokens * top slots).
+ * The experts' products over a plan of qnn_expert_plan() (tokens * top slots,
+ * at most 2^20 of them, top at most 1024).
  *
  * qnn_experts_dispatch: row p of y is the product of x[order[p] / top] with
  *   the weights of the expert that place p belongs to; x [tokens][k],

@@ -13,8 +13,9 @@
 namespace qnn {
 
 // Launches a kernel that may start while its predecessor in the stream still runs.  Every such kernel calls pdl_begin()
-// in all of its threads before it touches global memory: it lets its own successor start, then waits until the
-// predecessor has ended and its writes are visible.  Only the launch latency and the kernel's set-up overlap.
+// in all of its threads before it touches global memory: it waits until the predecessor has ended and its writes are
+// visible, and only then lets its own successor start, so that whatever a successor reads early was written by kernels
+// that have ended.  Only the launch latency and the kernel's set-up overlap.
 template <typename... P, typename... A>
 inline cudaError_t launch_pdl(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A... args)
 {
@@ -52,8 +53,8 @@ inline cudaError_t raise_smem(size_t bytes)
 
 __device__ __forceinline__ void pdl_begin()
 {
-    pdl_trigger();
     pdl_wait();
+    pdl_trigger();
 }
 
 template <typename T>

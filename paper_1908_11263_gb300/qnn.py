@@ -554,15 +554,17 @@ def _param(t, dtype, name, shape, device):
 
 
 def _run_with_workspace(call, size, device, stream):
-    """call(pointer, bytes) with the workspace that this device and stream have; where the library says that it is too
-    small (nothing is queued then), with one of size() bytes."""
+    """call(pointer, bytes, stream handle), without a workspace first (most calls need none; the library queues nothing
+    where it says that one is missing), then with the one of this device and stream.  A stream that is being captured
+    gets a buffer of its own: the graph would go on using the shared one after it was outgrown and freed."""
     handle = _stream_of(stream, device)
-    ws = _workspaces.get((device.index, handle))
-    st = call(None, 0, handle) if ws is None else call(ws.data_ptr(), ws.numel(), handle)
+    st = call(None, 0, handle)
     if st == QNN_EWORKSPACE:
         need = size()
-        ws = _workspace(need, device, stream)
-        st = call(_ptr(ws), need, handle)
+        with torch.cuda.stream(stream):
+            capturing = torch.cuda.is_current_stream_capturing()
+            ws = torch.empty(need, dtype=torch.uint8, device=device) if capturing else _workspace(need, device, stream)
+        st = call(ws.data_ptr(), need, handle)
     return st
 
 

@@ -235,6 +235,31 @@ def test_combine(t, top, experts, k, m, bits, residual):
     assert torch.equal(layer.combine(h, plan, cw, residual=res), y)
 
 
+def test_a_graph_keeps_its_own_workspace():
+    """A captured combine replays correctly after later calls have outgrown the stream's shared workspace."""
+    g = gen(11)
+    w, scale, _ = weights(96, 128, 4, BF, g, 8)
+    layer = qnn.PreparedExperts(w, scale=scale, bits=4, dtype=BF)
+    ids, cw = routed(40, 2, 8, g)
+    plan = qnn.expert_plan(ids, 8)
+    h = torch.randn(80, 128, generator=g, device="cuda").to(BF)
+    out = torch.empty(40, 96, dtype=BF, device="cuda")
+    want = layer.combine(h, plan, cw)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.combine(h, plan, cw, out=out)
+    big_ids, big_w = routed(4000, 2, 8, g)
+    big = qnn.expert_plan(big_ids, 8)
+    layer.combine(torch.randn(8000, 128, generator=g, device="cuda").to(BF), big, big_w)
+    torch.cuda.empty_cache()
+    junk = [torch.full((1 << 18,), 7, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and all(bool((j == 7).all()) for j in junk)
+
+
 # ---------------------------------------------------------------- refusals
 
 def test_refusals():
