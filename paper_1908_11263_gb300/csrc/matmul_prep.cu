@@ -122,15 +122,19 @@ __global__ void combine_kernel(const CombineArgs a)
         for (int j0 = 0; j0 < a.top; j0 += 4) {  // four rows in flight
             float4 v[4];
             float w[4];
+            int p[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int p = j0 + i < a.top ? a.position[t * a.top + j0 + i] : -1;
-                w[i] = 0.f;
+                p[i] = j0 + i < a.top ? a.position[t * a.top + j0 + i] : -1;
+                w[i] = j0 + i < a.top ? a.weights[t * a.top + j0 + i] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
                 v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (p >= 0) {
-                    w[i] = a.weights[t * a.top + j0 + i];
-                    v[i] = __ldcs(reinterpret_cast<const float4 *>(a.z + p * a.ldz + c));
-                }
+                if (p[i] >= 0)
+                    v[i] = __ldcs(reinterpret_cast<const float4 *>(a.z + p[i] * a.ldz + c));
+                else
+                    w[i] = 0.f;  // whatever weight a left-out choice has
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {

@@ -462,13 +462,15 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             int turn = 0;
             for (int id = pair; id < tiles && ok; id += pairs)
                 for (int kb = kb0; kb < kb1; ++kb, turn ^= 1) {
-                    if (turn != group) {
-                        advance();
-                        continue;
-                    }
+                    // Every stage is waited for, the other group's too: a barrier's parity tells two uses of a stage apart
+                    // only for who has seen the use before (copies may land out of order).
                     if (!wait_stage(full + st, phase, status)) {
                         ok = false;
                         break;
+                    }
+                    if (turn != group) {
+                        advance();
+                        continue;
                     }
                     const uint8_t *raw = sm_raw + st * 4 * kBlock + block * kBlock;
                     uint32_t w[2 * BITS];  // four runs of 16 codes: rows g, g + 8, g + 16, g + 24

@@ -209,17 +209,20 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
     uint32_t best = key[0];
 #pragma unroll
     for (int i = 1; i < NV; ++i) best = max(best, key[i]);
-    uint32_t least = best, floor_key = 1u;  // the k-th largest maximum; 1 (any open expert) where there are fewer
-    for (int j = 0; j < a.k; ++j) {
-        const uint32_t top_key = __reduce_max_sync(kFull, least);
-        if (top_key == 0u) {
-            floor_key = 1u;
-            break;
+    uint32_t floor_key = 1u;  // the k-th largest maximum; 1 (any open expert) where there are fewer, or few experts in all
+    if (a.groups == 1 || a.top_groups * a.group_size > 64) {
+        uint32_t least = best;
+        for (int j = 0; j < a.k; ++j) {
+            const uint32_t top_key = __reduce_max_sync(kFull, least);
+            if (top_key == 0u) {
+                floor_key = 1u;
+                break;
+            }
+            floor_key = top_key;
+            // one lane a step: equal maxima count one by one
+            const uint32_t who = __ballot_sync(kFull, least == top_key);
+            if (lane == __ffs(who) - 1) least = 0u;
         }
-        floor_key = top_key;
-        // one lane a step: equal maxima count one by one
-        const uint32_t who = __ballot_sync(kFull, least == top_key);
-        if (lane == __ffs(who) - 1) least = 0u;
     }
     int count = 0;
 #pragma unroll
@@ -339,7 +342,13 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
     const int64_t span = chunk / kPlanWarps;  // a multiple of 32
     const int64_t wb = begin + warp * span, we = wb + span < end ? wb + span : end;
     int32_t *mine = sm_plan + warp * experts;
-    for (int64_t s = wb + lane; s < we; s += 32) {
+    int held[4];  // the warp's first 128 slots stay in registers for the second pass
+#pragma unroll
+    for (int i = 0; i < 4; ++i) held[i] = expert_of(ids, wb + i * 32 + lane, we, experts);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (held[i] >= 0) atomicAdd(&mine[held[i]], 1);
+    for (int64_t s = wb + 128 + lane; s < we; s += 32) {
         const int e = expert_of(ids, s, we, experts);
         if (e >= 0) atomicAdd(&mine[e], 1);
     }
@@ -347,10 +356,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
     if (counts) {
         // a warp an expert: its slots over all blocks (at most 128), and over the blocks before this one
         const int blocks = gridDim.x, rounds = (experts + kPlanWarps - 1) / kPlanWarps;
-#pragma unroll 4
+        // every block starts at another expert: all of them at the same rows at once would queue at one L2 slice
+        const int first = static_cast<int>(blockIdx.x) % rounds;
+#pragma unroll 8
         for (int n = 0; n < rounds; ++n) {
-            // every block starts at another expert: all of them at the same rows at once would queue at one L2 slice
-            const int e = (n + static_cast<int>(blockIdx.x)) % rounds * kPlanWarps + warp;
+            const int turn = first + n < rounds ? first + n : first + n - rounds;
+            const int e = turn * kPlanWarps + warp;
             if (e >= experts) continue;
             int all = 0, before = 0;
 #pragma unroll
@@ -406,9 +417,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) offsets[experts] = running;
     // ranks: 32 slots at a time in order, equal experts by lane
-    for (int64_t s0 = wb; s0 < we; s0 += 32) {
-        const int64_t s = s0 + lane;
-        const int e = expert_of(ids, s, we, experts);
+    auto rank32 = [&](int64_t s, int e) {
         const uint32_t same = __match_any_sync(kFull, e);
         const int below = __popc(same & ((1u << lane) - 1u));
         const int32_t base = e >= 0 ? mine[e] : 0;
@@ -420,7 +429,10 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const int32_t 
             position[s] = at;
             if (at >= 0) order[at] = static_cast<int32_t>(s);
         }
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rank32(wb + i * 32 + lane, held[i]);
+    for (int64_t s0 = wb + 128; s0 < we; s0 += 32) rank32(s0 + lane, expert_of(ids, s0 + lane, we, experts));
     // the places after the last planned slot
     const int64_t from = begin > running ? begin : running;
     for (int64_t s = from + threadIdx.x; s < end; s += kPlanThreads) order[s] = -1;
