@@ -11,7 +11,7 @@
 //
 // Warps: 0 loads x and the weight blocks by tiled TMA, 1 issues the MMAs (first CTA of the pair), 2 hands
 // complete stages of 16-bit weights on, 3 owns the tensor memory, 4-11 run the epilogue, 12-19 expand packed codes into
-// the A operand, two groups on alternate stages.  Rows that an expert picks from x lie one after another before the
+// the A operand, two groups on alternate stages (an even number of stages).  Rows that an expert picks from x lie one after another before the
 // launch: picking them inside it held the MMAs up (692 us with four-row TMA gathers, which take some 80 cycles each, 371
 // with cp.async by two warps, for a product that takes 171 on rows in order and a copy that takes 30).
 // Every wait is bounded (mbar_wait_warp); a wait that gives up ends its role, and the kernel, with the status word set.
@@ -462,15 +462,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
             int turn = 0;
             for (int id = pair; id < tiles && ok; id += pairs)
                 for (int kb = kb0; kb < kb1; ++kb, turn ^= 1) {
-                    // Every stage is waited for, the other group's too: a barrier's parity tells two uses of a stage apart
-                    // only for who has seen the use before (copies may land out of order).
-                    if (!wait_stage(full + st, phase, status)) {
-                        ok = false;
-                        break;
-                    }
                     if (turn != group) {
                         advance();
                         continue;
+                    }
+                    if (!wait_stage(full + st, phase, status)) {
+                        ok = false;
+                        break;
                     }
                     const uint8_t *raw = sm_raw + st * 4 * kBlock + block * kBlock;
                     uint32_t w[2 * BITS];  // four runs of 16 codes: rows g, g + 8, g + 16, g + 24
@@ -578,6 +576,11 @@ TcShape shape_of(const MatmulArgs &a, int bits, int nt, int ranks)
     const uint32_t tab = (4 * (a.experts + 1) + 15) / 16 * 16;
     const uint32_t room = 227 * 1024 - kBarBytes - tab;
     s.stages = static_cast<int>(room / stage < kMaxStages ? room / stage : kMaxStages);
+    // With packed weights two groups take the stages by turns, so their number is even: a stage is then always the same
+    // group's, which has seen every use of it.  (A barrier's parity tells two uses of a stage apart only for who has seen
+    // the one before; copies may land out of order, and with an odd number a group could take the previous use of a stage,
+    // still in flight, for the one that it waits for.)
+    if (bits != 16) s.stages &= ~1;
     s.off_x = s.stages * kABytes;
     s.off_raw = s.off_x + s.stages * x;
     s.off_bar = s.off_raw + s.stages * raw;
