@@ -11,7 +11,7 @@
 //
 // Warps: 0 loads x and the weight blocks by tiled TMA, 1 issues the MMAs (first CTA of the pair), 2 hands
 // complete stages of 16-bit weights on, 3 owns the tensor memory, 4-11 run the epilogue, 12-19 expand packed codes into
-// the A operand, two groups on alternate stages (an even number of stages).  Rows that an expert picks from x lie one after another before the
+// the A operand, two groups on alternate stages.  Rows that an expert picks from x lie one after another before the
 // launch: picking them inside it held the MMAs up (692 us with four-row TMA gathers, which take some 80 cycles each, 371
 // with cp.async by two warps, for a product that takes 171 on rows in order and a copy that takes 30).
 // Every wait is bounded (mbar_wait_warp); a wait that gives up ends its role, and the kernel, with the status word set.
@@ -466,7 +466,12 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
                         advance();
                         continue;
                     }
-                    if (!wait_stage(full + st, phase, status)) {
+                    // A barrier's parity tells two uses of a stage apart only for who knows that the one before is over, and
+                    // with an odd number of stages that one was the other group's: its copies may still be in flight when a
+                    // later stage's have landed.  So the stage is seen to be released first, as by the loader.  (The use
+                    // before that was this group's own, and the MMAs, which go in order, have passed it: a group cannot be
+                    // two uses behind.)
+                    if (!wait_stage(empty + st, phase ^ 1, status) || !wait_stage(full + st, phase, status)) {
                         ok = false;
                         break;
                     }
@@ -576,11 +581,6 @@ TcShape shape_of(const MatmulArgs &a, int bits, int nt, int ranks)
     const uint32_t tab = (4 * (a.experts + 1) + 15) / 16 * 16;
     const uint32_t room = 227 * 1024 - kBarBytes - tab;
     s.stages = static_cast<int>(room / stage < kMaxStages ? room / stage : kMaxStages);
-    // With packed weights two groups take the stages by turns, so their number is even: a stage is then always the same
-    // group's, which has seen every use of it.  (A barrier's parity tells two uses of a stage apart only for who has seen
-    // the one before; copies may land out of order, and with an odd number a group could take the previous use of a stage,
-    // still in flight, for the one that it waits for.)
-    if (bits != 16) s.stages &= ~1;
     s.off_x = s.stages * kABytes;
     s.off_raw = s.off_x + s.stages * x;
     s.off_bar = s.off_raw + s.stages * raw;
