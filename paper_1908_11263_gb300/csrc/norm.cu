@@ -317,8 +317,8 @@ __global__ void __launch_bounds__(1024) block_norm_stream_kernel(const NormArgs 
     int st = 0, n = 0;
     uint32_t phase = 0;
     for (int64_t row = blockIdx.x; row < t; row += gridDim.x, ++n) {
-        const int64_t gate_row = a.gate ? static_cast<uint32_t>(row) / static_cast<uint32_t>(a.rows_per_gate) : -1;
-        if (hold && gate_row != held_gate) {
+        const int64_t gate_row = a.gate ? static_cast<int64_t>(static_cast<uint32_t>(row) / static_cast<uint32_t>(a.rows_per_gate)) : 0;
+        if (hold && a.gate && gate_row != held_gate) {
             hold_gate.load(a.gate, gate_row * a.d, a.d);
             held_gate = gate_row;
         }

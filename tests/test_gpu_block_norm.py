@@ -101,6 +101,32 @@ def test_forms(pad, gates, post, wide):
          f32 if wide in ("params", "both") else torch.bfloat16, "layer" if gates == 1 else "rms", post, gates, pad, seed=5)
 
 
+@pytest.mark.parametrize("t,d", [(7304, 520), (4692, 1736), (1920, 4096), (930, 8192), (459, 16384)])
+@pytest.mark.parametrize("gates", [0, 1, 3])
+@pytest.mark.parametrize("kind,post,residual,weights", [("rms", False, True, True), ("rms", True, True, True),
+                                                        ("layer", True, True, True), ("rms", False, False, False),
+                                                        ("layer", False, True, False)])
+@pytest.mark.parametrize("dtype,rdtype,pdtype", [(torch.bfloat16, torch.float32, torch.bfloat16),
+                                                 (torch.float16, torch.float16, torch.float16),
+                                                 (torch.bfloat16, torch.bfloat16, torch.float32),
+                                                 (torch.float32, torch.float32, torch.float32)])
+def test_many_rows(t, d, gates, kind, post, residual, weights, dtype, rdtype, pdtype):
+    """Enough whole rows for the blocks that stay resident, in every combination of optional operands."""
+    t = t // 3 * 3 if gates == 3 else t
+    case(t, d, dtype, rdtype, pdtype, kind, post, gates, 0, seed=t + d, weights=weights, residual=residual)
+
+
+def test_many_rows_strided_in_place_and_residual_only():
+    base = torch.randn(4700, 1744, device="cuda").bfloat16()
+    x, res = base[:, :1736], torch.randn(4700, 1736, device="cuda")
+    r, h = qnn.block_norm(x, res, scale=0.5)
+    r1, none = qnn.block_norm(x, res, scale=0.5, pre_norm=False)
+    assert none is None and torch.equal(r1, r)
+    x2, res2 = base.clone()[:, :1736], res.clone()
+    qnn.block_norm(x2, res2, scale=0.5, residual_out=res2, out=x2)
+    assert torch.equal(res2, r) and torch.equal(x2, h)
+
+
 def test_no_weights_no_residual():
     case(6, 520, torch.float16, torch.float16, torch.float16, "rms", True, 0, 0, seed=1, weights=False, residual=False)
     case(6, 520, torch.bfloat16, torch.float32, torch.bfloat16, "layer", False, 0, 0, seed=2, weights=False, residual=False)
