@@ -29,6 +29,9 @@
  *    significant bits.  Activations are unsigned, weights two's-complement.
  *  - Thread safety: calls may be made from several host threads; the only
  *    shared host state is a per-device cache of queried device properties.
+ *    A workspace belongs to one call at a time, on one stream too: calls of
+ *    several threads interleave their launches, and a call may hold data in
+ *    its workspace from one launch to the next.
  */
 #ifndef QNN_H
 #define QNN_H

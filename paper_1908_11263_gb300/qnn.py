@@ -235,21 +235,14 @@ def mma_operand_bits(desc: ConvDesc) -> int:
     return r
 
 
-_workspaces: dict = {}
-
-
 def _workspace(nbytes: int, device, stream):
-    """Workspace per (device, stream): calls on one stream never overlap."""
+    """A workspace for one call.  Each call has its own: calls that several host threads make on one stream interleave
+    their launches, and hold data in the workspace between them.  It is allocated on the launching stream, so it may go
+    back to the allocator as soon as the call has returned; in a stream capture it comes from the graph's own memory."""
     if nbytes == 0:
         return None
-    key = (device.index, stream.cuda_stream if stream is not None else torch.cuda.current_stream(device).cuda_stream)
-    buf = _workspaces.get(key)
-    if buf is None or buf.numel() < nbytes:
-        # allocated on the stream that uses it, so that a buffer outgrown while calls are queued is not handed on early
-        with torch.cuda.stream(stream):
-            buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        _workspaces[key] = buf
-    return buf
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def conv_hwc(x, w, kappa, lam, *, bias=None, shifts=None, shift=0, bits=8, stride=1, pad=0, algo=ALGO_AUTO,
@@ -555,15 +548,12 @@ def _param(t, dtype, name, shape, device):
 
 def _run_with_workspace(call, size, device, stream):
     """call(pointer, bytes, stream handle), without a workspace first (most calls need none; the library queues nothing
-    where it says that one is missing), then with the one of this device and stream.  A stream that is being captured
-    gets a buffer of its own: the graph would go on using the shared one after it was outgrown and freed."""
+    where it says that one is missing), then with one of this call's own."""
     handle = _stream_of(stream, device)
     st = call(None, 0, handle)
     if st == QNN_EWORKSPACE:
         need = size()
-        with torch.cuda.stream(stream):
-            capturing = torch.cuda.is_current_stream_capturing()
-            ws = torch.empty(need, dtype=torch.uint8, device=device) if capturing else _workspace(need, device, stream)
+        ws = _workspace(need, device, stream)
         st = call(ws.data_ptr(), need, handle)
     return st
 
