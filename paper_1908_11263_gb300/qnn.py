@@ -8,6 +8,11 @@ Tensor conventions (packed Q-bit data lives in uint8 tensors whose last
 dimension counts bytes):
   activations  uint8 [n, h, w, c*Q/8]    weights  int8/uint8 [m, kh, kw, c*Q/8]
   outputs      uint8 [n, oh, ow, m*Q/8]
+
+`stream` (a torch.cuda.Stream) is where a call's kernels are queued; without it, the current stream.  What a call allocates
+belongs to that stream, and the stream that is current at the call may use it too, once it is ordered after the call; other
+streams need record_stream(), as for any tensor.  Inputs are the caller's to keep until the stream has passed the call; only
+the weights that PreparedMatmul and PreparedExperts lay out may be dropped at once.
 """
 from __future__ import annotations
 
@@ -188,6 +193,18 @@ def _stream_of(stream, device):
     return _raw_stream(device.index) if stream is None else stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory of the launching stream.  Where `stream` is not the current one, memory of the current stream would not do: it
+    may be a block that queued work there still uses, and it would go back there when dropped, while `stream` still writes
+    it.  The current stream, where the caller goes on, is noted as a second user."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def _dev(t: torch.Tensor, dtype, name):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
@@ -265,7 +282,7 @@ def conv_hwc(x, w, kappa, lam, *, bias=None, shifts=None, shift=0, bits=8, strid
     oh = (h + 2 * desc.pad_h - kh) // desc.stride_h + 1
     ow = (wd + 2 * desc.pad_w - kw) // desc.stride_w + 1
     if out is None:
-        out = torch.empty((n, oh, ow, m // per), dtype=torch.uint8, device=x.device)
+        out = _empty((n, oh, ow, m // per), torch.uint8, x.device, stream)
     else:
         _dev(out, torch.uint8, "out")
     nbytes = workspace_size(desc)
@@ -300,7 +317,7 @@ def conv_hwc_pool2(x, w, kappa, lam, *, bias=None, shifts=None, shift=0, bits=8,
     oh = h + 2 * desc.pad_h - kh + 1
     ow = wd + 2 * desc.pad_w - kw + 1
     if out is None:
-        out = torch.empty((n, oh // 2, ow // 2, m // per), dtype=torch.uint8, device=x.device)
+        out = _empty((n, oh // 2, ow // 2, m // per), torch.uint8, x.device, stream)
     else:
         _dev(out, torch.uint8, "out")
     nbytes = workspace_size(desc)
@@ -333,7 +350,7 @@ def conv_hwc_thresholds(x, w, thresholds, *, bits, stride=1, pad=0, algo=ALGO_AU
     oh = (h + 2 * desc.pad_h - kh) // desc.stride_h + 1
     ow = (wd + 2 * desc.pad_w - kw) // desc.stride_w + 1
     if out is None:
-        out = torch.empty((n, oh, ow, m // per), dtype=torch.uint8, device=x.device)
+        out = _empty((n, oh, ow, m // per), torch.uint8, x.device, stream)
     else:
         _dev(out, torch.uint8, "out")
     nbytes = workspace_size(desc)
@@ -361,7 +378,7 @@ def conv_binary(x, w, thresholds, *, stride=1, pad=0, out=None, stream=None):
     oh = (h + 2 * desc.pad_h - kh) // desc.stride_h + 1
     ow = (wd + 2 * desc.pad_w - kw) // desc.stride_w + 1
     if out is None:
-        out = torch.empty((n, oh, ow, m // 8), dtype=torch.uint8, device=x.device)
+        out = _empty((n, oh, ow, m // 8), torch.uint8, x.device, stream)
     else:
         _dev(out, torch.uint8, "out")
     _check(load().qconv_hwc_binary(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(thresholds), _ptr(out), _stream(stream)),
@@ -425,7 +442,7 @@ class PreparedConv:
         self.ow = (wd + 2 * self.desc.pad_w - kw) // self.desc.stride_w + 1
         self.out_shape = (n, self.oh, self.ow, m // per)
         self.nbytes = workspace_size(self.desc)
-        self.workspace = torch.empty(max(self.nbytes, 1), dtype=torch.uint8, device=w.device)
+        self.workspace = _empty(max(self.nbytes, 1), torch.uint8, w.device, stream)
         self._keep = (w, kappa, lam, bias, shifts)
         st = load().qconv_hwc_prepare(ctypes.byref(self.desc), _ptr(w), _ptr(bias), _ptr(kappa), _ptr(lam),
                                       _ptr(shifts), _ptr(self.workspace), ctypes.c_size_t(self.nbytes),
@@ -435,7 +452,7 @@ class PreparedConv:
     def __call__(self, x, out=None, stream=None):
         _dev(x, torch.uint8, "x")
         if out is None:
-            out = torch.empty(self.out_shape, dtype=torch.uint8, device=x.device)
+            out = _empty(self.out_shape, torch.uint8, x.device, stream)
         st = load().qconv_hwc_run(ctypes.byref(self.desc), _ptr(x), _ptr(out), _ptr(self.workspace),
                                   ctypes.c_size_t(self.nbytes), _stream(stream))
         _check(st, "qconv_hwc_run")
@@ -447,7 +464,7 @@ class PreparedConv:
         _dev(x, torch.uint8, "x")
         if out is None:
             n, _, _, mb = self.out_shape
-            out = torch.empty((n, self.oh // 2, self.ow // 2, mb), dtype=torch.uint8, device=x.device)
+            out = _empty((n, self.oh // 2, self.ow // 2, mb), torch.uint8, x.device, stream)
         st = load().qconv_hwc_pool2_run(ctypes.byref(self.desc), _ptr(x), _ptr(out), _ptr(self.workspace),
                                         ctypes.c_size_t(self.nbytes), _stream(stream))
         _check(st, "qconv_hwc_pool2_run")
@@ -465,7 +482,7 @@ def linear(x, w, bias=None, *, out=None, stream=None):
     if k != k2:
         raise ValueError("x and w disagree on k")
     if out is None:
-        out = torch.empty((n, m), dtype=torch.int32, device=x.device)
+        out = _empty((n, m), torch.int32, x.device, stream)
     st = load().qlinear(n, k, m, _ptr(x), _ptr(w), _ptr(bias), _ptr(out), _stream(stream))
     _check(st, "qlinear")
     return out
@@ -478,7 +495,7 @@ def maxpool(x, k=2, s=2, bits=8, *, out=None, stream=None):
     c = cb * 8 // bits
     oh, ow = (h - k) // s + 1, (wd - k) // s + 1
     if out is None:
-        out = torch.empty((n, oh, ow, cb), dtype=torch.uint8, device=x.device)
+        out = _empty((n, oh, ow, cb), torch.uint8, x.device, stream)
     st = load().qmaxpool(n, h, wd, c, k, s, bits, _ptr(x), _ptr(out), _stream(stream))
     _check(st, "qmaxpool")
     return out
@@ -489,7 +506,7 @@ def pack_subbyte(src, bits, *, out=None, stream=None):
     _dev(src, torch.int8, "src")
     shape = tuple(src.shape[:-1]) + (src.shape[-1] * bits // 8,)
     if out is None:
-        out = torch.empty(shape, dtype=torch.uint8, device=src.device)
+        out = _empty(shape, torch.uint8, src.device, stream)
     st = load().pack_subbyte(_ptr(src), _ptr(out), src.numel(), bits, _stream(stream))
     _check(st, "pack_subbyte")
     return out
@@ -500,7 +517,7 @@ def unpack_subbyte(src, bits, signed, *, out=None, stream=None):
     _dev(src, (torch.uint8, torch.int8), "src")
     shape = tuple(src.shape[:-1]) + (src.shape[-1] * 8 // bits,)
     if out is None:
-        out = torch.empty(shape, dtype=torch.int8, device=src.device)
+        out = _empty(shape, torch.int8, src.device, stream)
     st = load().unpack_subbyte(_ptr(src), _ptr(out), out.numel(), bits, int(bool(signed)), _stream(stream))
     _check(st, "unpack_subbyte")
     return out
@@ -617,7 +634,7 @@ def block_norm(x, residual=None, *, pre_weight=None, pre_bias=None, pre_norm=Tru
     ppw, ppb = _param(post_weight, pdtype, "post_weight", row, dev), _param(post_bias, pdtype, "post_bias", row, dev)
     pw, pb = _param(pre_weight, pdtype, "pre_weight", row, dev), _param(pre_bias, pdtype, "pre_bias", row, dev)
     if residual_out is None:
-        residual_out = torch.empty(shape, dtype=rdtype, device=dev)
+        residual_out = _empty(shape, rdtype, dev, stream)
         pr, ldr = residual_out.data_ptr(), d
     else:
         pr, ldr = _rows(residual_out, rdtype, "residual_out", shape, dev)
@@ -625,7 +642,7 @@ def block_norm(x, residual=None, *, pre_weight=None, pre_bias=None, pre_norm=Tru
     if not pre_norm:
         out = None
     elif out is None:
-        out = torch.empty(shape, dtype=dtype, device=dev)
+        out = _empty(shape, dtype, dev, stream)
         ph = out.data_ptr()
     else:
         ph, ldh = _rows(out, dtype, "out", shape, dev)
@@ -653,8 +670,8 @@ def route_topk(logits, k, *, score="softmax", bias=None, groups=1, top_groups=No
     dev, (t, e) = logits.device, logits.shape
     pbias = _param(bias, torch.float32, "bias", (e,), dev)
     shape = (t, k if k > 0 else 0)
-    weights = torch.empty(shape, dtype=torch.float32, device=dev)
-    ids = torch.empty(shape, dtype=torch.int32, device=dev)
+    weights = _empty(shape, torch.float32, dev, stream)
+    ids = _empty(shape, torch.int32, dev, stream)
     desc = RouteDesc(ctypes.sizeof(RouteDesc), code, e, k, _SCORES[score], groups, groups if top_groups is None else top_groups,
                      _GROUP_SCORES[group_score], int(bool(renormalise)), scale, t, ld)
     st = load().qnn_route_topk(ctypes.byref(desc), p, pbias, weights.data_ptr(), ids.data_ptr(),
@@ -670,10 +687,10 @@ class ExpertPlan:
 
     __slots__ = ("tokens", "top", "experts", "device", "_buffer", "_offsets", "_order", "_position")
 
-    def __init__(self, tokens, top, experts, device):
+    def __init__(self, tokens, top, experts, device, stream=None):
         self.tokens, self.top, self.experts, self.device = tokens, top, experts, device
         slots = tokens * top
-        self._buffer = torch.empty(2 * slots + experts + 1, dtype=torch.int32, device=device)
+        self._buffer = _empty(2 * slots + experts + 1, torch.int32, device, stream)
         self._order = self._buffer.data_ptr()  # pointers
         self._position = self._order + 4 * slots
         self._offsets = self._position + 4 * slots
@@ -699,7 +716,7 @@ def expert_plan(ids, experts, *, stream=None) -> ExpertPlan:
     if experts <= 0:
         raise QnnError(QNN_EINVAL, "qnn_expert_plan")
     lib, p, (tokens, top) = load(), ids.data_ptr(), ids.shape
-    plan = ExpertPlan(tokens, top, experts, ids.device)
+    plan = ExpertPlan(tokens, top, experts, ids.device, stream)
 
     def size():
         need = ctypes.c_size_t(0)
@@ -748,10 +765,14 @@ class _Prepared:
         lib, need = load(), ctypes.c_size_t(0)
         _check(lib.qnn_matmul_image_size(self._desc, ctypes.byref(need)), "qnn_matmul_image_size")
         self.nbytes = need.value
-        self.image = torch.empty(self.nbytes, dtype=torch.uint8, device=w.device)
+        self.image = _empty(self.nbytes, torch.uint8, w.device, stream)
         self._image = self.image.data_ptr()
         st = lib.qnn_matmul_prepare(self._desc, _ptr(w), pscale, pbias, self.image.data_ptr(), self.nbytes, _stream(stream))
         _check(st, "qnn_matmul_prepare")
+        if stream is not None:  # the caller may drop them now
+            for t in (w, scale, bias):
+                if t is not None:
+                    t.record_stream(stream)
 
 
 class PreparedMatmul(_Prepared):
@@ -776,7 +797,7 @@ class PreparedMatmul(_Prepared):
             odtype = dtype if out_dtype is None else out_dtype
             if odtype is not dtype and odtype is not torch.float32:
                 raise TypeError(f"out_dtype must be {dtype} or float32, got {odtype}")
-            out = torch.empty((t, m), dtype=odtype, device=dev)
+            out = _empty((t, m), odtype, dev, stream)
             po, ldo = out.data_ptr(), m
         else:
             odtype = out.dtype
@@ -826,7 +847,7 @@ class PreparedExperts(_Prepared):
         px, ldx = _rows(x, self.dtype, "x", (tokens, self.k), self.device)
         shape = (tokens * top, self.m)
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = _empty(shape, self.dtype, self.device, stream)
         po, ldo = _rows(out, self.dtype, "out", shape, self.device)
         lib = load()
         self._run(lambda ws, n, handle: lib.qnn_experts_dispatch(
@@ -846,7 +867,7 @@ class PreparedExperts(_Prepared):
         shape = (tokens, self.m)
         pres, ldres = (None, self.m) if residual is None else _rows(residual, self.dtype, "residual", shape, self.device)
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = _empty(shape, self.dtype, self.device, stream)
         po, ldo = _rows(out, self.dtype, "out", shape, self.device)
         lib = load()
         self._run(lambda ws, n, handle: lib.qnn_experts_combine(
