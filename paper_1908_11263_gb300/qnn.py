@@ -9,7 +9,7 @@ dimension counts bytes):
   activations  uint8 [n, h, w, c*Q/8]    weights  int8/uint8 [m, kh, kw, c*Q/8]
   outputs      uint8 [n, oh, ow, m*Q/8]
 
-`stream` (a torch.cuda.Stream) is where a call's kernels are queued; without it, the current stream.  What a call allocates
+Tensors and streams are the current device's; others are refused.  `stream` (a torch.cuda.Stream) is where a call's kernels are queued; without it, the current stream.  What a call allocates
 belongs to that stream, and the stream that is current at the call may use it too, once it is ordered after the call; other
 streams need record_stream(), as for any tensor.  Inputs are the caller's to keep until the stream has passed the call; only
 the weights that PreparedMatmul and PreparedExperts lay out may be dropped at once.
@@ -172,13 +172,30 @@ def _check(status: int, what: str):
         raise QnnError(status, what)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _on_current(device, name):
+    """The library launches on the current device and asks that one for its properties: nothing may be on another."""
+    current = _current_device()
+    if device.index != current:
+        raise ValueError(f"{name} is on {device}, but the current device is cuda:{current}")
+
+
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    """Pointer of a tensor that is not another device's, or NULL."""
+    if t is None:
+        return None
+    if t.is_cuda:
+        _on_current(t.device, "a tensor")
+    return ctypes.c_void_p(t.data_ptr())
 
 
 def _stream(stream):
     if stream is None:
         stream = torch.cuda.current_stream()
+    else:
+        _on_current(stream.device, "stream")
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -189,8 +206,11 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 
 
 def _stream_of(stream, device):
-    """Handle of `stream`, or of the device's current stream."""
-    return _raw_stream(device.index) if stream is None else stream.cuda_stream
+    """Handle of `stream`, or of the device's current stream; `device` is the current one."""
+    if stream is None:
+        return _raw_stream(device.index)
+    _on_current(stream.device, "stream")
+    return stream.cuda_stream
 
 
 def _empty(shape, dtype, device, stream):
@@ -199,6 +219,7 @@ def _empty(shape, dtype, device, stream):
     it.  The current stream, where the caller goes on, is noted as a second user."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
+    _on_current(stream.device, "stream")
     with torch.cuda.stream(stream):
         t = torch.empty(shape, dtype=dtype, device=device)
     t.record_stream(torch.cuda.current_stream())
@@ -526,8 +547,9 @@ def unpack_subbyte(src, bits, signed, *, out=None, stream=None):
 # ---------------------------------------------------------------- language-model block operators
 
 def _rows(t: torch.Tensor, dtype, name, shape=None, device=None):
-    """A CUDA matrix with contiguous columns and any row stride; returns (pointer, row stride)."""
-    if t.dtype is dtype and t.is_cuda and (device is None or t.device == device):
+    """A CUDA matrix with contiguous columns and any row stride, on `device` (None: on the current one); returns (pointer,
+    row stride)."""
+    if t.dtype is dtype and t.is_cuda and (t.device.index == _current_device() if device is None else t.device == device):
         s = t.shape
         if len(s) == 2 and (shape is None or s == shape):
             ld, step = t.stride()
@@ -539,6 +561,8 @@ def _rows(t: torch.Tensor, dtype, name, shape=None, device=None):
 def _rows_slow(t, dtype, name, shape, device):
     if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{name} must be a CUDA tensor" + ("" if device is None else f" on {device}"))
+    if device is None:
+        _on_current(t.device, name)
     if t.dtype != dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
@@ -711,6 +735,7 @@ class ExpertPlan:
 def expert_plan(ids, experts, *, stream=None) -> ExpertPlan:
     """The plan of ids int32 [tokens, top] over `experts`; ids outside [0, experts) go to no expert."""
     _dev(ids, torch.int32, "ids")
+    _on_current(ids.device, "ids")
     if ids.dim() != 2:
         raise ValueError(f"ids must have shape [tokens, top], got {tuple(ids.shape)}")
     if experts <= 0:
@@ -757,7 +782,7 @@ class _Prepared:
             raise ValueError("a gated product needs as many gate rows as up rows")
         self.dtype, self.device, self.experts = dtype, w.device, w.shape[0] if experts else 1
         self.m, self.k = rows // 2 if gated else rows, w.shape[-1] * per
-        pscale = _param(scale, torch.float32, "scale", w.shape[:-1], w.device)
+        pw, pscale = _ptr(w), _param(scale, torch.float32, "scale", w.shape[:-1], w.device)
         pbias = _param(bias, torch.float32, "bias", w.shape[:-1], w.device)
         self.desc = MatmulDesc(ctypes.sizeof(MatmulDesc), self.experts, self.m, self.k, bits, _DTYPES[dtype], int(bool(gated)),
                                _ACTS[act])
@@ -767,7 +792,7 @@ class _Prepared:
         self.nbytes = need.value
         self.image = _empty(self.nbytes, torch.uint8, w.device, stream)
         self._image = self.image.data_ptr()
-        st = lib.qnn_matmul_prepare(self._desc, _ptr(w), pscale, pbias, self.image.data_ptr(), self.nbytes, _stream(stream))
+        st = lib.qnn_matmul_prepare(self._desc, pw, pscale, pbias, self.image.data_ptr(), self.nbytes, _stream(stream))
         _check(st, "qnn_matmul_prepare")
         if stream is not None:  # the caller may drop them now
             for t in (w, scale, bias):
@@ -788,6 +813,7 @@ class PreparedMatmul(_Prepared):
     def __call__(self, x, residual=None, *, out=None, out_dtype=None, stream=None):
         """x [t, k] -> [t, m] in x's dtype, or float32 with out_dtype=torch.float32.  out may be the residual."""
         dtype, dev, m = self.dtype, self.device, self.m
+        _on_current(dev, "the layer")
         px, ldx = _rows(x, dtype, "x", None, dev)
         t, k = x.shape
         if k != self.k:
@@ -825,6 +851,7 @@ class PreparedExperts(_Prepared):
         super().__init__(w, scale, bias, bits, dtype, gated, act, True, stream)
 
     def _check_plan(self, plan):
+        _on_current(self.device, "the layer")
         if plan.experts != self.experts:
             raise ValueError(f"the plan is over {plan.experts} experts, the weights over {self.experts}")
         if plan.device != self.device:
