@@ -490,13 +490,11 @@ cudaError_t launch_expert_plan(const int32_t *ids, int64_t slots, int experts, i
     const int nb = plan_blocks(slots, &chunk);
     int32_t *counts = nb > 1 ? static_cast<int32_t *>(workspace) : nullptr;
     const size_t smem = sizeof(int32_t) * (kPlanWarps + 2) * experts;
-    if (smem > 48 * 1024) {
-        const cudaError_t e = raise_smem<plan_place_kernel>(sizeof(int32_t) * (kPlanWarps + 2) * 1024);
-        if (e != cudaSuccess) return e;
-    }
+    // The limit counts static memory too: always the most that any number of experts takes, before anything is queued.
+    cudaError_t e = raise_smem<plan_place_kernel>(sizeof(int32_t) * (kPlanWarps + 2) * 1024);
+    if (e != cudaSuccess) return e;
     if (counts) {
-        const cudaError_t e = launch_pdl(plan_count_kernel, dim3(nb), kPlanThreads, sizeof(int32_t) * experts, stream, 1, ids, slots,
-                                         chunk, experts, counts);
+        e = launch_pdl(plan_count_kernel, dim3(nb), kPlanThreads, sizeof(int32_t) * experts, stream, 1, ids, slots, chunk, experts, counts);
         if (e != cudaSuccess) return e;
     }
     return launch_pdl(plan_place_kernel, dim3(nb), kPlanThreads, smem, stream, 1, ids, slots, chunk, experts, counts, offsets,
