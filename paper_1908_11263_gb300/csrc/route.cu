@@ -55,6 +55,10 @@ __device__ __forceinline__ float score_of(float v, int sigmoid, float top)
     if (sigmoid) return v > -INFINITY ? sigmoid_of(v) : 0.f;
     return v > -INFINITY ? exp_from(v, top) : 0.f;
 }
+
+// Below this, sums of scores lose their leading bits to underflow (exp(-69)).
+constexpr float kLeastScore = 1e-30f;
+
 // NV (a multiple of four) neighbouring logits.
 template <typename T, int NV>
 __device__ __forceinline__ void load_run(const T *p, float (&x)[NV])
@@ -135,16 +139,24 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
 #pragma unroll
     for (int i = 0; i < NV; ++i) key[i] = x[i] > -INFINITY ? order_key(c[i]) : 0u;
     if (a.groups > 1) {
-        // sums need the scores themselves
-        if (!scored && a.two) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) c[i] = score_of(x[i], 0, top);
-        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) of[i] = key[i] == 0u ? -INFINITY : c[i];
-    }
-    if (a.groups > 1) {
-        uint32_t mine = 0u;  // key of this lane's group; the group's first lane speaks for it
+        // Keys of this lane's group: `mine` while there is one in it to choose, then `far`.  Both find the group's two best
+        // first; where the choice goes by logits, the sum is that of their softmax numerators.  A sum that would underflow (of
+        // a group that lies 69 or more below the row's largest logit) is compared by its logarithm, which keeps its order;
+        // these groups come after all of the others.
+        uint32_t mine = 0u, far = 0u;
+        auto rank_group = [&](float best, float second) {
+            if (!a.two) {
+                mine = order_key(best);
+            } else if (scored) {
+                mine = order_key(second > -INFINITY ? best + second : best);
+            } else if (best > -INFINITY) {
+                const float sum = exp_from(best, top) + score_of(second, 0, top);
+                if (sum >= kLeastScore) mine = order_key(sum);
+                else far = order_key(best + log1pf(expf(second - best)));
+            }
+        };
         int group;
         const int width = a.group_size / NV;  // lanes a group
         const bool lanes = a.group_size % NV == 0 && (width & (width - 1)) == 0;
@@ -160,9 +172,8 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
                 second = fmaxf(fmaxf(second, s), fminf(best, b));
                 best = fmaxf(best, b);
             }
-            if (a.two && second > -INFINITY) best += second;
             group = lane / width;
-            mine = group < a.groups ? order_key(best) : 0u;
+            if (group < a.groups) rank_group(best, second);
         } else {
             float *sc = sm_scores + (threadIdx.x >> 5) * a.e;
 #pragma unroll
@@ -179,14 +190,18 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
                     best = fmaxf(best, v);
                     j = j + 1 == a.group_size ? 0 : j + 1;
                 }
-                if (a.two && second > -INFINITY) best += second;
-                mine = order_key(best);
+                rank_group(best, second);
             }
         }
         uint32_t keep = 0u;
         for (int n = 0; n < a.top_groups; ++n) {
-            const uint32_t top_key = __reduce_max_sync(kFull, mine);
-            if (top_key == 0u) break;
+            uint32_t top_key = __reduce_max_sync(kFull, mine);
+            if (top_key == 0u) {  // (a second time round both are 0)
+                mine = far;
+                far = 0u;
+                top_key = __reduce_max_sync(kFull, mine);
+                if (top_key == 0u) break;
+            }
             const uint32_t g = __reduce_min_sync(kFull, mine == top_key ? static_cast<uint32_t>(group) : kFull);
             keep |= 1u << g;
             if (static_cast<uint32_t>(group) == g) mine = 0u;
