@@ -79,6 +79,20 @@ __device__ __forceinline__ void load_run(const T *p, float (&x)[NV])
     }
 }
 
+// This lane's share of the chosen scores where all of them underflow (a bias may choose any expert): that of exp(logit), for
+// sigmoid scores as well (exp(l) / (1 + exp(l)), the divisor 1 there), taken from the largest of them.  0 where none is chosen.
+__device__ __noinline__ float tiny_share(float l)
+{
+    float m = l;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+    const float w = l > -INFINITY ? exp_from(l, m) : 0.f;
+    float s = w;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+    return s > 0.f ? w / s : 0.f;
+}
+
 template <typename T, int NV>
 __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const RouteArgs a)
 {
@@ -297,7 +311,8 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_topk_kernel(const Rout
         float s = w;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-        w = s > 0.f ? w / s : w;
+        if (s >= kLeastScore) w /= s;
+        else if (top < INFINITY) w = tiny_share(id >= 0 ? to_f32<T>(row[id]) : -INFINITY);
     }
     if (lane < a.k) {
         a.weights[token * a.k + lane] = w * a.scale;

@@ -63,3 +63,26 @@ def test_closed_groups_stay_closed():
     x[0, 1], x[0, 6] = 0.0, -3e38
     w, ids = qnn.route_topk(x, 3, groups=4, top_groups=3, group_score="top2")
     assert ids.tolist() == [[1, 6, -1]] and w.tolist() == [[1.0, 0.0, 0.0]]
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_shares_of_chosen_experts_that_all_underflow(score):
+    """A balance bias may choose experts whose scores are all tiny; their shares add up to one all the same."""
+    x = logits(40, 64, 5).clamp(-4, 4)
+    bias = torch.zeros(64, device="cuda")
+    far = torch.arange(3, 64, 9, device="cuda")
+    if score == "softmax":
+        x[:, far] -= 180.0
+    else:
+        x -= 180.0
+    bias[far] = 10.0 + torch.arange(far.numel(), device="cuda")
+    check(x, 5, score=score, bias=bias, scale=2.5)
+
+
+def test_an_infinite_logit_leaves_the_others_nothing():
+    x = logits(3, 16, 6)
+    x[:, 2] = math.inf
+    bias = torch.zeros(16, device="cuda")
+    bias[8:] = 10.0
+    w, ids = qnn.route_topk(x, 4, bias=bias)
+    assert bool((ids >= 8).all()) and bool((w == 0).all())
