@@ -478,7 +478,9 @@ enum {
  * A weight matrix [rows][k], or one for each of `experts` experts; rows is m,
  * or 2 m for a gated product: m gate rows, then m up rows.  Weights are 16-bit
  * floats of type `dtype`, or packed signed 8/4/2-bit codes in the sub-byte
- * order above with one float scale a row.
+ * order above with one float scale a row.  experts * rows * k, with the rows
+ * of an expert counted in 32s (gate and up rows in 8s each before that) and k
+ * in 64s, is at most 2^40.
  */
 typedef struct {
     uint32_t struct_size;      /* = sizeof(qnn_matmul_desc) */
@@ -509,7 +511,7 @@ qnn_status qnn_matmul_prepare(const qnn_matmul_desc *d, const void *w, const flo
  *   y = residual + act(v)             or  residual + act(v_gate) * v_up
  *
  * rounded once.  x [t][k], residual [t][m] or NULL, y [t][m] of type dtype, or
- * float when out_f32 is set; t is at most 2^20.  y may be the residual itself (same pointer,
+ * float when out_f32 is set; t is at most 2^20, t * m at most 2^38.  y may be the residual itself (same pointer,
  * stride and type), no other overlap.  Workspace (256-byte aligned) as
  * qnn_matmul_workspace_size() says for the same d, t, x and ldx.
  */
@@ -520,7 +522,7 @@ qnn_status qnn_matmul_run(const qnn_matmul_desc *d, const void *image, size_t im
 
 /*
  * The experts' products over a plan of qnn_expert_plan() (tokens * top slots,
- * at most 2^20 of them, top at most 1024).
+ * at most 2^20 of them, top at most 1024, slots * m at most 2^38).
  *
  * qnn_experts_dispatch: row p of y is the product of x[order[p] / top] with
  *   the weights of the expert that place p belongs to; x [tokens][k],

@@ -14,6 +14,10 @@ bool dtype_ok(int32_t t) { return t == QNN_F16 || t == QNN_BF16 || t == QNN_F32;
 uintptr_t dtype_size(int32_t t) { return t == QNN_F32 ? 4 : 2; }
 bool flag_ok(int32_t v) { return v == 0 || v == 1; }
 
+// What the kernels' 32-bit counters of tiles and of units of work hold, whatever tile the launch takes: 2^40 weights in
+// 32 x 64 blocks, 2^38 outputs and 2^20 rows of x give less than 2^30 tiles and 2^31 units.
+constexpr int64_t kMaxBlocks = 1ll << 29, kMaxOutputs = 1ll << 38, kMaxRows = 1 << 20;
+
 qnn_status check_matmul(const qnn_matmul_desc *d)
 {
     if (!d || d->struct_size != sizeof(qnn_matmul_desc)) return QNN_EINVAL;
@@ -22,10 +26,15 @@ qnn_status check_matmul(const qnn_matmul_desc *d)
     if (d->dtype == QNN_F32 || (d->bits != 16 && d->bits != 8 && d->bits != 4 && d->bits != 2)) return QNN_EUNSUPPORTED;
     if (d->experts > 1024 || d->m > (1 << 24) || d->k > (1 << 24)) return QNN_EUNSUPPORTED;
     if (d->bits < 8 && d->k % (8 / d->bits)) return QNN_EUNSUPPORTED;
-    return QNN_OK;
+    const MatmulImage g = matmul_image(d->experts, d->m, d->k, d->bits, d->gated);
+    return static_cast<int64_t>(d->experts) * g.mb * g.kb > kMaxBlocks ? QNN_EUNSUPPORTED : QNN_OK;
 }
 
-constexpr int64_t kMaxRows = 1 << 20;  // rows of x in one call
+// An output of `rows` rows.
+qnn_status check_rows(const qnn_matmul_desc &d, int64_t rows)
+{
+    return rows > kMaxRows || rows * d.m > kMaxOutputs ? QNN_EUNSUPPORTED : QNN_OK;
+}
 
 MatmulArgs base_args(const qnn_matmul_desc &d, const void *image, const void *x, int64_t ldx, void *y, int64_t ldy)
 {
@@ -88,8 +97,8 @@ qnn_status check_slots(const qnn_matmul_desc *d, int64_t tokens, int32_t top)
     const qnn_status st = check_matmul(d);
     if (st != QNN_OK) return st;
     if (tokens < 0 || top <= 0) return QNN_EINVAL;
-    if (top > 1024 || tokens > kMaxRows || tokens * top > kMaxRows) return QNN_EUNSUPPORTED;
-    return QNN_OK;
+    if (top > 1024 || tokens > kMaxRows) return QNN_EUNSUPPORTED;
+    return check_rows(*d, tokens * top);
 }
 
 }  // namespace
@@ -188,9 +197,8 @@ qnn_status qnn_matmul_workspace_size(const qnn_matmul_desc *d, int64_t t, const 
     const qnn_status st = check_matmul(d);
     if (st != QNN_OK) return st;
     if (t < 0 || ldx < d->k) return QNN_EINVAL;
-    if (t > kMaxRows) return QNN_EUNSUPPORTED;
     *bytes = staging_bytes(*d, t, 0, false, x, ldx);
-    return QNN_OK;
+    return check_rows(*d, t);
 }
 
 qnn_status qnn_matmul_run(const qnn_matmul_desc *d, const void *image, size_t image_bytes, int64_t t, const void *x,

@@ -416,7 +416,6 @@ cudaError_t launch_matmul_stream(const MatmulArgs &a, int dtype, int bits, cudaS
     int64_t tiles = (a.rows + nt - 1) / nt;
     if (a.offsets) tiles += a.experts < a.rows ? a.experts : a.rows;  // each expert may end in a partial tile
     if (tiles == 0) return cudaSuccess;
-    if (tiles * a.mb * ((a.kb + 7) / 8) > 0x7fffffff) return cudaErrorInvalidConfiguration;  // the kernel's counters have 32 bits
     return dtype == QNN_F16 ? launch_bits<__half>(a, bits, nt, tiles, st)
                             : launch_bits<__nv_bfloat16>(a, bits, nt, tiles, st);
 }

@@ -663,7 +663,6 @@ cudaError_t launch_matmul_tc(const MatmulArgs &a, int dtype, int bits, cudaStrea
     int64_t u = (a.rows + nt - 1) / nt;
     if (a.offsets) u += a.experts < a.rows ? a.experts : a.rows;
     const int64_t tiles = u * s.mt;  // at most; experts' tiles are counted by the kernel
-    if (tiles > 0x7fffffff / 2) return cudaErrorInvalidConfiguration;
     CUtensorMap map;
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.k), static_cast<cuuint64_t>(a.x_rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a.ldx) * 2};
