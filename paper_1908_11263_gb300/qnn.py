@@ -9,10 +9,12 @@ dimension counts bytes):
   activations  uint8 [n, h, w, c*Q/8]    weights  int8/uint8 [m, kh, kw, c*Q/8]
   outputs      uint8 [n, oh, ow, m*Q/8]
 
-Tensors and streams are the current device's; others are refused.  `stream` (a torch.cuda.Stream) is where a call's kernels are queued; without it, the current stream.  What a call allocates
-belongs to that stream, and the stream that is current at the call may use it too, once it is ordered after the call; other
-streams need record_stream(), as for any tensor.  Inputs are the caller's to keep until the stream has passed the call; only
-the weights that PreparedMatmul and PreparedExperts lay out may be dropped at once.
+Tensors and streams are the current device's; others are refused, and so are tensors that require a gradient outside
+torch.no_grad() and torch.inference_mode().  `stream` (a torch.cuda.Stream) is where a call's kernels are queued; without
+it, the current stream.  What a call allocates belongs to that stream, and the stream that is current at the call may use it
+too, once it is ordered after the call; other streams need record_stream(), as for any tensor.  Inputs are the caller's to
+keep until the stream has passed the call; only the weights that PreparedMatmul and PreparedExperts lay out may be dropped
+at once.
 """
 from __future__ import annotations
 
@@ -546,10 +548,17 @@ def unpack_subbyte(src, bits, signed, *, out=None, stream=None):
 
 # ---------------------------------------------------------------- language-model block operators
 
+def _no_gradient(t, name):
+    """The library computes no gradients: a result that a graph should hold would leave it without a word."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which this library does not compute; make the call under torch.no_grad()")
+
+
 def _rows(t: torch.Tensor, dtype, name, shape=None, device=None):
     """A CUDA matrix with contiguous columns and any row stride, on `device` (None: on the current one); returns (pointer,
     row stride)."""
-    if t.dtype is dtype and t.is_cuda and (t.device.index == _current_device() if device is None else t.device == device):
+    if t.dtype is dtype and t.is_cuda and not t.requires_grad and (
+            t.device.index == _current_device() if device is None else t.device == device):
         s = t.shape
         if len(s) == 2 and (shape is None or s == shape):
             ld, step = t.stride()
@@ -563,6 +572,7 @@ def _rows_slow(t, dtype, name, shape, device):
         raise ValueError(f"{name} must be a CUDA tensor" + ("" if device is None else f" on {device}"))
     if device is None:
         _on_current(t.device, name)
+    _no_gradient(t, name)
     if t.dtype != dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
@@ -579,6 +589,7 @@ def _param(t, dtype, name, shape, device):
     if t is None:
         return None
     if t.dtype is dtype and t.device == device and t.shape == shape and t.is_contiguous():
+        _no_gradient(t, name)
         return t.data_ptr()
     if t.device != device:
         raise ValueError(f"{name} must be on {device}")
@@ -767,6 +778,7 @@ class _Prepared:
             if w.dtype not in (torch.float16, torch.bfloat16) or dtype not in (None, w.dtype):
                 raise TypeError(f"16-bit weights must be float16 or bfloat16 and dtype, if given, theirs; got {w.dtype}, {dtype}")
             _dev(w, None, "w")
+            _no_gradient(w, "w")
             dtype, per = w.dtype, 1
         elif bits in (8, 4, 2):
             _dev(w, (torch.uint8, torch.int8), "w")
