@@ -188,9 +188,10 @@ def _ptr(t):
     """Pointer of a tensor that is not another device's, or NULL."""
     if t is None:
         return None
-    if t.is_cuda:
+    index = t.get_device()  # -1: host memory
+    if index >= 0 and index != _current_device():
         _on_current(t.device, "a tensor")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream(stream):
@@ -279,10 +280,36 @@ def _workspace(nbytes: int, device, stream):
     """A workspace for one call.  Each call has its own: calls that several host threads make on one stream interleave
     their launches, and hold data in the workspace between them.  It is allocated on the launching stream, so it may go
     back to the allocator as soon as the call has returned; in a stream capture it comes from the graph's own memory."""
-    if nbytes == 0:
-        return None
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _run_with_workspace(call, size, device, stream):
+    """call(pointer, bytes, stream handle), without a workspace first (most calls need none; the library queues nothing
+    where it says that one is missing), then with one of this call's own."""
+    handle = _stream_of(stream, device)
+    st = call(None, 0, handle)
+    if st == QNN_EWORKSPACE:
+        need = size()
+        ws = _workspace(need, device, stream)
+        st = call(ws.data_ptr(), need, handle)
+    return st
+
+
+def _run_conv(name, desc, tensors, workspace, stream):
+    """name(desc, *tensors, workspace, bytes, stream) with the caller's workspace, or one of its own where it needs one."""
+    call, device = getattr(load(), name), tensors[0].device
+    d, pointers = ctypes.byref(desc), [_ptr(t) for t in tensors]
+    if workspace is None:
+        st = _run_with_workspace(lambda ws, n, handle: call(d, *pointers, ws, n, handle), lambda: workspace_size(desc), device, stream)
+    else:
+        nbytes = workspace_size(desc)
+        if workspace.numel() < nbytes:
+            raise ValueError("workspace too small")
+        st = call(d, *pointers, _ptr(workspace), nbytes, _stream_of(stream, device))
+    _check(st, name)
 
 
 def conv_hwc(x, w, kappa, lam, *, bias=None, shifts=None, shift=0, bits=8, stride=1, pad=0, algo=ALGO_AUTO,
@@ -308,14 +335,7 @@ def conv_hwc(x, w, kappa, lam, *, bias=None, shifts=None, shift=0, bits=8, strid
         out = _empty((n, oh, ow, m // per), torch.uint8, x.device, stream)
     else:
         _dev(out, torch.uint8, "out")
-    nbytes = workspace_size(desc)
-    if workspace is None:
-        workspace = _workspace(nbytes, x.device, stream)
-    elif workspace.numel() < nbytes:
-        raise ValueError("workspace too small")
-    st = load().qconv_hwc(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(kappa), _ptr(lam), _ptr(shifts),
-                          _ptr(out), _ptr(workspace), ctypes.c_size_t(nbytes), _stream(stream))
-    _check(st, "qconv_hwc")
+    _run_conv("qconv_hwc", desc, (x, w, bias, kappa, lam, shifts, out), workspace, stream)
     return out
 
 
@@ -343,14 +363,7 @@ def conv_hwc_pool2(x, w, kappa, lam, *, bias=None, shifts=None, shift=0, bits=8,
         out = _empty((n, oh // 2, ow // 2, m // per), torch.uint8, x.device, stream)
     else:
         _dev(out, torch.uint8, "out")
-    nbytes = workspace_size(desc)
-    if workspace is None:
-        workspace = _workspace(nbytes, x.device, stream)
-    elif workspace.numel() < nbytes:
-        raise ValueError("workspace too small")
-    st = load().qconv_hwc_pool2(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(kappa), _ptr(lam),
-                                _ptr(shifts), _ptr(out), _ptr(workspace), ctypes.c_size_t(nbytes), _stream(stream))
-    _check(st, "qconv_hwc_pool2")
+    _run_conv("qconv_hwc_pool2", desc, (x, w, bias, kappa, lam, shifts, out), workspace, stream)
     return out
 
 
@@ -376,14 +389,7 @@ def conv_hwc_thresholds(x, w, thresholds, *, bits, stride=1, pad=0, algo=ALGO_AU
         out = _empty((n, oh, ow, m // per), torch.uint8, x.device, stream)
     else:
         _dev(out, torch.uint8, "out")
-    nbytes = workspace_size(desc)
-    if workspace is None:
-        workspace = _workspace(nbytes, x.device, stream)
-    elif workspace.numel() < nbytes:
-        raise ValueError("workspace too small")
-    st = load().qconv_hwc_thresholds(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(thresholds), _ptr(out),
-                                     _ptr(workspace), ctypes.c_size_t(nbytes), _stream(stream))
-    _check(st, "qconv_hwc_thresholds")
+    _run_conv("qconv_hwc_thresholds", desc, (x, w, thresholds, out), workspace, stream)
     return out
 
 
@@ -558,7 +564,7 @@ def _rows(t: torch.Tensor, dtype, name, shape=None, device=None):
     """A CUDA matrix with contiguous columns and any row stride, on `device` (None: on the current one); returns (pointer,
     row stride)."""
     if t.dtype is dtype and t.is_cuda and not t.requires_grad and (
-            t.device.index == _current_device() if device is None else t.device == device):
+            t.get_device() == _current_device() if device is None else t.device == device):
         s = t.shape
         if len(s) == 2 and (shape is None or s == shape):
             ld, step = t.stride()
@@ -596,18 +602,6 @@ def _param(t, dtype, name, shape, device):
     if t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(t.shape)}")
-
-
-def _run_with_workspace(call, size, device, stream):
-    """call(pointer, bytes, stream handle), without a workspace first (most calls need none; the library queues nothing
-    where it says that one is missing), then with one of this call's own."""
-    handle = _stream_of(stream, device)
-    st = call(None, 0, handle)
-    if st == QNN_EWORKSPACE:
-        need = size()
-        ws = _workspace(need, device, stream)
-        st = call(ws.data_ptr(), need, handle)
-    return st
 
 
 def _float_dtype(t, name):
