@@ -11,6 +11,35 @@
 namespace qnn {
 
 // ---- norms around a block -- norm.cu
+// Blocks of the resident norm kernel and their rings.  As many blocks as the threads of an SM allow (64 registers each) while
+// every block has two stages or more; all of them have to fit the SM at once, with their static memory and the 1 KB that the
+// system takes of each, or those that do not start only when the others have done their rows.  (161318 rows of 832, 16
+// blocks an SM: 294 us with rings of four stages, of which 15 fit, 215 with three; 101066 rows of 1328, ten blocks: 295 and
+// 205 us.)
+constexpr int kNormItems = 2;                  // vectors of eight values a thread
+constexpr uint32_t kNormRoom = 208 * 1024;     // of ring on an SM at most: the rest of the 256 KB stays L1
+constexpr uint32_t kNormSm = 228 * 1024;       // shared memory of an SM
+constexpr uint32_t kNormStatic = 1152;         // of a block
+struct NormRing {
+    int threads, per_sm, stages;
+    uint32_t x_bytes, res_bytes, smem;  // of a row of x and of the residual (0 without one); of a block's ring
+};
+inline NormRing norm_ring(int d, uint32_t x_bytes, uint32_t res_bytes)
+{
+    NormRing r = {((d + 8 * kNormItems - 1) / (8 * kNormItems) + 31) / 32 * 32, 0, 0, x_bytes, res_bytes, 0};
+    if (r.threads < 64) r.threads = 64;
+    const uint32_t stage = x_bytes + res_bytes;
+    auto room = [](int blocks) {  // of each of so many blocks; memory is given out in units of 128 bytes
+        const uint32_t ring = kNormRoom / blocks, whole = kNormSm / blocks / 128 * 128 - kNormStatic - 1024;
+        return ring < whole ? ring : whole;
+    };
+    r.per_sm = 1024 / r.threads;
+    while (r.per_sm > 1 && room(r.per_sm) < 2 * stage) --r.per_sm;
+    const uint32_t fit = room(r.per_sm) / stage;
+    r.stages = fit > 4 ? 4 : static_cast<int>(fit);
+    r.smem = r.stages * stage;
+    return r;
+}
 cudaError_t launch_block_norm(const qnn_norm_desc &d, const void *x, const void *residual, const void *gate,
                               const void *post_w, const void *post_b, const void *pre_w, const void *pre_b, void *r,
                               void *h, cudaStream_t st);

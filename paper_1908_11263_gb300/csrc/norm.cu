@@ -271,19 +271,19 @@ struct Held<float, VEC> {  // 32-bit rows: read again for each row
     __device__ __forceinline__ void scale(float (&)[2][8]) const {}
 };
 
-struct StreamShape {
-    int stages;
-    uint32_t x_bytes, res_bytes;  // of a row; res_bytes 0 without a residual
+struct NormShared {
+    float part[2][4][32];
+    uint64_t full[8];
 };
-
-constexpr int kNormItems = 2;  // 16 values a thread
+static_assert((sizeof(NormShared) + 127) / 128 * 128 == kNormStatic, "shared memory that norm_ring() reckons with");
 
 template <typename T, typename R, int VEC>
-__global__ void __launch_bounds__(1024) block_norm_stream_kernel(const NormArgs a, const StreamShape s, int64_t t, int *status)
+__global__ void __launch_bounds__(1024) block_norm_stream_kernel(const NormArgs a, const NormRing s, int64_t t, int *status)
 {
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ __align__(16) float part[2][4][32];
-    __shared__ uint64_t full[8];
+    __shared__ __align__(16) NormShared shared;
+    auto &part = shared.part;
+    uint64_t *full = shared.full;
     using Q = Row<VEC, kNormItems, true>;
     const uint32_t stage_bytes = s.x_bytes + s.res_bytes;
     if (threadIdx.x == 0) {
@@ -385,24 +385,14 @@ cudaError_t launch_stream(const NormArgs &a, int64_t t, cudaStream_t stream, boo
     if (a.d % 8 || a.d > 8192 * kNormItems) return cudaSuccess;
     int *status = device_status_ptr();
     if (!status) return cudaErrorNotSupported;
-    StreamShape s;
-    s.x_bytes = a.d * sizeof(T);
-    s.res_bytes = a.residual ? a.d * sizeof(R) : 0;
-    int threads = ((a.d + 8 * kNormItems - 1) / (8 * kNormItems) + 31) / 32 * 32;
-    if (threads < 64) threads = 64;
-    const int sms = device_sm_count();
-    const uint32_t room = 208 * 1024, stage = s.x_bytes + s.res_bytes;
-    int per_sm = 1024 / threads;
-    while (per_sm > 1 && room / per_sm < 2 * stage) --per_sm;
-    const uint32_t fit = room / per_sm / stage;
-    s.stages = fit > 4 ? 4 : static_cast<int>(fit);
+    const NormRing s = norm_ring(a.d, a.d * sizeof(T), a.residual ? a.d * sizeof(R) : 0);
+    const int blocks = s.per_sm * device_sm_count();
     // a few rows a block at least, or the ring does not pay for itself
-    if (s.stages < 2 || t < 3ll * per_sm * sms) return cudaSuccess;
-    const size_t smem = static_cast<size_t>(s.stages) * stage;
-    const cudaError_t e = raise_smem<block_norm_stream_kernel<T, R, VEC>>(room);
+    if (s.stages < 2 || t < 3ll * blocks) return cudaSuccess;
+    const cudaError_t e = raise_smem<block_norm_stream_kernel<T, R, VEC>>(kNormRoom);
     if (e != cudaSuccess) return e;
     *taken = true;
-    return launch_pdl(block_norm_stream_kernel<T, R, VEC>, dim3(per_sm * sms), threads, smem, stream, 1, a, s, t, status);
+    return launch_pdl(block_norm_stream_kernel<T, R, VEC>, dim3(blocks), s.threads, s.smem, stream, 1, a, s, t, status);
 }
 
 bool rows_aligned(const void *p, int64_t ld, int size)
