@@ -1,6 +1,7 @@
 // The weight image of the matrix products (qnn_matmul_prepare) and the weighted sum over a token's experts that ends
-// qnn_experts_combine.  Both are bound by memory: each byte is read and written once.  8192 x 8192 INT-4 are laid out in
-// 64 us; the sum over 4099 x 4 rows of 2048 takes 25.
+// qnn_experts_combine.  The preparation is bound by its instructions, not by its bytes: a thread gathers the codes of a
+// 16-byte vector one by one (8192 x 8192: 79 us with 16-bit weights, 70 INT-8, 66 INT-4 and INT-2, where the bytes of INT-4
+// take 10).  It runs once, when a layer is set up.  The sum is bound by memory: 4099 x 4 rows of 2048 take 25 us.
 #include "matmul.cuh"
 
 namespace qnn {

@@ -14,8 +14,10 @@
 // the A operand, two groups on alternate stages.  Rows that an expert picks from x lie one after another before the
 // launch: picking them inside it held the MMAs up (692 us with four-row TMA gathers, which take some 80 cycles each, 371
 // with cp.async by two warps, for a product that takes 165 on rows in order and a copy that takes 27).
-// Bound by the tensor pipe from about 500 rows of x on: 8192 x 4096 x 2 * 8192, gated silu, 536 us with 16-bit weights
-// (2.05 PFLOP/s), 639 INT-8, 566 INT-4; below that by the weights (64 x 8192 x 8192 16-bit 28 us) and, for small
+// Bound by the tensor pipe from about 500 rows of x on, with packed weights by the expansion, which every tile of x repeats
+// and which hands a stage on in some 600 cycles where the MMAs take 512: 8192 x 4096 x 2 * 8192, gated silu, 533 us with
+// 16-bit weights in ten calls in a row (2.06 PFLOP/s) and 556 in a hundred, where the power cap has set in; 734 INT-8, 644
+// INT-4 and 616 INT-2 in a hundred.  Below 500 rows by the weights (64 x 8192 x 8192 16-bit 28 us) and, for small
 // matrices, by its fixed cost of some 10 us.
 // Every wait is bounded (mbar_wait_warp); a wait that gives up ends its role, and the kernel, with the status word set.
 #include <cuda.h>

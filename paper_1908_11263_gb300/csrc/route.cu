@@ -5,7 +5,8 @@
 // lanes and the lowest index among equals one integer minimum: ties go to the lowest index by construction.  The choice
 // uses the score itself (the logit where softmax scores carry no bias: the same order without rounding).  Groups that are
 // whole lanes, a power of two of them, find their two best with a few shuffles; other splits go through shared memory.
-// The kernel is bound by its instructions, not by the logits' bytes: 32768 tokens, 8 of 256 experts in 16 groups, 32 us.
+// The kernel is bound by its instructions, not by the logits' bytes: 32768 tokens, 8 of 256 experts in 16 groups, sigmoid
+// with a bias, 30 us, 930 instructions a token.
 //
 // expert plan: a stable counting sort of the slots (token * top + choice) by expert.  Ranks come from ordered per-warp
 // counts, never from the order in which atomics land, so the plan is the same on every run.  262144 slots over 256
