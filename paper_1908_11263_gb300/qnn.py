@@ -594,14 +594,16 @@ def _param(t, dtype, name, shape, device):
     """An optional contiguous parameter; returns its pointer or None."""
     if t is None:
         return None
-    if t.dtype is dtype and t.device == device and t.shape == shape and t.is_contiguous():
-        _no_gradient(t, name)
+    if t.dtype is dtype and t.device == device and t.shape == shape and not t.requires_grad and t.is_contiguous():
         return t.data_ptr()
     if t.device != device:
         raise ValueError(f"{name} must be on {device}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(t.shape)}")
+    _no_gradient(t, name)
+    return t.data_ptr()
 
 
 def _float_dtype(t, name):
