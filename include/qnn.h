@@ -541,6 +541,157 @@ qnn_status qnn_experts_combine(const qnn_matmul_desc *d, const void *image, size
                                const void *x, int64_t ldx, const void *residual, int64_t ldres, void *y, int64_t ldy,
                                void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The attention half of a block, for serving: rotary positions, a paged cache
+ * of keys and values, attention over it, and cross attention to an encoder's
+ * states.  Heads are strided (elements); a head's elements are contiguous.
+ * ---------------------------------------------------------------------- */
+
+/* Frequencies f_i of the pairs i < dim / 2 (radians a position):
+ * f_i = base^(-2 i / dim), and for contexts `factor` times as long: */
+enum {
+    QNN_ROPE_NONE = 0,
+    QNN_ROPE_LINEAR = 1,       /* f_i / factor */
+    QNN_ROPE_BASE = 2,         /* base * factor^(dim / (dim - 2)) as the base (dim > 2) */
+    QNN_ROPE_RAMP = 3          /* g f_i + (1 - g) f_i / factor, g = (context * f_i / 2 pi - low) / (high - low) in 0 .. 1:
+                                  pairs that turn `high` times or more in the original context stay, those that turn
+                                  `low` times or less are stretched */
+};
+
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_rope_scaling) */
+    int32_t dim;               /* rotated elements of a head, even */
+    int32_t scaling;           /* QNN_ROPE_* */
+    int32_t context;           /* original context (QNN_ROPE_RAMP) */
+    double base;               /* > 1 */
+    double factor;             /* >= 1 */
+    double low, high;          /* rotations (QNN_ROPE_RAMP), low < high */
+} qnn_rope_scaling;
+
+/*
+ * The frequencies as the kernels take them: turns[i] (host, dim / 2 of them)
+ * is f_i / 2 pi as a binary fraction of 64 bits, so that position * turns[i]
+ * modulo 2^64 is the pair's phase, exact at any position of either sign.
+ * Frequencies of one's own may be given the same way.
+ */
+qnn_status qnn_rope_turns(const qnn_rope_scaling *s, uint64_t *turns);
+
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_rope_desc) */
+    int32_t dtype;             /* of x and y */
+    int32_t heads;
+    int32_t head_dim;          /* at most 1024 */
+    int32_t dim;               /* rotated elements, the first of a head: even, 0 .. head_dim */
+    int32_t interleaved;       /* pairs (2 i, 2 i + 1), else (i, i + dim / 2) */
+    int32_t wide;              /* positions are int64, else int32 */
+    float amplitude;           /* of the rotated elements */
+    int64_t t;                 /* tokens; t * heads below 2^31 */
+    int64_t ldx, hx, ldy, hy;  /* strides of tokens and heads */
+} qnn_rope_desc;
+
+/*
+ * y = x with every pair (a, b) of its rotated elements turned by the angle p f_i of its token's position p:
+ *   amplitude * (a cos - b sin, a sin + b cos)
+ * in 32 bits, rounded once; the other elements are copied.  A position -p turns back.  y may be x (same strides), no
+ * other overlap.
+ *   turns device uint64[dim / 2]    positions device int64 or int32 [t]
+ */
+qnn_status qnn_rope(const qnn_rope_desc *d, const uint64_t *turns, const void *positions, const void *x, void *y, void *stream);
+
+/*
+ * A cache of keys and values in pages.  Row r of page p and head h begins at
+ * p * k_page + h * k_head + r * k_row elements of the keys (values likewise),
+ * so any order of the dimensions may be given.  16-byte aligned rows: the
+ * strides are multiples of 8, the pointers 16-byte aligned (else QNN_EALIGN).
+ */
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_cache_desc) */
+    int32_t dtype;             /* QNN_F16 or QNN_BF16: keys, values, queries, outputs */
+    int32_t kv_heads;          /* at most 1024 */
+    int32_t head_dim;          /* a multiple of 8, at most 256 */
+    int32_t page_size;         /* rows of a page */
+    int64_t pages;
+    int64_t k_page, k_head, k_row;
+    int64_t v_page, v_head, v_row;
+} qnn_cache_desc;
+
+/*
+ * The sequences of a call.  Sequence s has lengths[s] tokens, the call's new
+ * ones included: token j of it lies in row j % page_size of page
+ * table[s * ldt + j / page_size].  A table entry outside [0, pages) stands for
+ * no page: nothing is written there, and its tokens are not attended to.
+ * Tokens past the table's width are not in the cache.
+ *
+ * The call's t tokens are the sequences' new ones: ragged, sequence s has rows
+ * offsets[s] .. offsets[s + 1] (rising; rows before the first and behind the
+ * last are in no sequence, and are neither read nor written); else t / seqs
+ * rows each.  New token i of n is token lengths[s] - n + i.
+ *
+ * table int32, lengths int32[seqs], offsets int32[seqs + 1]: device.
+ */
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_batch_desc) */
+    int32_t seqs;
+    int32_t width;             /* pages of a row of the table; width * page_size at most 2^30 */
+    int32_t ragged;            /* 1: with offsets */
+    int64_t t;                 /* a multiple of seqs unless ragged */
+    int64_t ldt;               /* row stride of the table */
+} qnn_batch_desc;
+
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_append_desc) */
+    int32_t heads;             /* of q; 0: no queries */
+    int32_t dim;               /* as in qnn_rope_desc; 0: nothing is rotated */
+    int32_t interleaved, wide;
+    float amplitude;
+    int64_t ldk, hk, ldv, hv, ldq, hq, ldo, ho;  /* strides of tokens and heads: k, v, q, q_out */
+} qnn_append_desc;
+
+/*
+ * Writes the sequences' new keys, rotated, and values to their places, and the
+ * rotated queries to q_out (which may be q, same strides).  k and v [t][kv_heads][head_dim], q
+ * [t][heads][head_dim].  The rotation goes by the token's place in its
+ * sequence, or by positions[t] when given.  A token whose place is not in the
+ * cache is not written.  Tokens of one call whose places are the same leave
+ * the elements of either.
+ */
+qnn_status qnn_cache_append(const qnn_cache_desc *c, const qnn_batch_desc *b, const qnn_append_desc *d, const int32_t *table,
+                            const int32_t *lengths, const int32_t *offsets, const uint64_t *turns, const void *positions,
+                            const void *k, const void *v, const void *q, void *k_pages, void *v_pages, void *q_out,
+                            void *stream);
+
+typedef struct {
+    uint32_t struct_size;      /* = sizeof(qnn_attention_desc) */
+    int32_t heads;             /* of q, a multiple of kv_heads: query head h reads key head h / (heads / kv_heads) */
+    int32_t causal;            /* 1: a new token sees the tokens up to itself; 0: all of its sequence */
+    int32_t window;            /* > 0: it sees no token `window` or more before itself; 0: no limit */
+    float scale;               /* of the products, > 0 */
+    int64_t q_seq, ldq, hq;    /* strides of q: sequences (not ragged), tokens, heads */
+    int64_t o_seq, ldo, ho;    /* of out */
+} qnn_attention_desc;
+
+/*
+ * out = sum_j softmax_j(scale * q . k_j) v_j over the tokens j that the new
+ * token sees; zero where it sees none.  lse (or NULL), float[t][heads]: the
+ * logarithm of the sum of exp(scale * q . k_j), -inf where there is none.
+ *
+ * table NULL: sequence s has the one page s (width at most 1), as for the
+ * states of an encoder.  lengths NULL: every sequence is width * page_size
+ * long.  q and out [t][heads][head_dim]; out overlaps nothing.  Rows of the
+ * cache that no new token sees may hold anything, also NaN; those that one
+ * sees are finite.
+ *
+ * 16-bit products are summed in 32 bits; the weights 2^(z - max) are rounded
+ * to 16 bits before they multiply the values, the sum of them is not.
+ * t * heads below 2^31.  Workspace as qnn_attention_workspace_size() says
+ * (256-byte aligned; NULL when 0).
+ */
+qnn_status qnn_attention_workspace_size(const qnn_cache_desc *c, const qnn_batch_desc *b, const qnn_attention_desc *d,
+                                        size_t *bytes);
+qnn_status qnn_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, const qnn_attention_desc *d, const int32_t *table,
+                         const int32_t *lengths, const int32_t *offsets, const void *q, const void *k_pages,
+                         const void *v_pages, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,7 @@ at once.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import threading
 
@@ -37,7 +38,8 @@ EXPORTED = ("qconv_hwc_workspace_size", "qconv_hwc", "qconv_hwc_prepare", "qconv
             "qconv_hwc_mma_operand_bits", "qconv_hwc_tc_kernel", "qnn_block_norm", "qnn_route_topk",
             "qnn_expert_plan_workspace_size", "qnn_expert_plan", "qnn_matmul_image_size", "qnn_matmul_prepare",
             "qnn_matmul_workspace_size", "qnn_matmul_run", "qnn_experts_workspace_size", "qnn_experts_dispatch",
-            "qnn_experts_combine")
+            "qnn_experts_combine", "qnn_rope_turns", "qnn_rope", "qnn_cache_append", "qnn_attention_workspace_size",
+            "qnn_attention")
 
 F16, BF16, F32 = 0, 1, 2  # QNN_F16, QNN_BF16, QNN_F32
 _DTYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
@@ -69,6 +71,38 @@ class RouteDesc(ctypes.Structure):
 class MatmulDesc(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in (
         "experts", "m", "k", "bits", "dtype", "gated", "act")]
+
+
+class RopeScaling(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in ("dim", "scaling", "context")] + [
+        (f, ctypes.c_double) for f in ("base", "factor", "low", "high")]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in (
+        "dtype", "heads", "head_dim", "dim", "interleaved", "wide")] + [("amplitude", ctypes.c_float)] + [
+            (f, ctypes.c_int64) for f in ("t", "ldx", "hx", "ldy", "hy")]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in (
+        "dtype", "kv_heads", "head_dim", "page_size")] + [(f, ctypes.c_int64) for f in (
+            "pages", "k_page", "k_head", "k_row", "v_page", "v_head", "v_row")]
+
+
+class BatchDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in ("seqs", "width", "ragged")] + [
+        (f, ctypes.c_int64) for f in ("t", "ldt")]
+
+
+class AppendDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in ("heads", "dim", "interleaved", "wide")] + [
+        ("amplitude", ctypes.c_float)] + [(f, ctypes.c_int64) for f in ("ldk", "hk", "ldv", "hv", "ldq", "hq", "ldo", "ho")]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(f, ctypes.c_int32) for f in ("heads", "causal", "window")] + [
+        ("scale", ctypes.c_float)] + [(f, ctypes.c_int64) for f in ("q_seq", "ldq", "hq", "o_seq", "ldo", "ho")]
 
 
 _lock = threading.Lock()
@@ -150,6 +184,17 @@ def load(build_if_missing: bool = False):
         lib.qnn_experts_dispatch.restype = I32
         lib.qnn_experts_combine.argtypes = [MP, P, SZ, I64, I32, P, P, P, P, I64, P, I64, P, I64, P, SZ, P]
         lib.qnn_experts_combine.restype = I32
+        lib.qnn_rope_turns.argtypes = [ctypes.POINTER(RopeScaling), P]
+        lib.qnn_rope_turns.restype = I32
+        lib.qnn_rope.argtypes = [ctypes.POINTER(RopeDesc)] + [P] * 5
+        lib.qnn_rope.restype = I32
+        CP, BP, AP = ctypes.POINTER(CacheDesc), ctypes.POINTER(BatchDesc), ctypes.POINTER(AttentionDesc)
+        lib.qnn_cache_append.argtypes = [CP, BP, ctypes.POINTER(AppendDesc)] + [P] * 12
+        lib.qnn_cache_append.restype = I32
+        lib.qnn_attention_workspace_size.argtypes = [CP, BP, AP, ctypes.POINTER(SZ)]
+        lib.qnn_attention_workspace_size.restype = I32
+        lib.qnn_attention.argtypes = [CP, BP, AP] + [P] * 9 + [SZ, P]
+        lib.qnn_attention.restype = I32
         lib.qnn_selftest_wait_timeout.argtypes = [I64, P]
         lib.qnn_selftest_wait_timeout.restype = I32
         lib.qnn_device_status.argtypes = [P]
@@ -909,6 +954,283 @@ class PreparedExperts(_Prepared):
             self._desc, self._image, self.nbytes, tokens, top, plan._offsets, plan._position, pw, px, ldx, pres, ldres, po,
             ldo, ws, n, handle), plan, 1, px, ldx, stream)
         return out
+
+
+# ---------------------------------------------------------------- rotary positions, paged cache, attention
+
+_SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+def _heads(t, dtype, name, shape=None, device=None):
+    """A CUDA tensor [..., heads, head_dim] with contiguous heads and any other strides, on `device` (None: on the current
+    one); returns (pointer, strides without the last), with a stride of 0 where a dimension has one element."""
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be a CUDA tensor" + ("" if device is None else f" on {device}"))
+    if device is None:
+        _on_current(t.device, name)
+    if t.requires_grad:
+        _no_gradient(t, name)
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    sizes, strides = t.shape, t.stride()
+    if shape is not None and sizes != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(sizes)}")
+    if strides[-1] != 1 and sizes[-1] > 1:
+        raise ValueError(f"{name} must have contiguous heads")
+    return t.data_ptr(), [0 if n == 1 else d for n, d in zip(sizes[:-1], strides)]
+
+
+def _int32(t, name, shape, device):
+    """A contiguous int32 tensor; returns its pointer."""
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.dtype is not torch.int32:
+        raise TypeError(f"{name} must have dtype torch.int32, got {t.dtype}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _positions(t, tokens, device):
+    """Pointer of int32 or int64 positions, and whether they are int64."""
+    if t.device != device:
+        raise ValueError(f"positions must be on {device}")
+    if t.dtype is not torch.int64 and t.dtype is not torch.int32:
+        raise TypeError(f"positions must be int32 or int64, got {t.dtype}")
+    if t.shape != (tokens,) or not t.is_contiguous():
+        raise ValueError(f"positions must be contiguous with shape {(tokens,)}, got {tuple(t.shape)}")
+    return t.data_ptr(), int(t.dtype is torch.int64)
+
+
+class Rotary:
+    """Frequencies of a position rotation over the first `dim` elements of a head, laid out once (qnn_rope_turns): pairs
+    (i, i + dim / 2), or neighbours with interleaved=True, turn by base^(-2 i / dim) radians a position.  For contexts
+    `factor` times as long, scaling is "linear" (frequencies divided by the factor), "base" (a larger base) or "ramp"
+    (pairs that turn `high` times or more in the original `context` stay as they are, those that turn `low` times or less
+    are divided, those between blended); "none" takes no factor.  `amplitude` multiplies the rotated elements.
+    `frequencies` (dim / 2 numbers, radians a position) replaces all of that."""
+
+    __slots__ = ("dim", "interleaved", "amplitude", "turns", "device")
+
+    def __init__(self, dim, *, base=10000.0, interleaved=False, scaling="none", factor=1.0, context=0, low=1.0, high=32.0,
+                 amplitude=1.0, frequencies=None, device=None, stream=None):
+        if scaling not in _SCALINGS:
+            raise ValueError(f"scaling must be one of {sorted(_SCALINGS)}, got {scaling!r}")
+        if dim <= 0 or dim % 2:
+            raise ValueError(f"dim must be positive and even, got {dim}")
+        if not math.isfinite(amplitude):
+            raise ValueError(f"amplitude must be finite, got {amplitude}")
+        turns = (ctypes.c_uint64 * (dim // 2))()
+        if frequencies is None:
+            desc = RopeScaling(ctypes.sizeof(RopeScaling), dim, _SCALINGS[scaling], context, base, factor, low, high)
+            _check(load().qnn_rope_turns(ctypes.byref(desc), turns), "qnn_rope_turns")
+        else:
+            frequencies = [float(f) for f in frequencies]
+            if len(frequencies) != dim // 2 or not all(math.isfinite(f) for f in frequencies):
+                raise ValueError(f"frequencies must be {dim // 2} finite numbers")
+            for i, f in enumerate(frequencies):
+                turns[i] = int(f / math.tau % 1.0 * 2.0 ** 64) % (1 << 64)
+        self.dim, self.interleaved, self.amplitude = dim, int(bool(interleaved)), float(amplitude)
+        host = torch.frombuffer(bytearray(turns), dtype=torch.int64)
+        self.turns = _empty((dim // 2,), torch.int64, torch.device("cuda", _current_device()) if device is None else
+                            torch.device(device), stream)
+        self.device = self.turns.device
+        _on_current(self.device, "the rotation")
+        with torch.cuda.stream(torch.cuda.current_stream() if stream is None else stream):
+            self.turns.copy_(host)
+
+
+def rope(x, positions, rotary, *, out=None, stream=None):
+    """x [tokens, heads, head_dim] with the pairs of each head's first rotary.dim elements turned by their token's position
+    (qnn_rope); positions int32 or int64 [tokens], which may be negative.  Tokens and heads may be strided; out may be x."""
+    code = _float_dtype(x, "x")
+    if x.dim() != 3:
+        raise ValueError(f"x must have shape [tokens, heads, head_dim], got {tuple(x.shape)}")
+    dtype, dev, shape = x.dtype, x.device, x.shape
+    px, (ldx, hx) = _heads(x, dtype, "x")
+    t, heads, d = shape
+    if rotary.device != dev:
+        raise ValueError(f"the rotation must be on {dev}")
+    if rotary.dim > d:
+        raise ValueError(f"the rotation takes {rotary.dim} elements of a head, which has {d}")
+    ppos, wide = _positions(positions, t, dev)
+    if out is None:
+        out = _empty(shape, dtype, dev, stream)
+        py, ldy, hy = out.data_ptr(), heads * d, d
+    else:
+        py, (ldy, hy) = _heads(out, dtype, "out", shape, dev)
+    desc = RopeDesc(ctypes.sizeof(RopeDesc), code, heads, d, rotary.dim, rotary.interleaved, wide, rotary.amplitude, t, ldx, hx,
+                    ldy, hy)
+    st = load().qnn_rope(ctypes.byref(desc), rotary.turns.data_ptr(), ppos, px, py, _stream_of(stream, dev))
+    _check(st, "qnn_rope")
+    return out
+
+
+def _attention(cache, batch, heads, causal, window, scale, table, lengths, offsets, pq, qs, pk, pv, out, pout, os, lse, dev, stream):
+    """The call behind PagedCache.attend and cross_attention; qs, os: strides of sequences, tokens and heads."""
+    if window is not None and window <= 0:
+        raise ValueError(f"window must be positive, got {window}")
+    desc = AttentionDesc(ctypes.sizeof(AttentionDesc), heads, int(bool(causal)), window or 0,
+                         1.0 / math.sqrt(cache.head_dim) if scale is None else scale, *qs, *os)
+    lib, c, b, d = load(), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(desc)
+    need = ctypes.c_size_t(0)
+    _check(lib.qnn_attention_workspace_size(c, b, d, ctypes.byref(need)), "qnn_attention_workspace_size")
+    need, pws, handle = need.value, None, _stream_of(stream, dev)
+    if need:
+        ws = _workspace(need, dev, stream)
+        pws = ws.data_ptr()
+    st = lib.qnn_attention(c, b, d, table, lengths, offsets, pq, pk, pv, pout, None if lse is None else lse.data_ptr(), pws,
+                           need, handle)
+    _check(st, "qnn_attention")
+    return out if lse is None else (out, lse)
+
+
+class PagedCache:
+    """Keys and values in pages: k and v [pages, heads, page_size, head_dim], float16 or bfloat16, with contiguous heads and
+    any other strides of 16 bytes (a cache kept as [pages, page_size, heads, head_dim] is given as k.transpose(1, 2)).  The
+    tensors are the caller's, and keep what is appended.
+
+    The sequences of a call are a table int32 [seqs, width] of pages (token j in row j % page_size of page table[s, j //
+    page_size]; an entry outside [0, pages) is no page: nothing is written there, nothing read), lengths int32 [seqs] with
+    the new tokens counted, and offsets int32 [seqs + 1]: sequence s has the rows offsets[s] .. offsets[s + 1] of the call's
+    tensors as its new tokens, the last of them at position lengths[s] - 1.  Without offsets every sequence has as many.
+    Rows in no sequence are left as they were."""
+
+    def __init__(self, k, v):
+        for t, name in ((k, "k"), (v, "v")):
+            if t.dtype not in (torch.float16, torch.bfloat16):
+                raise TypeError(f"{name} must be float16 or bfloat16, got {t.dtype}")
+            if t.dim() != 4:
+                raise ValueError(f"{name} must have shape [pages, heads, page_size, head_dim], got {tuple(t.shape)}")
+        self.k, self.v = k, v
+        self.dtype, self.device = k.dtype, k.device
+        self.pages, self.heads, self.page_size, self.head_dim = k.shape
+        self._k, ks = _heads(k, k.dtype, "k")
+        self._v, vs = _heads(v, k.dtype, "v", k.shape, k.device)
+        self.desc = CacheDesc(ctypes.sizeof(CacheDesc), _DTYPES[k.dtype], self.heads, self.head_dim, self.page_size, self.pages, *ks, *vs)
+
+    def _batch(self, tokens, table, lengths, offsets):
+        dev = self.device
+        _on_current(dev, "the cache")
+        if self.k.requires_grad or self.v.requires_grad:
+            _no_gradient(self.k, "k")
+            _no_gradient(self.v, "v")
+        if table.dim() != 2:
+            raise ValueError(f"table must have shape [seqs, width], got {tuple(table.shape)}")
+        if table.device != dev:
+            raise ValueError(f"table must be on {dev}")
+        if table.dtype is not torch.int32:
+            raise TypeError(f"table must have dtype torch.int32, got {table.dtype}")
+        seqs, width = table.shape
+        ld, step = table.stride()
+        if step != 1 and width > 1:
+            raise ValueError("table must have contiguous rows")
+        plen = _int32(lengths, "lengths", (seqs,), dev)
+        if offsets is None:
+            if tokens % seqs if seqs else tokens:
+                raise ValueError(f"{tokens} tokens do not split evenly over {seqs} sequences; give offsets")
+            poff = None
+        else:
+            poff = _int32(offsets, "offsets", (seqs + 1,), dev)
+        batch = BatchDesc(ctypes.sizeof(BatchDesc), seqs, width, int(poff is not None), tokens, 0 if seqs == 1 else ld)
+        return batch, table.data_ptr(), plen, poff
+
+    def append(self, k, v, table, lengths, offsets=None, *, rotary=None, q=None, positions=None, q_out=None, stream=None):
+        """Writes the new tokens' keys, rotated by `rotary`, and values k, v [tokens, heads, head_dim] to their places
+        (qnn_cache_append), and returns the rotated queries q [tokens, q heads, head_dim] (None without q); q_out may be q.
+        The rotation goes by the tokens' places in their sequences, or by positions (int32 or int64 [tokens]).  A token
+        whose place is not in the cache is not written.  The new tokens' places are different ones."""
+        dtype, dev, d = self.dtype, self.device, self.head_dim
+        tokens = k.shape[0]
+        batch, ptable, plen, poff = self._batch(tokens, table, lengths, offsets)
+        shape = (tokens, self.heads, d)
+        pk, ks = _heads(k, dtype, "k", shape, dev)
+        pv, vs = _heads(v, dtype, "v", shape, dev)
+        heads, pq, pout, qs, os = 0, None, None, (0, 0), (0, 0)
+        if q is not None:
+            if q.dim() != 3:
+                raise ValueError(f"q must have shape [tokens, heads, head_dim], got {tuple(q.shape)}")
+            heads = q.shape[1]
+            shape = (tokens, heads, d)
+            pq, qs = _heads(q, dtype, "q", shape, dev)
+            if q_out is None:
+                # rows that are in no sequence are not written
+                q_out = _empty(shape, dtype, dev, stream)
+                pout, os = q_out.data_ptr(), (heads * d, d)
+            else:
+                pout, os = _heads(q_out, dtype, "q_out", shape, dev)
+        elif q_out is not None:
+            raise ValueError("q_out needs q")
+        dim = interleaved = wide = 0
+        amplitude, pturns, ppos = 1.0, None, None
+        if rotary is not None:
+            if rotary.device != dev:
+                raise ValueError(f"the rotation must be on {dev}")
+            if rotary.dim > d:
+                raise ValueError(f"the rotation takes {rotary.dim} elements of a head, which has {d}")
+            dim, interleaved, amplitude, pturns = rotary.dim, rotary.interleaved, rotary.amplitude, rotary.turns.data_ptr()
+            if positions is not None:
+                ppos, wide = _positions(positions, tokens, dev)
+        elif positions is not None:
+            raise ValueError("positions need a rotation")
+        desc = AppendDesc(ctypes.sizeof(AppendDesc), heads, dim, interleaved, wide, amplitude, *ks, *vs, *qs, *os)
+        st = load().qnn_cache_append(ctypes.byref(self.desc), ctypes.byref(batch), ctypes.byref(desc), ptable, plen, poff, pturns,
+                                     ppos, pk, pv, pq, self._k, self._v, pout, _stream_of(stream, dev))
+        _check(st, "qnn_cache_append")
+        return q_out
+
+    def attend(self, q, table, lengths, offsets=None, *, causal=True, window=None, scale=None, out=None, lse=False, stream=None):
+        """Attention of the new tokens' queries q [tokens, heads, head_dim] over their sequences (qnn_attention): one token a
+        sequence or many, each seeing the tokens up to itself (causal), of these the last `window` if one is given.  Heads
+        are a multiple of the cache's, which neighbouring heads share.  scale: 1 / sqrt(head_dim) by default.  Returns out
+        [tokens, heads, head_dim], zero for a token that sees none, or with lse=True (out, float32 [tokens, heads]): the
+        logarithm of the sum of exponentials."""
+        if q.dim() != 3:
+            raise ValueError(f"q must have shape [tokens, heads, head_dim], got {tuple(q.shape)}")
+        dtype, dev, shape = self.dtype, self.device, q.shape
+        tokens, heads, d = shape
+        batch, ptable, plen, poff = self._batch(tokens, table, lengths, offsets)
+        if d != self.head_dim or heads % self.heads or heads == 0:
+            raise ValueError(f"q must have heads of {self.head_dim} elements, a multiple of {self.heads} of them, got {tuple(shape)}")
+        pq, (ldq, hq) = _heads(q, dtype, "q", None, dev)
+        if out is None:
+            out = _empty(shape, dtype, dev, stream)
+            pout, ldo, ho = out.data_ptr(), heads * d, d
+        else:
+            pout, (ldo, ho) = _heads(out, dtype, "out", shape, dev)
+        each = tokens // batch.seqs if batch.seqs else 0
+        logs = _empty((tokens, heads), torch.float32, dev, stream) if lse else None
+        return _attention(self.desc, batch, heads, causal, window, scale, ptable, plen, poff, pq, (each * ldq, ldq, hq), self._k,
+                          self._v, out, pout, (each * ldo, ldo, ho), logs, dev, stream)
+
+
+def cross_attention(q, k, v, lengths=None, *, scale=None, out=None, lse=False, stream=None):
+    """Attention of q [batch, tokens, heads, head_dim] to the states of an encoder (qnn_attention): k, v [batch, source,
+    key heads, head_dim], float16 or bfloat16, of which lengths int32 [batch] (None: all) count; heads are a multiple of the
+    key heads.  All but the heads may be strided, keys and values by 16 bytes.  Returns out like q, zero where there are no
+    keys, or with lse=True (out, float32 [batch, tokens, heads])."""
+    if q.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        if t.dim() != 4:
+            raise ValueError(f"{name} must have shape [batch, tokens, heads, head_dim], got {tuple(t.shape)}")
+    dtype, dev, shape = q.dtype, q.device, q.shape
+    b, n, heads, d = shape
+    kb, source, kv, kd = k.shape
+    if kb != b or kd != d or kv == 0 or heads == 0 or heads % kv:
+        raise ValueError(f"q {tuple(shape)} and k {tuple(k.shape)} must agree on the batch and the head's elements, with a multiple "
+                         "of k's heads in q")
+    pq, qs = _heads(q, dtype, "q")
+    pk, ks = _heads(k, dtype, "k", None, dev)
+    pv, vs = _heads(v, dtype, "v", k.shape, dev)
+    plen = None if lengths is None else _int32(lengths, "lengths", (b,), dev)
+    if out is None:
+        out = _empty(shape, dtype, dev, stream)
+    pout, os = _heads(out, dtype, "out", shape, dev)
+    cache = CacheDesc(ctypes.sizeof(CacheDesc), _DTYPES[dtype], kv, d, max(source, 1), b, ks[0], ks[2], ks[1], vs[0], vs[2], vs[1])
+    batch = BatchDesc(ctypes.sizeof(BatchDesc), b, int(source > 0), 0, b * n, 0)
+    logs = _empty((b, n, heads), torch.float32, dev, stream) if lse else None
+    return _attention(cache, batch, heads, False, None, scale, None, plen, None, pq, qs, pk, pv, out, pout, os, logs, dev, stream)
 
 
 def selftest_wait_timeout(limit_cycles: int, stream=None):
