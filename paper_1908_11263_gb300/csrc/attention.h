@@ -48,14 +48,16 @@ struct AttnArgs {
     int seqs, width, page_size, each;  // each: queries of every sequence without offsets
     int heads, kv_heads, group, d;
     int causal, window;         // window 0: none
-    int q_vec, out_vec;         // rows of q are 16-byte aligned, rows of out hold aligned pairs
+    int q_vec, out_vec, out_vec8;  // rows of q are 16-byte aligned; rows of out hold aligned pairs; are 16-byte aligned
     int few;                    // rows (queries * group) of a sequence up to which it is the streaming kernel's; the rest is attention_tc's
     float scale;                // of q k, times log2(e)
-    float *part;                // workspace
+    float *part, *tc_part;      // workspaces of attention_rows and attention_tc, or null
 };
 // Blocks of the streaming kernel, and the bytes that the parts of shared rows take.
 int attention_rows_blocks(int d);
 size_t attention_rows_workspace(int d);
 cudaError_t launch_attention_rows(const AttnArgs &a, int dtype, cudaStream_t st);
+size_t attention_tc_workspace(int d);
+cudaError_t launch_attention_tc(const AttnArgs &a, int dtype, cudaStream_t st);  // heads of 128 elements at most
 
 }  // namespace qnn

@@ -1,0 +1,886 @@
+// Attention of many rows on the 5th-generation tensor cores: prompts, chunks of them, cross attention.
+//
+// A tile is 256 rows of a sequence and key head (two halves of 128, the M of an MMA) over the keys that any of them sees, in
+// units of 128.  The tiles' units, one tile after another, are shared evenly between the SMs, so causal, ragged and single
+// long sequences load all of them alike; a tile that several share leaves parts (sum of 2^(z - m) v, m, sum of 2^(z - m))
+// that a second launch joins in order.
+//
+// For each unit and half: S = Q K^T (A and B in shared memory, S in tensor memory); a thread a row takes S to registers,
+// m = max, P = 2^(scale S - m), which replaces S in tensor memory as the A operand of O += P V.  Keys and values lie in
+// shared memory as they come, rows of keys: for Q K^T that is K-major, for P V it is MN-major, so nothing is transposed.
+// m is raised only where the maximum has grown by more than 2^8 (the weights stay below 2^8 then, and any m gives the same
+// quotient), so that O, in tensor memory too, is rarely rescaled.  P is rounded to the element type, off by half a step (2^-8
+// of it for bf16, as the values are); its sum, m and O have 32 bits.
+//
+// Warps: 0-7 softmax and output, a group of four for each half; 8-11 load by cp.async, which takes rows from wherever their
+// pages lie and fills with zeros what the cache does not have (past the length, in no page), whatever lies there; 12 issues
+// the MMAs.  While the tensor cores work for one half, the other's softmax runs.
+#include <type_traits>
+
+#include "attention.cuh"
+
+namespace qnn {
+namespace {
+
+constexpr int kTcThreads = 512, kTcUnit = 128, kTcRows = 256, kLive = 8, kBins = 128;
+constexpr float kRaise = 8.f;  // growth of the maximum (log2) that is left to the weights
+
+template <int D>
+struct TcRing {
+    static constexpr int kStages = D == 64 ? 8 : 5;
+    static constexpr uint32_t kHalf = 128 * 128;                // 128 rows of 64 elements
+    static constexpr uint32_t kTile = kHalf * (D / 64);         // 128 rows of D
+    static constexpr uint32_t kRing = 2 * kTile, kBars = kRing + kStages * kTile;
+    static constexpr uint32_t kSmem = kBars + kLive * 16 + kBins * 8 + 8 * (2 * kStages + 2 + 6 + 1 + kLive) + 16;
+};
+static_assert(TcRing<128>::kSmem <= 227 * 1024, "shared memory");
+
+// ---------------------------------------------------------------- tensor memory
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float *v)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+          "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
+          "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
+          "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float *v)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(
+            taddr),
+        "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
+        "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]),
+        "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]),
+        "f"(v[31])
+        : "memory");
+}
+
+// D (+)= A B^T with A in tensor memory.
+__device__ __forceinline__ void mma_f16_ts_warp(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// 128-byte swizzle, groups of eight rows 1024 bytes apart; `lbo`: bytes between blocks of 64 elements (MN-major operands).
+__device__ __forceinline__ uint64_t swizzled(uint32_t saddr, uint32_t lbo)
+{
+    return static_cast<uint64_t>((saddr >> 4) & 0x3FFFu) | static_cast<uint64_t>(lbo >> 4) << 16 |
+           static_cast<uint64_t>(1024 >> 4) << 32 | static_cast<uint64_t>(1) << 46 | static_cast<uint64_t>(2) << 61;
+}
+
+__device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, int *status)
+{
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return mbar_wait_warp(bar, parity, status);
+}
+
+// (x, y) * (s, s) + (c, c), (x, y) + (u, v)
+__device__ __forceinline__ float2 fma2(float2 x, float2 s, float2 c)
+{
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(*reinterpret_cast<uint64_t *>(&r))
+        : "l"(*reinterpret_cast<const uint64_t *>(&x)), "l"(*reinterpret_cast<const uint64_t *>(&s)),
+          "l"(*reinterpret_cast<const uint64_t *>(&c)));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y)
+{
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(*reinterpret_cast<uint64_t *>(&r))
+        : "l"(*reinterpret_cast<const uint64_t *>(&x)), "l"(*reinterpret_cast<const uint64_t *>(&y)));
+    return r;
+}
+
+// ---------------------------------------------------------------- tiles
+
+// The keys that the rows of a tile see, in units.
+struct TileKeys {
+    int first, units, lo, hi;
+};
+__device__ __forceinline__ int tile_count(const AttnArgs &a, const Sequence &q)
+{
+    const int64_t rows = static_cast<int64_t>(q.n) * a.group;
+    return rows > a.few ? static_cast<int>((rows + kTcRows - 1) / kTcRows) : 0;
+}
+__device__ __forceinline__ TileKeys tile_keys(const AttnArgs &a, const Sequence &q, int rt)
+{
+    const int64_t r0 = static_cast<int64_t>(rt) * kTcRows, last = (r0 + kTcRows - 1) / a.group;
+    TileKeys t;
+    int x, y;
+    keys_of(a, q, static_cast<int>(r0 / a.group), t.lo, x);
+    keys_of(a, q, static_cast<int>(last < q.n - 1 ? last : q.n - 1), y, t.hi);
+    if (x > t.hi) t.hi = x;
+    t.first = t.lo / kTcUnit;
+    t.units = (t.hi + kTcUnit - 1) / kTcUnit - t.first;
+    if (t.units < 1) t.units = 1;
+    return t;
+}
+
+// A place in the order of units.
+struct TcCursor {
+    Sequence q;
+    TileKeys w;
+    int s, rt, h, u, tiles;
+
+    __device__ __forceinline__ void open(const AttnArgs &a)
+    {
+        q = sequence(a, s);
+        tiles = tile_count(a, q);
+    }
+    __device__ __forceinline__ int rows(const AttnArgs &a) const  // of the tile
+    {
+        const int64_t left = static_cast<int64_t>(q.n) * a.group - static_cast<int64_t>(rt) * kTcRows;
+        return left < kTcRows ? static_cast<int>(left) : kTcRows;
+    }
+    __device__ __forceinline__ void next_tile(const AttnArgs &a)
+    {
+        u = 0;
+        if (++h < a.kv_heads) return;
+        h = 0;
+        if (++rt >= tiles) {
+            rt = 0;
+            do {
+                if (++s >= a.seqs) return;
+                open(a);
+            } while (tiles == 0);
+        }
+        w = tile_keys(a, q, rt);
+    }
+};
+
+__device__ __forceinline__ int64_t warp_scan(int64_t v)  // inclusive
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int64_t o = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+// Units of the sequences s0 + lane (those below s1) for one key head; all lanes of a warp.
+__device__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
+{
+    const int lane = threadIdx.x & 31, s = s0 + lane;
+    Sequence q = {0, 0, 0, 0};
+    int tiles = 0;
+    if (s < s1) {
+        q = sequence(a, s);
+        tiles = tile_count(a, q);
+    }
+    int64_t sum = 0;
+    if (tiles <= 4)
+        for (int rt = 0; rt < tiles; ++rt) sum += tile_keys(a, q, rt).units;
+    for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 4); many; many &= many - 1) {
+        const int from = __ffs(many) - 1;
+        Sequence o;
+        o.first = 0;
+        o.n = __shfl_sync(0xffffffffu, q.n, from);
+        o.keys = __shfl_sync(0xffffffffu, q.keys, from);
+        o.at = __shfl_sync(0xffffffffu, q.at, from);
+        const int t = __shfl_sync(0xffffffffu, tiles, from);
+        int64_t part = 0;
+        for (int rt = lane; rt < t; rt += 32) part += tile_keys(a, o, rt).units;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
+        if (lane == from) sum = part;
+    }
+    return sum;
+}
+
+// Where a block's share begins.
+struct Start {
+    int64_t x0, x1, total, u0, u1;  // share; all units; units of the tile with the first
+    int s, rt, h, u;
+};
+
+// Called by all threads: units in bins of sequences, the share, and (first warp) the place of its first unit.
+__device__ void find_start(const AttnArgs &a, int64_t *bins, Start *out)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int chunks = (a.seqs + 31) / 32, per = (chunks + kBins - 1) / kBins, used = (chunks + per - 1) / per;
+    for (int b = warp; b < used; b += kTcThreads / 32) {
+        int64_t sum = 0;
+        for (int c = b * per; c < (b + 1) * per && c < chunks; ++c) sum += sequence_units(a, c * 32, a.seqs);
+        sum = __shfl_sync(0xffffffffu, warp_scan(sum), 31);
+        if (lane == 0) bins[b] = sum * a.kv_heads;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        int64_t mine[kBins / 32], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kBins / 32; ++i) {
+            const int b = lane * (kBins / 32) + i;
+            mine[i] = b < used ? bins[b] : 0;
+            sum += mine[i];
+        }
+        const int64_t end = warp_scan(sum), total = __shfl_sync(0xffffffffu, end, 31);
+        const int64_t x0 = total * blockIdx.x / gridDim.x, x1 = total * (blockIdx.x + 1) / gridDim.x;
+        int64_t before = end - sum;
+        int bin = -1;
+        int64_t at = 0;
+#pragma unroll
+        for (int i = 0; i < kBins / 32; ++i) {
+            if (before <= x0 && x0 < before + mine[i]) {
+                bin = lane * (kBins / 32) + i;
+                at = before;
+            }
+            before += mine[i];
+        }
+        Start st = {x0, x1, total, 0, 0, 0, 0, 0, 0};
+        if (total > 0) {
+            const int who = __ffs(__ballot_sync(0xffffffffu, bin >= 0)) - 1;
+            bin = __shfl_sync(0xffffffffu, bin, who);
+            at = __shfl_sync(0xffffffffu, at, who);
+            // the sequence
+            for (int c = bin * per;; ++c) {
+                const int64_t n = sequence_units(a, c * 32, a.seqs) * a.kv_heads, e = at + warp_scan(n);
+                const uint32_t hit = __ballot_sync(0xffffffffu, e - n <= x0 && x0 < e);
+                if (hit) {
+                    st.s = c * 32 + __ffs(hit) - 1;
+                    at = __shfl_sync(0xffffffffu, e - n, __ffs(hit) - 1);
+                    break;
+                }
+                at = __shfl_sync(0xffffffffu, e, 31);
+                if ((c + 1) * 32 >= a.seqs) break;  // not reached: the bin holds the unit
+            }
+            // the row tile
+            const Sequence q = sequence(a, st.s);
+            const int tiles = tile_count(a, q);
+            for (int r0 = 0; r0 < tiles; r0 += 32) {
+                const int units = r0 + lane < tiles ? tile_keys(a, q, r0 + lane).units : 0;
+                const int64_t n = static_cast<int64_t>(units) * a.kv_heads, e = at + warp_scan(n);
+                const uint32_t hit = __ballot_sync(0xffffffffu, e - n <= x0 && x0 < e);
+                if (hit) {
+                    const int l = __ffs(hit) - 1, each = __shfl_sync(0xffffffffu, units, l);
+                    at = __shfl_sync(0xffffffffu, e - n, l);
+                    st.rt = r0 + l;
+                    st.h = static_cast<int>((x0 - at) / each);
+                    st.u = static_cast<int>(x0 - at - static_cast<int64_t>(st.h) * each);
+                    st.u0 = x0 - st.u;
+                    st.u1 = st.u0 + each;
+                    break;
+                }
+                at = __shfl_sync(0xffffffffu, e, 31);
+            }
+        }
+        if (lane == 0) *out = st;
+    }
+    __syncthreads();
+}
+
+// ---------------------------------------------------------------- parts of shared tiles
+
+struct TcRecord {
+    int64_t u0, u1, total;
+    int s, h, rt, pad;
+};
+struct TcParts {
+    float *sums, *stats;  // [2 * blocks][256][D], [2 * blocks][2][256]: m, then l
+    TcRecord *records;    // [blocks]
+};
+template <int D>
+__device__ __forceinline__ TcParts tc_parts(float *p, int blocks)
+{
+    TcParts s;
+    s.sums = p;
+    s.stats = p + static_cast<int64_t>(2 * blocks) * kTcRows * D;
+    s.records = reinterpret_cast<TcRecord *>(s.stats + 2 * blocks * 2 * kTcRows);
+    return s;
+}
+
+// ---------------------------------------------------------------- the kernel
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnArgs a, int *status)
+{
+    using R = TcRing<D>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint32_t *live = reinterpret_cast<uint32_t *>(smem + R::kBars);  // [kLive][4]: keys of a unit that are in the cache
+    int64_t *bins = reinterpret_cast<int64_t *>(live + kLive * 4);
+    uint64_t *full = reinterpret_cast<uint64_t *>(bins + kBins), *empty = full + R::kStages;
+    uint64_t *q_full = empty + R::kStages, *q_empty = q_full + 1, *s_full = q_empty + 1, *p_full = s_full + 2, *pv_done = p_full + 2;
+    uint64_t *drained = pv_done + 2, *live_full = drained + 1;
+    uint32_t *slot = reinterpret_cast<uint32_t *>(live_full + kLive);
+    __shared__ Start start;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < R::kStages; ++i) {
+            mbar_init(full + i, 4);
+            mbar_init(empty + i, 1);
+        }
+        mbar_init(q_full, 4);
+        mbar_init(q_empty, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(s_full + i, 1);
+            mbar_init(p_full + i, 4);
+            mbar_init(pv_done + i, 1);
+        }
+        mbar_init(drained, 1);
+        for (int i = 0; i < kLive; ++i) mbar_init(live_full + i, 4);
+        fence_mbar_init();
+    }
+    if (warp == 12) {
+        tmem_alloc(slot, 512);
+        tmem_relinquish();
+        tc_fence_before();
+    }
+    pdl_begin();
+    find_start(a, bins, &start);
+    tc_fence_after();
+    const uint32_t tmem = *slot;
+    const TcParts parts = tc_parts<D>(a.tc_part, gridDim.x);
+    if (threadIdx.x == 0 && a.tc_part) {
+        TcRecord &r = parts.records[blockIdx.x];
+        r.u0 = start.u0;
+        r.u1 = start.u1;
+        r.total = start.total;
+        r.s = start.s;
+        r.h = start.h;
+        r.rt = start.rt;
+    }
+    int64_t left = start.x1 - start.x0;
+    TcCursor at;
+    at.s = start.s;
+    at.rt = start.rt;
+    at.h = start.h;
+    at.u = start.u;
+    if (left > 0) {
+        at.open(a);
+        at.w = tile_keys(a, at.q, at.rt);
+    }
+    const int steps = (a.d + 15) / 16, width = steps * 16;  // 16-element steps of a head
+    bool ok = true;
+
+    if (warp < 8) {
+        // ------------------------------------------------ softmax and output: thread a row
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        const int half = warp >> 2;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t s_at = tmem + lanes + half * 128, o_at_ = tmem + lanes + 256 + half * D;
+        uint32_t s_phase = 0, pv_phase = 0;  // parities of the next waits
+        int unit = 0;                        // of the block, for the ring of masks
+        bool whole = at.u == 0;
+        const float2 scale2 = make_float2(a.scale, a.scale);
+        while (left > 0 && ok) {
+            const int rows = at.rows(a), count = static_cast<int>(at.w.units - at.u < left ? at.w.units - at.u : left);
+            const bool last = at.u + count == at.w.units;
+            left -= count;
+            if (rows <= half * 128) {  // nothing in this half
+                unit += count;
+                whole = true;
+                at.next_tile(a);
+                continue;
+            }
+            const int r = half * 128 + (warp & 3) * 32 + lane;
+            const int64_t row = static_cast<int64_t>(at.rt) * kTcRows + r;
+            const int qi = static_cast<int>(row / a.group);
+            int lo = 0, hi = 0, lo_most, hi_least, x;
+            if (r < rows) keys_of(a, at.q, qi, lo, hi);
+            {
+                // keys that every row of the half sees: from the last query's first to the first query's last
+                const int64_t r0 = static_cast<int64_t>(at.rt) * kTcRows + half * 128;
+                const int64_t r1 = static_cast<int64_t>(at.rt) * kTcRows + min(rows, half * 128 + 128) - 1;
+                keys_of(a, at.q, static_cast<int>(r0 / a.group), x, hi_least);
+                keys_of(a, at.q, static_cast<int>(r1 / a.group), lo_most, x);
+            }
+            float m = -INFINITY, l = 0.f;
+            for (int i = 0; i < count; ++i, ++unit) {
+                const int key0 = (at.w.first + at.u + i) * kTcUnit;
+                if (!wait_bar(live_full + unit % kLive, (unit / kLive) & 1, status) || !wait_bar(s_full + half, s_phase, status)) {
+                    ok = false;
+                    break;
+                }
+                s_phase ^= 1;
+                tc_fence_after();
+                float z[128];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, z + 32 * c);
+                tmem_wait_ld();
+                const uint4 there = *reinterpret_cast<const uint4 *>(live + (unit % kLive) * 4);
+                if (!(key0 >= lo_most && key0 + kTcUnit <= hi_least && (there.x & there.y & there.z & there.w) == 0xffffffffu)) {
+                    const uint32_t words[4] = {there.x, there.y, there.z, there.w};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        // bits [lo, hi) of the 32 keys
+                        const int b0 = min(max(lo - key0 - 32 * c, 0), 32), b1 = min(max(hi - key0 - 32 * c, 0), 32);
+                        const uint32_t below = b1 == 32 ? 0xffffffffu : (1u << b1) - 1, under = b0 == 32 ? 0xffffffffu : (1u << b0) - 1;
+                        const uint32_t seen = words[c] & below & ~under;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(seen >> e & 1)) z[32 * c + e] = -INFINITY;
+                    }
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int e = 0; e < 128; e += 8)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], fmaxf(z[e + 2 * c], z[e + 2 * c + 1]));
+                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale;
+                if (i == 0) {
+                    m = most;
+                } else if (__any_sync(0xffffffffu, most > m + kRaise)) {
+                    // S was computed after the last P V ended: O is at rest
+                    const float raised = fmaxf(m, most), factor = raised == -INFINITY ? 1.f : exp2_fast(m - raised);
+                    m = raised;
+                    l *= factor;
+                    for (int c = 0; c < D; c += 32) {
+                        float o[32];
+                        if (c >= width) break;
+                        tmem_ld32(o_at_ + c, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] *= factor;
+                        tmem_st32(o_at_ + c, o);
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.f : -m;
+                const float2 ref2 = make_float2(ref, ref);
+                float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float p[32];  // pairs of weights
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float2 v0 = fma2(make_float2(z[64 * c + 2 * e], z[64 * c + 2 * e + 1]), scale2, ref2);
+                        float2 v1 = fma2(make_float2(z[64 * c + 2 * e + 2], z[64 * c + 2 * e + 3]), scale2, ref2);
+                        v0 = make_float2(exp2_fast(v0.x), exp2_fast(v0.y));
+                        v1 = make_float2(exp2_fast(v1.x), exp2_fast(v1.y));
+                        sum0 = add2(sum0, v0);
+                        sum1 = add2(sum1, v1);
+                        p[e] = __uint_as_float(pack2<T>(v0.x, v0.y));
+                        p[e + 1] = __uint_as_float(pack2<T>(v1.x, v1.y));
+                    }
+                    tmem_st32(s_at + 32 * c, p);
+                }
+                l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + half);
+                __syncwarp();
+                pv_phase ^= 1;
+            }
+            if (!ok) break;
+            // the last P V of the share
+            if (!wait_bar(pv_done + half, pv_phase ^ 1, status)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const bool complete = whole && last;
+            const int64_t part_row = (2 * blockIdx.x + (whole ? 1 : 0)) * static_cast<int64_t>(kTcRows) + r;
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const int head = at.h * a.group + static_cast<int>(row - static_cast<int64_t>(qi) * a.group);
+            T *y = static_cast<T *>(a.out);
+            if (r < rows) y += o_at(a, at.q, qi, head);
+            float *sums = parts.sums + part_row * D;
+            for (int c = 0; c < D; c += 32) {
+                float o[32];
+                if (c >= a.d) break;
+                tmem_ld32(o_at_ + c, o);
+                tmem_wait_ld();
+                if (r < rows) {
+                    if (complete) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            if (c + e < a.d) {
+                                if (a.out_vec8) {
+                                    *reinterpret_cast<uint4 *>(y + c + e) =
+                                        make_uint4(pack2<T>(o[e] * inv, o[e + 1] * inv), pack2<T>(o[e + 2] * inv, o[e + 3] * inv),
+                                                   pack2<T>(o[e + 4] * inv, o[e + 5] * inv), pack2<T>(o[e + 6] * inv, o[e + 7] * inv));
+                                } else {
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j) y[c + e + j] = from_f32<T>(o[e + j] * inv);
+                                }
+                            }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            *reinterpret_cast<float4 *>(sums + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    }
+                }
+            }
+            if (r < rows) {
+                if (!complete) {
+                    const int64_t base = (2 * blockIdx.x + (whole ? 1 : 0)) * static_cast<int64_t>(2 * kTcRows);
+                    parts.stats[base + r] = m;
+                    parts.stats[base + kTcRows + r] = l;
+                } else if (a.lse) {
+                    a.lse[lse_at(a, at.q, qi, head)] = l > 0.f ? kLn2 * m + logf(l) : -INFINITY;
+                }
+            }
+            tc_fence_before();  // O is read before the next tile's first P, after which it is written again
+            whole = true;
+            at.next_tile(a);
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp < 12) {
+            // ------------------------------------------------ loads: each warp 32 keys of a unit
+            const int quarter = warp - 8, chunks = width / 8;
+            constexpr int kChunks = D / 8, kPass = 32 / kChunks;  // 16-byte chunks of a row, rows a pass
+            const int chunk = lane % kChunks, sub = lane / kChunks;
+            const uint32_t base = smem_addr(smem);
+            const uint32_t at_chunk = (chunk >> 3) * R::kHalf;
+            int st = 0, told = 0, unit = 0;  // stage to fill, stage to announce next
+            uint32_t phase = 0, q_phase = 0;
+            int pending = 0, q_after = 0;    // stages filled but not announced; q came with the one of this number
+            auto announce = [&]() {  // the oldest, which has arrived
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(full + told);
+                    if (q_after == 1) mbar_arrive(q_full);
+                }
+                if (q_after > 0) --q_after;
+                if (++told == R::kStages) told = 0;
+                --pending;
+            };
+            auto flush = [&]() {
+                copy_wait<0>();
+                while (pending > 0) announce();
+            };
+            auto push = [&](bool with_q) {  // the stage is filled
+                copy_commit();
+                if (++st == R::kStages) {
+                    st = 0;
+                    phase ^= 1;
+                }
+                ++pending;
+                if (with_q) q_after = pending;
+                if (pending > 2) {
+                    copy_wait<2>();
+                    announce();
+                }
+            };
+            int page = -1, row = 0;
+            auto find = [&](int u) {
+                const int key = (at.w.first + u) * kTcUnit + quarter * 32 + lane;
+                page = -1;
+                if (key >= at.w.lo && key < at.w.hi) {
+                    const int column = key / a.page_size;
+                    row = key - column * a.page_size;
+                    page = page_of(a, at.s, column);
+                }
+            };
+            auto claim = [&]() {  // the next stage is free
+                if (!__all_sync(0xffffffffu, mbar_try_wait(empty + st, phase ^ 1))) {
+                    flush();
+                    if (!mbar_wait_warp(empty + st, phase ^ 1, status)) ok = false;
+                }
+            };
+            auto fill = [&](const void *from, int64_t place) {  // a row's offset for each lane, -1: zeros
+                const uint32_t to = base + R::kRing + st * R::kTile + at_chunk;
+                const T *p = static_cast<const T *>(from);
+#pragma unroll 4
+                for (int i = 0; i < 32 / kPass; ++i) {
+                    const int rr = i * kPass + sub;
+                    const int64_t off = __shfl_sync(0xffffffffu, place, rr);
+                    const bool there = off >= 0 && chunk * 8 < a.d;
+                    const int key = quarter * 32 + rr;
+                    if (chunk < chunks)
+                        copy16(to + key * 128 + (((chunk & 7) ^ (key & 7)) * 16), there ? p + off + chunk * 8 : p, there ? 16 : 0);
+                }
+            };
+            while (left > 0 && ok) {
+                const int rows = at.rows(a), count = static_cast<int>(at.w.units - at.u < left ? at.w.units - at.u : left);
+                left -= count;
+                find(at.u);
+                for (int i = 0; i < count && ok; ++i, ++unit) {
+                    const int64_t pk = page < 0 ? -1 : page * a.k_page + at.h * a.k_head + row * a.k_row;
+                    const int64_t pv = page < 0 ? -1 : page * a.v_page + at.h * a.v_head + row * a.v_row;
+                    const uint32_t live_keys = __ballot_sync(0xffffffffu, page >= 0);
+                    if (i + 1 < count) find(at.u + i + 1);
+                    claim();
+                    if (!ok) break;
+                    // the ring's stages free the mask's place long before: see kLive
+                    if (lane == 0) {
+                        live[(unit % kLive) * 4 + quarter] = live_keys;
+                        mbar_arrive(live_full + unit % kLive);
+                    }
+                    __syncwarp();
+                    fill(a.k, pk);
+                    if (i == 0) {  // the tile's rows of q
+                        if (!__all_sync(0xffffffffu, mbar_try_wait(q_empty, q_phase ^ 1))) {
+                            flush();
+                            if (!mbar_wait_warp(q_empty, q_phase ^ 1, status)) {
+                                ok = false;
+                                break;
+                            }
+                        }
+                        q_phase ^= 1;
+                        const T *q = static_cast<const T *>(a.q);
+                        const int need = rows > 128 ? 256 : 128;
+                        for (int r0 = quarter * kPass; r0 < need; r0 += 4 * kPass) {
+                            const int r = r0 + sub;
+                            const int64_t rr = static_cast<int64_t>(at.rt) * kTcRows + r;
+                            const bool there = r < rows && chunk * 8 < a.d;
+                            const T *p = q;
+                            if (there) {
+                                const int qi = static_cast<int>(rr / a.group);
+                                p += q_at(a, at.q, qi, at.h * a.group + static_cast<int>(rr - static_cast<int64_t>(qi) * a.group)) + chunk * 8;
+                            }
+                            if (chunk >= chunks) continue;
+                            const uint32_t off = (r >> 7) * R::kTile + at_chunk + (r & 127) * 128 + (((chunk & 7) ^ (r & 7)) * 16);
+                            if (a.q_vec || !there) {
+                                copy16(base + off, p, there ? 16 : 0);
+                            } else {
+                                const uint16_t *e = reinterpret_cast<const uint16_t *>(p);
+                                *reinterpret_cast<uint4 *>(smem + off) =
+                                    make_uint4(e[0] | static_cast<uint32_t>(e[1]) << 16, e[2] | static_cast<uint32_t>(e[3]) << 16,
+                                               e[4] | static_cast<uint32_t>(e[5]) << 16, e[6] | static_cast<uint32_t>(e[7]) << 16);
+                            }
+                        }
+                    }
+                    push(i == 0);
+                    claim();
+                    if (!ok) break;
+                    fill(a.v, pv);
+                    push(false);
+                }
+                at.next_tile(a);
+            }
+            if (ok) flush();
+            copy_wait<0>();
+        } else if (warp == 12) {
+            // ------------------------------------------------ MMAs
+            constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            const uint32_t types = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (8u << 24);
+            const uint32_t qk = types | (static_cast<uint32_t>(kTcUnit >> 3) << 17);
+            const uint32_t pv = types | (1u << 16) | (static_cast<uint32_t>(width >> 3) << 17);  // values: MN-major
+            const uint32_t base = smem_addr(smem);
+            int st = 0;
+            uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, pv_phase[2] = {0, 0};
+            auto wait_stage = [&]() {
+                if (!wait_bar(full + st, phase, status)) ok = false;
+                tc_fence_after();
+            };
+            auto advance = [&]() {
+                if (++st == R::kStages) {
+                    st = 0;
+                    phase ^= 1;
+                }
+            };
+            auto scores = [&](int half, int stage) {
+                const uint32_t q = base + half * R::kTile, k = base + R::kRing + stage * R::kTile;
+                for (int i = 0; i < steps; ++i) {
+                    const uint32_t off = (i >> 2) * R::kHalf + (i & 3) * 32;
+                    mma_f16_ss_warp(tmem + half * 128, swizzled(q + off, 16), swizzled(k + off, 16), qk, i > 0);
+                }
+                mma_commit_warp(s_full + half);
+            };
+            auto weigh = [&](int half, int stage, bool add) {
+                const uint32_t v = base + R::kRing + stage * R::kTile;
+                for (int i = 0; i < kTcUnit / 16; ++i)
+                    mma_f16_ts_warp(tmem + 256 + half * D, tmem + half * 128 + i * 8, swizzled(v + i * 2048, R::kHalf), pv, add || i > 0);
+                mma_commit_warp(pv_done + half);
+            };
+            auto wait_weights = [&](int half) {
+                if (!wait_bar(p_full + half, p_phase[half], status)) ok = false;
+                p_phase[half] ^= 1;
+                tc_fence_after();
+            };
+            auto wait_sum = [&](int half) {  // P, in the place of S, has been read
+                if (!wait_bar(pv_done + half, pv_phase[half], status)) ok = false;
+                pv_phase[half] ^= 1;
+                tc_fence_after();
+            };
+            while (left > 0 && ok) {
+                const bool two = at.rows(a) > 128;
+                const int count = static_cast<int>(at.w.units - at.u < left ? at.w.units - at.u : left);
+                left -= count;
+                if (!wait_bar(q_full, q_phase, status)) ok = false;
+                q_phase ^= 1;
+                if (!ok) break;
+                wait_stage();
+                if (!ok) break;
+                scores(0, st);
+                if (two) scores(1, st);
+                mma_commit_warp(empty + st);
+                if (count == 1) mma_commit_warp(q_empty);
+                advance();
+                for (int i = 0; i < count; ++i) {
+                    const int v = st;
+                    wait_stage();
+                    if (!ok) break;
+                    advance();
+                    const int k = st;
+                    const bool more = i + 1 < count;
+                    wait_weights(0);
+                    if (!ok) break;
+                    weigh(0, v, i > 0);
+                    if (more) wait_stage();
+                    wait_sum(0);
+                    if (!ok) break;
+                    if (more) scores(0, k);
+                    if (two) {
+                        wait_weights(1);
+                        if (!ok) break;
+                        weigh(1, v, i > 0);
+                    }
+                    mma_commit_warp(empty + v);
+                    if (two) {
+                        wait_sum(1);
+                        if (!ok) break;
+                        if (more) scores(1, k);
+                    }
+                    if (more) {
+                        mma_commit_warp(empty + k);
+                        if (i + 2 == count) mma_commit_warp(q_empty);
+                        advance();
+                    }
+                }
+                at.next_tile(a);
+            }
+            // whatever was issued has ended before the tensor memory is given back
+            mma_commit_warp(drained);
+            wait_bar(drained, 0, status);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 12) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Joins a tile that several blocks share, as the streaming kernel's parts are: blocks of row (b, 8 rows) do where b is the
+// first block whose share begins inside the tile.  Few parts: a warp a row; many: all warps share a row's parts.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const int blocks)
+{
+    constexpr int kVec = D / 32;
+    __shared__ float part_max[8], part_sum[8], part_o[8][D];
+    const int b = blockIdx.x + 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    pdl_begin();
+    const TcParts space = tc_parts<D>(a.tc_part, blocks);
+    const TcRecord rec = space.records[b];
+    if (rec.total == 0) return;
+    auto begin = [&](int c) { return rec.total * c / blocks; };
+    if (begin(b) <= rec.u0 || begin(b) >= rec.u1 || begin(b - 1) > rec.u0) return;
+    const Sequence q = sequence(a, rec.s);
+    const int64_t row0 = static_cast<int64_t>(rec.rt) * kTcRows, left = static_cast<int64_t>(q.n) * a.group - row0;
+    const int r0 = blockIdx.y * 8, rows = left < r0 + 8 ? static_cast<int>(left) - r0 : 8;
+    if (rows <= 0) return;
+    const int c0 = b - 1, end = static_cast<int>((rec.u1 * blocks + rec.total - 1) / rec.total);
+    auto none = [&](int c) { return rec.total < blocks && begin(c + 1) <= begin(c); };
+    auto slot_of = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
+    auto stat = [&](int c, int r) { return space.stats + slot_of(c) * static_cast<int64_t>(2 * kTcRows) + r; };
+    auto finish = [&](int r, float most, float sum, const float *o) {  // o: columns lane + 32 i
+        const int64_t row = row0 + r;
+        const int qi = static_cast<int>(row / a.group), head = rec.h * a.group + static_cast<int>(row - static_cast<int64_t>(qi) * a.group);
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (lane + 32 * i < a.d) y[lane + 32 * i] = from_f32<T>(o[i] * inv);
+        if (a.lse && lane == 0) a.lse[lse_at(a, q, qi, head)] = sum > 0.f ? kLn2 * most + logf(sum) : -INFINITY;
+    };
+    auto gather = [&](int r, int c_from, int step, float ref, float &sum, float (&o)[kVec]) {
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) o[i] = 0.f;
+#pragma unroll 4
+        for (int c = c_from; c < end; c += step) {
+            if (none(c)) continue;
+            const float w = exp2_fast(*stat(c, r) - ref);
+            sum += w * stat(c, r)[kTcRows];
+            const float *p = space.sums + (slot_of(c) * static_cast<int64_t>(kTcRows) + r) * D + lane;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if (lane + 32 * i < a.d) o[i] += w * p[32 * i];
+        }
+    };
+    if (end - c0 <= 8) {
+        const int r = r0 + warp;
+        if (warp >= rows) return;
+        float most = -INFINITY, sum, o[kVec];
+        for (int c = c0; c < end; ++c)
+            if (!none(c)) most = fmaxf(most, *stat(c, r));
+        gather(r, c0, 1, most == -INFINITY ? 0.f : most, sum, o);
+        finish(r, most, sum, o);
+        return;
+    }
+    for (int r = r0; r < r0 + rows; ++r) {
+        float most = -INFINITY, sum, o[kVec];
+        for (int c = c0 + threadIdx.x; c < end; c += 256)
+            if (!none(c)) most = fmaxf(most, *stat(c, r));
+#pragma unroll
+        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        if (lane == 0) part_max[warp] = most;
+        __syncthreads();
+        for (int w = 0; w < 8; ++w) most = fmaxf(most, part_max[w]);
+        gather(r, c0 + warp, 8, most == -INFINITY ? 0.f : most, sum, o);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) part_o[warp][lane + 32 * i] = o[i];
+        if (lane == 0) part_sum[warp] = sum;
+        __syncthreads();
+        if (warp == 0) {
+            sum = 0.f;
+            for (int w = 0; w < 8; ++w) sum += part_sum[w];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                o[i] = 0.f;
+                for (int w = 0; w < 8; ++w) o[i] += part_o[w][lane + 32 * i];
+            }
+            finish(r, most, sum, o);
+        }
+        __syncthreads();
+    }
+}
+
+int padded(int d) { return d <= 64 ? 64 : 128; }
+
+template <typename T, int D>
+cudaError_t launch(const AttnArgs &a, cudaStream_t st)
+{
+    using R = TcRing<D>;
+    int *status = device_status_ptr();
+    if (!status) return cudaErrorNotSupported;
+    cudaError_t e = raise_smem<attention_tc_kernel<T, D>>(R::kSmem);
+    if (e != cudaSuccess) return e;
+    const int blocks = device_sm_count();
+    e = launch_pdl(attention_tc_kernel<T, D>, dim3(blocks), kTcThreads, R::kSmem, st, 1, a, status);
+    // nothing is shared where every tile is one unit
+    if (e != cudaSuccess || blocks < 2 || static_cast<int64_t>(a.width) * a.page_size <= kTcUnit) return e;
+    const int64_t rows = (a.offsets ? a.t : a.each) * static_cast<int64_t>(a.group);
+    return launch_pdl(join_tc_kernel<T, D>, dim3(blocks - 1, static_cast<unsigned>(rows < kTcRows ? (rows + 7) / 8 : kTcRows / 8)), 256, 0, st,
+                      1, a, blocks);
+}
+
+}  // namespace
+
+size_t attention_tc_workspace(int d)
+{
+    const size_t blocks = device_sm_count();
+    return 2 * blocks * kTcRows * (padded(d) + 2) * sizeof(float) + blocks * sizeof(TcRecord);
+}
+
+cudaError_t launch_attention_tc(const AttnArgs &a, int dtype, cudaStream_t st)
+{
+    if (a.t == 0 || a.seqs == 0) return cudaSuccess;
+    if (a.d <= 64) return dtype == QNN_F16 ? launch<__half, 64>(a, st) : launch<__nv_bfloat16, 64>(a, st);
+    return dtype == QNN_F16 ? launch<__half, 128>(a, st) : launch<__nv_bfloat16, 128>(a, st);
+}
+
+}  // namespace qnn

@@ -87,10 +87,28 @@ qnn_status check_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, con
     return st;
 }
 
-size_t workspace_of(const qnn_cache_desc &c, const qnn_batch_desc &b, const qnn_attention_desc &)
+// Rows (queries times the heads that share a key head) of a sequence up to which the streaming kernel takes it, and which
+// kernels a call may need: without offsets all sequences have as many rows, with them the kernels find out.
+constexpr int kFewRows = 16;
+struct Kernels {
+    bool rows, tc;
+    int few;
+    size_t rows_bytes, tc_bytes;  // workspaces
+};
+Kernels kernels_of(const qnn_cache_desc &c, const qnn_batch_desc &b, const qnn_attention_desc &d)
 {
-    if (b.t == 0 || static_cast<int64_t>(b.width) * c.page_size <= 64) return 0;
-    return attention_rows_workspace(c.head_dim);
+    Kernels k = {true, false, 0x7fffffff, 0, 0};
+    if (b.t == 0 || b.seqs == 0) return k;
+    const int64_t most = (b.ragged ? b.t : b.t / b.seqs) * (d.heads / c.kv_heads);
+    if (c.head_dim <= 128) {
+        k.few = kFewRows;
+        k.tc = most > kFewRows;
+        k.rows = b.ragged || !k.tc;
+    }
+    const int64_t room = static_cast<int64_t>(b.width) * c.page_size;
+    if (k.rows && room > 64) k.rows_bytes = (attention_rows_workspace(c.head_dim) + 255) / 256 * 256;
+    if (k.tc && room > 128) k.tc_bytes = attention_tc_workspace(c.head_dim);
+    return k;
 }
 
 }  // namespace
@@ -198,7 +216,8 @@ qnn_status qnn_attention_workspace_size(const qnn_cache_desc *c, const qnn_batch
     if (!bytes) return QNN_EINVAL;
     const qnn_status st = check_attention(c, b, d);
     if (st != QNN_OK) return st;
-    *bytes = workspace_of(*c, *b, *d);
+    const Kernels k = kernels_of(*c, *b, *d);
+    *bytes = k.rows_bytes + k.tc_bytes;
     return QNN_OK;
 }
 
@@ -217,7 +236,8 @@ qnn_status qnn_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, const
     if (!aligned(q, 2) || !aligned(out, 2) || !aligned(lse, 4)) return QNN_EALIGN;
     for (const void *p : {table, lengths, offsets})
         if (!aligned(p, 4)) return QNN_EALIGN;
-    const size_t need = workspace_of(*c, *b, *d);
+    const Kernels use = kernels_of(*c, *b, *d);
+    const size_t need = use.rows_bytes + use.tc_bytes;
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return QNN_EWORKSPACE;
     AttnArgs a = {};
     a.q = q; a.k = k_pages; a.v = v_pages; a.out = out; a.lse = lse;
@@ -232,10 +252,15 @@ qnn_status qnn_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, const
     a.causal = d->causal; a.window = d->window;
     a.q_vec = aligned(q, 16) && d->q_seq % 8 == 0 && d->ldq % 8 == 0 && d->hq % 8 == 0;
     a.out_vec = aligned(out, 4) && d->o_seq % 2 == 0 && d->ldo % 2 == 0 && d->ho % 2 == 0;
-    a.few = 0x7fffffff;
+    a.out_vec8 = aligned(out, 16) && d->o_seq % 8 == 0 && d->ldo % 8 == 0 && d->ho % 8 == 0;
+    a.few = use.few;
     a.scale = d->scale * 1.4426950408889634f;
-    a.part = static_cast<float *>(workspace);
-    return from_cuda(launch_attention_rows(a, c->dtype, static_cast<cudaStream_t>(stream)));
+    if (use.rows_bytes) a.part = static_cast<float *>(workspace);
+    if (use.tc_bytes) a.tc_part = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + use.rows_bytes);
+    const cudaStream_t st_ = static_cast<cudaStream_t>(stream);
+    cudaError_t e = use.tc ? launch_attention_tc(a, c->dtype, st_) : cudaSuccess;
+    if (e == cudaSuccess && use.rows) e = launch_attention_rows(a, c->dtype, st_);
+    return from_cuda(e);
 }
 
 }  // extern "C"
