@@ -87,6 +87,12 @@ __device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, int *st
     return mbar_wait_warp(bar, parity, status);
 }
 
+// Arrives on the barrier (whose count includes it) once this thread's copies so far have landed.
+__device__ __forceinline__ void copy_arrive(uint64_t *bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
 // (x, y) * (s, s) + (c, c), (x, y) + (u, v)
 __device__ __forceinline__ float2 fma2(float2 x, float2 s, float2 c)
 {
@@ -114,16 +120,17 @@ struct TileKeys {
 };
 __device__ __forceinline__ int tile_count(const AttnArgs &a, const Sequence &q)
 {
-    const int64_t rows = static_cast<int64_t>(q.n) * a.group;
-    return rows > a.few ? static_cast<int>((rows + kTcRows - 1) / kTcRows) : 0;
+    const int rows = q.n * a.group;  // tokens times heads are below 2^31
+    return rows > a.few ? (rows - 1) / kTcRows + 1 : 0;
 }
 __device__ __forceinline__ TileKeys tile_keys(const AttnArgs &a, const Sequence &q, int rt)
 {
-    const int64_t r0 = static_cast<int64_t>(rt) * kTcRows, last = (r0 + kTcRows - 1) / a.group;
+    const uint32_t r0 = static_cast<uint32_t>(rt) * kTcRows;
+    const int last = static_cast<int>((r0 + kTcRows - 1) / static_cast<uint32_t>(a.group));
     TileKeys t;
     int x, y;
-    keys_of(a, q, static_cast<int>(r0 / a.group), t.lo, x);
-    keys_of(a, q, static_cast<int>(last < q.n - 1 ? last : q.n - 1), y, t.hi);
+    keys_of(a, q, static_cast<int>(r0 / static_cast<uint32_t>(a.group)), t.lo, x);
+    keys_of(a, q, last < q.n - 1 ? last : q.n - 1, y, t.hi);
     if (x > t.hi) t.hi = x;
     t.first = t.lo / kTcUnit;
     t.units = (t.hi + kTcUnit - 1) / kTcUnit - t.first;
@@ -144,8 +151,8 @@ struct TcCursor {
     }
     __device__ __forceinline__ int rows(const AttnArgs &a) const  // of the tile
     {
-        const int64_t left = static_cast<int64_t>(q.n) * a.group - static_cast<int64_t>(rt) * kTcRows;
-        return left < kTcRows ? static_cast<int>(left) : kTcRows;
+        const int left = q.n * a.group - rt * kTcRows;
+        return left < kTcRows ? left : kTcRows;
     }
     __device__ __forceinline__ void next_tile(const AttnArgs &a)
     {
@@ -323,10 +330,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < R::kStages; ++i) {
-            mbar_init(full + i, 4);
+            mbar_init(full + i, 128);
             mbar_init(empty + i, 1);
         }
-        mbar_init(q_full, 4);
+        mbar_init(q_full, 128);
         mbar_init(q_empty, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_full + i, 1);
@@ -390,16 +397,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                 continue;
             }
             const int r = half * 128 + (warp & 3) * 32 + lane;
-            const int64_t row = static_cast<int64_t>(at.rt) * kTcRows + r;
-            const int qi = static_cast<int>(row / a.group);
+            const uint32_t row = at.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
+            const int qi = static_cast<int>(row / group);
             int lo = 0, hi = 0, lo_most, hi_least, x;
             if (r < rows) keys_of(a, at.q, qi, lo, hi);
             {
                 // keys that every row of the half sees: from the last query's first to the first query's last
-                const int64_t r0 = static_cast<int64_t>(at.rt) * kTcRows + half * 128;
-                const int64_t r1 = static_cast<int64_t>(at.rt) * kTcRows + min(rows, half * 128 + 128) - 1;
-                keys_of(a, at.q, static_cast<int>(r0 / a.group), x, hi_least);
-                keys_of(a, at.q, static_cast<int>(r1 / a.group), lo_most, x);
+                const uint32_t r0 = at.rt * static_cast<uint32_t>(kTcRows) + half * 128;
+                const uint32_t r1 = at.rt * static_cast<uint32_t>(kTcRows) + min(rows, half * 128 + 128) - 1;
+                keys_of(a, at.q, static_cast<int>(r0 / group), x, hi_least);
+                keys_of(a, at.q, static_cast<int>(r1 / group), lo_most, x);
             }
             float m = -INFINITY, l = 0.f;
             for (int i = 0; i < count; ++i, ++unit) {
@@ -488,7 +495,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
             const bool complete = whole && last;
             const int64_t part_row = (2 * blockIdx.x + (whole ? 1 : 0)) * static_cast<int64_t>(kTcRows) + r;
             const float inv = l > 0.f ? 1.f / l : 0.f;
-            const int head = at.h * a.group + static_cast<int>(row - static_cast<int64_t>(qi) * a.group);
+            const int head = at.h * a.group + static_cast<int>(row - qi * group);
             T *y = static_cast<T *>(a.out);
             if (r < rows) y += o_at(a, at.q, qi, head);
             float *sums = parts.sums + part_row * D;
@@ -540,37 +547,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
             const int chunk = lane % kChunks, sub = lane / kChunks;
             const uint32_t base = smem_addr(smem);
             const uint32_t at_chunk = (chunk >> 3) * R::kHalf;
-            int st = 0, told = 0, unit = 0;  // stage to fill, stage to announce next
+            int st = 0, unit = 0;
             uint32_t phase = 0, q_phase = 0;
-            int pending = 0, q_after = 0;    // stages filled but not announced; q came with the one of this number
-            auto announce = [&]() {  // the oldest, which has arrived
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(full + told);
-                    if (q_after == 1) mbar_arrive(q_full);
-                }
-                if (q_after > 0) --q_after;
-                if (++told == R::kStages) told = 0;
-                --pending;
-            };
-            auto flush = [&]() {
-                copy_wait<0>();
-                while (pending > 0) announce();
-            };
-            auto push = [&](bool with_q) {  // the stage is filled
-                copy_commit();
-                if (++st == R::kStages) {
-                    st = 0;
-                    phase ^= 1;
-                }
-                ++pending;
-                if (with_q) q_after = pending;
-                if (pending > 2) {
-                    copy_wait<2>();
-                    announce();
-                }
-            };
             int page = -1, row = 0;
             auto find = [&](int u) {
                 const int key = (at.w.first + u) * kTcUnit + quarter * 32 + lane;
@@ -582,10 +560,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                 }
             };
             auto claim = [&]() {  // the next stage is free
-                if (!__all_sync(0xffffffffu, mbar_try_wait(empty + st, phase ^ 1))) {
-                    flush();
-                    if (!mbar_wait_warp(empty + st, phase ^ 1, status)) ok = false;
-                }
+                if (!wait_bar(empty + st, phase ^ 1, status)) ok = false;
             };
             auto fill = [&](const void *from, int64_t place) {  // a row's offset for each lane, -1: zeros
                 const uint32_t to = base + R::kRing + st * R::kTile + at_chunk;
@@ -598,6 +573,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                     const int key = quarter * 32 + rr;
                     if (chunk < chunks)
                         copy16(to + key * 128 + (((chunk & 7) ^ (key & 7)) * 16), there ? p + off + chunk * 8 : p, there ? 16 : 0);
+                }
+                copy_arrive(full + st);
+                if (++st == R::kStages) {
+                    st = 0;
+                    phase ^= 1;
                 }
             };
             while (left > 0 && ok) {
@@ -619,46 +599,52 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                     __syncwarp();
                     fill(a.k, pk);
                     if (i == 0) {  // the tile's rows of q
-                        if (!__all_sync(0xffffffffu, mbar_try_wait(q_empty, q_phase ^ 1))) {
-                            flush();
-                            if (!mbar_wait_warp(q_empty, q_phase ^ 1, status)) {
-                                ok = false;
-                                break;
-                            }
+                        if (!wait_bar(q_empty, q_phase ^ 1, status)) {
+                            ok = false;
+                            break;
                         }
                         q_phase ^= 1;
+                        // the warp's rows of each half: a lane finds one of either, as it does for keys
                         const T *q = static_cast<const T *>(a.q);
-                        const int need = rows > 128 ? 256 : 128;
-                        for (int r0 = quarter * kPass; r0 < need; r0 += 4 * kPass) {
-                            const int r = r0 + sub;
-                            const int64_t rr = static_cast<int64_t>(at.rt) * kTcRows + r;
-                            const bool there = r < rows && chunk * 8 < a.d;
-                            const T *p = q;
-                            if (there) {
-                                const int qi = static_cast<int>(rr / a.group);
-                                p += q_at(a, at.q, qi, at.h * a.group + static_cast<int>(rr - static_cast<int64_t>(qi) * a.group)) + chunk * 8;
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            if (half * 128 >= rows) break;
+                            const int mine = half * 128 + quarter * 32 + lane;
+                            int64_t place = -1;
+                            if (mine < rows) {
+                                const uint32_t row = at.rt * static_cast<uint32_t>(kTcRows) + mine, group = a.group, qi = row / group;
+                                place = q_at(a, at.q, static_cast<int>(qi), at.h * a.group + static_cast<int>(row - qi * group));
                             }
-                            if (chunk >= chunks) continue;
-                            const uint32_t off = (r >> 7) * R::kTile + at_chunk + (r & 127) * 128 + (((chunk & 7) ^ (r & 7)) * 16);
-                            if (a.q_vec || !there) {
-                                copy16(base + off, p, there ? 16 : 0);
-                            } else {
-                                const uint16_t *e = reinterpret_cast<const uint16_t *>(p);
-                                *reinterpret_cast<uint4 *>(smem + off) =
-                                    make_uint4(e[0] | static_cast<uint32_t>(e[1]) << 16, e[2] | static_cast<uint32_t>(e[3]) << 16,
-                                               e[4] | static_cast<uint32_t>(e[5]) << 16, e[6] | static_cast<uint32_t>(e[7]) << 16);
+                            const uint32_t to = half * R::kTile + at_chunk;
+#pragma unroll 4
+                            for (int i = 0; i < 32 / kPass; ++i) {
+                                const int rr = i * kPass + sub, r = quarter * 32 + rr;
+                                const int64_t off = __shfl_sync(0xffffffffu, place, rr);
+                                const bool there = off >= 0 && chunk * 8 < a.d;
+                                const uint32_t dst = to + r * 128 + (((chunk & 7) ^ (r & 7)) * 16);
+                                if (chunk >= chunks) continue;
+                                if (a.q_vec || !there) {
+                                    copy16(base + dst, there ? q + off + chunk * 8 : q, there ? 16 : 0);
+                                } else {
+                                    const uint16_t *e = reinterpret_cast<const uint16_t *>(q + off + chunk * 8);
+                                    *reinterpret_cast<uint4 *>(smem + dst) =
+                                        make_uint4(e[0] | static_cast<uint32_t>(e[1]) << 16, e[2] | static_cast<uint32_t>(e[3]) << 16,
+                                                   e[4] | static_cast<uint32_t>(e[5]) << 16, e[6] | static_cast<uint32_t>(e[7]) << 16);
+                                }
                             }
                         }
+                        __syncwarp();
+                        if (a.q_vec) copy_arrive(q_full);
+                        else mbar_arrive(q_full);
+                        __syncwarp();
                     }
-                    push(i == 0);
                     claim();
                     if (!ok) break;
                     fill(a.v, pv);
-                    push(false);
                 }
                 at.next_tile(a);
             }
-            if (ok) flush();
+            copy_commit();
             copy_wait<0>();
         } else if (warp == 12) {
             // ------------------------------------------------ MMAs
@@ -671,6 +657,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
             uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, pv_phase[2] = {0, 0};
             auto wait_stage = [&]() {
                 if (!wait_bar(full + st, phase, status)) ok = false;
+                fence_proxy_async_smem();  // the copies wrote through the generic proxy
                 tc_fence_after();
             };
             auto advance = [&]() {
@@ -708,6 +695,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                 const int count = static_cast<int>(at.w.units - at.u < left ? at.w.units - at.u : left);
                 left -= count;
                 if (!wait_bar(q_full, q_phase, status)) ok = false;
+                fence_proxy_async_smem();
                 q_phase ^= 1;
                 if (!ok) break;
                 wait_stage();
