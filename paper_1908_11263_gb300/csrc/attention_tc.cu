@@ -13,16 +13,18 @@
 // of it for bf16, as the values are); its sum, m and O have 32 bits.
 //
 // Warps: 0-7 softmax and output, a group of four for each half; 8-11 load by cp.async, which takes rows from wherever their
-// pages lie and fills with zeros what the cache does not have (past the length, in no page), whatever lies there; 12 issues
-// the MMAs.  While the tensor cores work for one half, the other's softmax runs.
+// pages lie and fills with zeros what the cache does not have (past the length, in no page), whatever lies there; 12 and 13
+// issue the MMAs of a half each.  While the tensor cores work for one half, the other's softmax runs.
 #include <type_traits>
 
 #include "attention.cuh"
+#include "tensor_map.h"
 
 namespace qnn {
 namespace {
 
 constexpr int kTcThreads = 512, kTcUnit = 128, kTcRows = 256, kLive = 8, kBins = 128;
+constexpr int kTileCost = 2;       // of a tile beside its units, in units: filling the pipeline, output
 constexpr float kRaise = 8.f;  // growth of the maximum (log2) that is left to the weights
 
 template <int D>
@@ -31,7 +33,10 @@ struct TcRing {
     static constexpr uint32_t kHalf = 128 * 128;                // 128 rows of 64 elements
     static constexpr uint32_t kTile = kHalf * (D / 64);         // 128 rows of D
     static constexpr uint32_t kRing = 2 * kTile, kBars = kRing + kStages * kTile;
-    static constexpr uint32_t kSmem = kBars + kLive * 16 + kBins * 8 + 8 * (2 * kStages + 2 + 6 + 1 + kLive) + 16;
+    static constexpr uint32_t kSmem = kBars + kLive * 16 + kBins * 8 + 8 * (2 * kStages + 4 + 10 + 2 + kLive) + 16;
+    // P beside S where tensor memory has room: the next scores then need not wait until P V has read the weights
+    static constexpr bool kApart = D == 64;
+    static constexpr uint32_t kPAt = kApart ? 256 : 0, kPStep = kApart ? 64 : 128, kOAt = kApart ? 384 : 256;
 };
 static_assert(TcRing<128>::kSmem <= 227 * 1024, "shared memory");
 
@@ -93,6 +98,24 @@ __device__ __forceinline__ void copy_arrive(uint64_t *bar)
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
+// More bytes to come for the barrier's phase; arrivals for a warp.
+__device__ __forceinline__ void expect_bytes(uint64_t *bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void arrive_warp(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], 32;" ::"r"(smem_addr(bar)) : "memory");
+}
+// Box of a four-dimensional tensor.
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_addr(bar))
+        : "memory");
+}
+
 // (x, y) * (s, s) + (c, c), (x, y) + (u, v)
 __device__ __forceinline__ float2 fma2(float2 x, float2 s, float2 c)
 {
@@ -142,7 +165,7 @@ __device__ __forceinline__ TileKeys tile_keys(const AttnArgs &a, const Sequence 
 struct TcCursor {
     Sequence q;
     TileKeys w;
-    int s, rt, h, u, tiles;
+    int s, rt, h, pos, tiles;  // pos: in the tile's kTileCost + units
 
     __device__ __forceinline__ void open(const AttnArgs &a)
     {
@@ -156,7 +179,7 @@ struct TcCursor {
     }
     __device__ __forceinline__ void next_tile(const AttnArgs &a)
     {
-        u = 0;
+        pos = 0;
         if (++h < a.kv_heads) return;
         h = 0;
         if (++rt >= tiles) {
@@ -170,6 +193,24 @@ struct TcCursor {
     }
 };
 
+// What a share has of the tile it is at: units begin .. begin + count.
+struct Segment {
+    int begin, count;
+    bool whole, last;  // with the first, the last unit
+};
+__device__ __forceinline__ Segment take(const TcCursor &at, int64_t &left)
+{
+    const int room = at.w.units + kTileCost - at.pos, n = static_cast<int>(room < left ? room : left);
+    left -= n;
+    Segment g;
+    g.begin = max(0, at.pos - kTileCost);
+    const int end = max(0, at.pos + n - kTileCost);
+    g.count = end - g.begin;
+    g.whole = g.begin == 0;
+    g.last = end == at.w.units;
+    return g;
+}
+
 __device__ __forceinline__ int64_t warp_scan(int64_t v)  // inclusive
 {
     const int lane = threadIdx.x & 31;
@@ -181,7 +222,7 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v)  // inclusive
     return v;
 }
 
-// Units of the sequences s0 + lane (those below s1) for one key head; all lanes of a warp.
+// Units (with the tiles' own cost) of the sequences s0 + lane (those below s1) for one key head; all lanes of a warp.
 __device__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
 {
     const int lane = threadIdx.x & 31, s = s0 + lane;
@@ -193,7 +234,7 @@ __device__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
     }
     int64_t sum = 0;
     if (tiles <= 4)
-        for (int rt = 0; rt < tiles; ++rt) sum += tile_keys(a, q, rt).units;
+        for (int rt = 0; rt < tiles; ++rt) sum += tile_keys(a, q, rt).units + kTileCost;
     for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 4); many; many &= many - 1) {
         const int from = __ffs(many) - 1;
         Sequence o;
@@ -203,7 +244,7 @@ __device__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
         o.at = __shfl_sync(0xffffffffu, q.at, from);
         const int t = __shfl_sync(0xffffffffu, tiles, from);
         int64_t part = 0;
-        for (int rt = lane; rt < t; rt += 32) part += tile_keys(a, o, rt).units;
+        for (int rt = lane; rt < t; rt += 32) part += tile_keys(a, o, rt).units + kTileCost;
 #pragma unroll
         for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
         if (lane == from) sum = part;
@@ -213,8 +254,8 @@ __device__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
 
 // Where a block's share begins.
 struct Start {
-    int64_t x0, x1, total, u0, u1;  // share; all units; units of the tile with the first
-    int s, rt, h, u;
+    int64_t x0, x1, total, u0, u1;  // share; all units; those of the tile with the first, without the tile's own cost
+    int s, rt, h, pos;
 };
 
 // Called by all threads: units in bins of sequences, the share, and (first warp) the place of its first unit.
@@ -271,7 +312,7 @@ __device__ void find_start(const AttnArgs &a, int64_t *bins, Start *out)
             const Sequence q = sequence(a, st.s);
             const int tiles = tile_count(a, q);
             for (int r0 = 0; r0 < tiles; r0 += 32) {
-                const int units = r0 + lane < tiles ? tile_keys(a, q, r0 + lane).units : 0;
+                const int units = r0 + lane < tiles ? tile_keys(a, q, r0 + lane).units + kTileCost : 0;
                 const int64_t n = static_cast<int64_t>(units) * a.kv_heads, e = at + warp_scan(n);
                 const uint32_t hit = __ballot_sync(0xffffffffu, e - n <= x0 && x0 < e);
                 if (hit) {
@@ -279,9 +320,9 @@ __device__ void find_start(const AttnArgs &a, int64_t *bins, Start *out)
                     at = __shfl_sync(0xffffffffu, e - n, l);
                     st.rt = r0 + l;
                     st.h = static_cast<int>((x0 - at) / each);
-                    st.u = static_cast<int>(x0 - at - static_cast<int64_t>(st.h) * each);
-                    st.u0 = x0 - st.u;
-                    st.u1 = st.u0 + each;
+                    st.pos = static_cast<int>(x0 - at - static_cast<int64_t>(st.h) * each);
+                    st.u0 = x0 - st.pos + kTileCost;
+                    st.u1 = x0 - st.pos + each;
                     break;
                 }
                 at = __shfl_sync(0xffffffffu, e, 31);
@@ -315,32 +356,38 @@ __device__ __forceinline__ TcParts tc_parts(float *p, int blocks)
 // ---------------------------------------------------------------- the kernel
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnArgs a, int *status)
+__global__ void __launch_bounds__(kTcThreads, 1)
+    attention_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                        const __grid_constant__ CUtensorMap v_map, const AttnArgs a, int *status)
 {
     using R = TcRing<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     uint32_t *live = reinterpret_cast<uint32_t *>(smem + R::kBars);  // [kLive][4]: keys of a unit that are in the cache
     int64_t *bins = reinterpret_cast<int64_t *>(live + kLive * 4);
     uint64_t *full = reinterpret_cast<uint64_t *>(bins + kBins), *empty = full + R::kStages;
-    uint64_t *q_full = empty + R::kStages, *q_empty = q_full + 1, *s_full = q_empty + 1, *p_full = s_full + 2, *pv_done = p_full + 2;
-    uint64_t *drained = pv_done + 2, *live_full = drained + 1;
+    uint64_t *q_full = empty + R::kStages, *q_empty = q_full + 2, *s_full = q_empty + 2, *s_read = s_full + 2;
+    uint64_t *p_full = s_read + 2, *pv_done = p_full + 4, *drained = pv_done + 2, *live_full = drained + 2;  // p_full: [half][64 keys]
     uint32_t *slot = reinterpret_cast<uint32_t *>(live_full + kLive);
     __shared__ Start start;
+    __shared__ volatile int lead;  // units whose first weights the first half has
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < R::kStages; ++i) {
             mbar_init(full + i, 128);
-            mbar_init(empty + i, 1);
+            mbar_init(empty + i, 2);
         }
-        mbar_init(q_full, 128);
-        mbar_init(q_empty, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_full + i, 1);
-            mbar_init(p_full + i, 4);
+            mbar_init(s_read + i, 4);
+            mbar_init(p_full + 2 * i, 4);
+            mbar_init(p_full + 2 * i + 1, 4);
             mbar_init(pv_done + i, 1);
+            mbar_init(q_full + i, 128);
+            mbar_init(q_empty + i, 1);
+            mbar_init(drained + i, 1);
         }
-        mbar_init(drained, 1);
+        lead = 0;
         for (int i = 0; i < kLive; ++i) mbar_init(live_full + i, 4);
         fence_mbar_init();
     }
@@ -368,7 +415,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
     at.s = start.s;
     at.rt = start.rt;
     at.h = start.h;
-    at.u = start.u;
+    at.pos = start.pos;
     if (left > 0) {
         at.open(a);
         at.w = tile_keys(a, at.q, at.rt);
@@ -381,18 +428,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
         asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int half = warp >> 2;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem + lanes + half * 128, o_at_ = tmem + lanes + 256 + half * D;
+        const uint32_t s_at = tmem + lanes + half * 128, p_at = tmem + lanes + R::kPAt + half * R::kPStep;
+        const uint32_t o_at_ = tmem + lanes + R::kOAt + half * D;
         uint32_t s_phase = 0, pv_phase = 0;  // parities of the next waits
         int unit = 0;                        // of the block, for the ring of masks
-        bool whole = at.u == 0;
         const float2 scale2 = make_float2(a.scale, a.scale);
         while (left > 0 && ok) {
-            const int rows = at.rows(a), count = static_cast<int>(at.w.units - at.u < left ? at.w.units - at.u : left);
-            const bool last = at.u + count == at.w.units;
-            left -= count;
-            if (rows <= half * 128) {  // nothing in this half
-                unit += count;
-                whole = true;
+            const int rows = at.rows(a);
+            const Segment seg = take(at, left);
+            if (rows <= half * 128 || seg.count == 0) {  // nothing in this half
+                unit += seg.count;
                 at.next_tile(a);
                 continue;
             }
@@ -409,8 +454,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                 keys_of(a, at.q, static_cast<int>(r1 / group), lo_most, x);
             }
             float m = -INFINITY, l = 0.f;
-            for (int i = 0; i < count; ++i, ++unit) {
-                const int key0 = (at.w.first + at.u + i) * kTcUnit;
+            for (int i = 0; i < seg.count; ++i, ++unit) {
+                const int key0 = (at.w.first + seg.begin + i) * kTcUnit;
                 if (!wait_bar(live_full + unit % kLive, (unit / kLive) & 1, status) || !wait_bar(s_full + half, s_phase, status)) {
                     ok = false;
                     break;
@@ -421,6 +466,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, z + 32 * c);
                 tmem_wait_ld();
+                if constexpr (R::kApart) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(s_read + half);
+                    __syncwarp();
+                }
                 const uint4 there = *reinterpret_cast<const uint4 *>(live + (unit % kLive) * 4);
                 if (!(key0 >= lo_most && key0 + kTcUnit <= hi_least && (there.x & there.y & there.z & there.w) == 0xffffffffu)) {
                     const uint32_t words[4] = {there.x, there.y, there.z, there.w};
@@ -441,10 +492,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
 #pragma unroll
                     for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], fmaxf(z[e + 2 * c], z[e + 2 * c + 1]));
                 const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale;
+                if constexpr (R::kApart) {  // the last P V of the tile has read its weights, and O is at rest
+                    if (i > 0) {
+                        if (!wait_bar(pv_done + half, pv_phase ^ 1, status)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                    }
+                }
                 if (i == 0) {
                     m = most;
                 } else if (__any_sync(0xffffffffu, most > m + kRaise)) {
-                    // S was computed after the last P V ended: O is at rest
+                    // where P replaces S, S was computed after the last P V ended
                     const float raised = fmaxf(m, most), factor = raised == -INFINITY ? 1.f : exp2_fast(m - raised);
                     m = raised;
                     l *= factor;
@@ -475,14 +535,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                         p[e] = __uint_as_float(pack2<T>(v0.x, v0.y));
                         p[e + 1] = __uint_as_float(pack2<T>(v1.x, v1.y));
                     }
-                    tmem_st32(s_at + 32 * c, p);
+                    tmem_st32(p_at + 32 * c, p);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full + 2 * half + c);
+                    if (!R::kApart && c == 0 && threadIdx.x == 0) lead = unit + 1;
+                    __syncwarp();
                 }
                 l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_full + half);
-                __syncwarp();
                 pv_phase ^= 1;
             }
             if (!ok) break;
@@ -492,8 +553,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                 break;
             }
             tc_fence_after();
-            const bool complete = whole && last;
-            const int64_t part_row = (2 * blockIdx.x + (whole ? 1 : 0)) * static_cast<int64_t>(kTcRows) + r;
+            const bool complete = seg.whole && seg.last;
+            const int64_t part_row = (2 * blockIdx.x + (seg.whole ? 1 : 0)) * static_cast<int64_t>(kTcRows) + r;
             const float inv = l > 0.f ? 1.f / l : 0.f;
             const int head = at.h * a.group + static_cast<int>(row - qi * group);
             T *y = static_cast<T *>(a.out);
@@ -527,7 +588,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
             }
             if (r < rows) {
                 if (!complete) {
-                    const int64_t base = (2 * blockIdx.x + (whole ? 1 : 0)) * static_cast<int64_t>(2 * kTcRows);
+                    const int64_t base = (2 * blockIdx.x + (seg.whole ? 1 : 0)) * static_cast<int64_t>(2 * kTcRows);
                     parts.stats[base + r] = m;
                     parts.stats[base + kTcRows + r] = l;
                 } else if (a.lse) {
@@ -535,7 +596,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                 }
             }
             tc_fence_before();  // O is read before the next tile's first P, after which it is written again
-            whole = true;
             at.next_tile(a);
         }
     } else {
@@ -547,8 +607,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
             const int chunk = lane % kChunks, sub = lane / kChunks;
             const uint32_t base = smem_addr(smem);
             const uint32_t at_chunk = (chunk >> 3) * R::kHalf;
-            int st = 0, unit = 0;
-            uint32_t phase = 0, q_phase = 0;
+            int st = 0, unit = 0, uses = 0;
+            uint32_t phase = 0, q_phase[2] = {0, 0};
             int page = -1, row = 0;
             auto find = [&](int u) {
                 const int key = (at.w.first + u) * kTcUnit + quarter * 32 + lane;
@@ -562,33 +622,49 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
             auto claim = [&]() {  // the next stage is free
                 if (!wait_bar(empty + st, phase ^ 1, status)) ok = false;
             };
-            auto fill = [&](const void *from, int64_t place) {  // a row's offset for each lane, -1: zeros
-                const uint32_t to = base + R::kRing + st * R::kTile + at_chunk;
-                const T *p = static_cast<const T *>(from);
+            // The warp's keys to the next stage: rows that lie in pages by tiled copies where all 32 are there, else by
+            // cp.async, with zeros for those that are not.
+            auto fill = [&](const void *from, const CUtensorMap &map, bool whole, int pg, int rw, int64_t place) {
+                const uint32_t to = base + R::kRing + st * R::kTile;
+                if (whole) {
+                    const int boxes = 32 / a.box, box = lane % boxes, part = lane / boxes;
+                    const int p = __shfl_sync(0xffffffffu, pg, box * a.box), r = __shfl_sync(0xffffffffu, rw, box * a.box);
+                    if (lane == 0) expect_bytes(full + st, 32 * 128 * (D / 64));
+                    __syncwarp();
+                    if (part < D / 64)
+                        tma_box(to + part * R::kHalf + (quarter * 32 + box * a.box) * 128, &map, part * 64, r, at.h, p, full + st);
+                    if (lane == 0) arrive_warp(full + st);
+                    __syncwarp();
+                } else {
+                    const T *p = static_cast<const T *>(from);
 #pragma unroll 4
-                for (int i = 0; i < 32 / kPass; ++i) {
-                    const int rr = i * kPass + sub;
-                    const int64_t off = __shfl_sync(0xffffffffu, place, rr);
-                    const bool there = off >= 0 && chunk * 8 < a.d;
-                    const int key = quarter * 32 + rr;
-                    if (chunk < chunks)
-                        copy16(to + key * 128 + (((chunk & 7) ^ (key & 7)) * 16), there ? p + off + chunk * 8 : p, there ? 16 : 0);
+                    for (int i = 0; i < 32 / kPass; ++i) {
+                        const int rr = i * kPass + sub;
+                        const int64_t off = __shfl_sync(0xffffffffu, place, rr);
+                        const bool there = off >= 0 && chunk * 8 < a.d;
+                        const int key = quarter * 32 + rr;
+                        if (chunk < chunks)
+                            copy16(to + at_chunk + key * 128 + (((chunk & 7) ^ (key & 7)) * 16), there ? p + off + chunk * 8 : p, there ? 16 : 0);
+                    }
+                    copy_arrive(full + st);
                 }
-                copy_arrive(full + st);
+                ++uses;
                 if (++st == R::kStages) {
                     st = 0;
                     phase ^= 1;
                 }
             };
             while (left > 0 && ok) {
-                const int rows = at.rows(a), count = static_cast<int>(at.w.units - at.u < left ? at.w.units - at.u : left);
-                left -= count;
-                find(at.u);
-                for (int i = 0; i < count && ok; ++i, ++unit) {
+                const int rows = at.rows(a);
+                const Segment seg = take(at, left);
+                if (seg.count > 0) find(seg.begin);
+                for (int i = 0; i < seg.count && ok; ++i, ++unit) {
                     const int64_t pk = page < 0 ? -1 : page * a.k_page + at.h * a.k_head + row * a.k_row;
                     const int64_t pv = page < 0 ? -1 : page * a.v_page + at.h * a.v_head + row * a.v_row;
                     const uint32_t live_keys = __ballot_sync(0xffffffffu, page >= 0);
-                    if (i + 1 < count) find(at.u + i + 1);
+                    const bool whole = a.box && live_keys == 0xffffffffu;
+                    const int pg = page, rw = row;
+                    if (i + 1 < seg.count) find(seg.begin + i + 1);
                     claim();
                     if (!ok) break;
                     // the ring's stages free the mask's place long before: see kLive
@@ -597,28 +673,32 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                         mbar_arrive(live_full + unit % kLive);
                     }
                     __syncwarp();
-                    fill(a.k, pk);
-                    if (i == 0) {  // the tile's rows of q
-                        if (!wait_bar(q_empty, q_phase ^ 1, status)) {
+                    fill(a.k, k_map, whole, pg, rw, pk);
+                    for (int half = 0; i == 0 && half * 128 < rows; ++half) {  // the tile's rows of q
+                        if (!wait_bar(q_empty + half, q_phase[half] ^ 1, status)) {
                             ok = false;
                             break;
                         }
-                        q_phase ^= 1;
-                        // the warp's rows of each half: a lane finds one of either, as it does for keys
-                        const T *q = static_cast<const T *>(a.q);
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            if (half * 128 >= rows) break;
-                            const int mine = half * 128 + quarter * 32 + lane;
-                            int64_t place = -1;
-                            if (mine < rows) {
-                                const uint32_t row = at.rt * static_cast<uint32_t>(kTcRows) + mine, group = a.group, qi = row / group;
-                                place = q_at(a, at.q, static_cast<int>(qi), at.h * a.group + static_cast<int>(row - qi * group));
-                            }
+                        q_phase[half] ^= 1;
+                        const uint32_t mine = at.rt * static_cast<uint32_t>(kTcRows) + half * 128 + quarter * 32 + (a.q_box ? 0 : lane);
+                        const uint32_t group = a.group, qi = mine / group;
+                        const int head = at.h * a.group + static_cast<int>(mine - qi * group);
+                        if (a.q_box) {
+                            if (lane == 0) expect_bytes(q_full + half, 32 * 128 * (D / 64));
+                            __syncwarp();
+                            if (lane < D / 64)
+                                tma_box(base + half * R::kTile + lane * R::kHalf + quarter * 32 * 128, &q_map, lane * 64, head,
+                                        static_cast<int>(a.offsets ? at.q.first + qi : qi), a.offsets ? 0 : static_cast<int>(at.q.first),
+                                        q_full + half);
+                            if (lane == 0) arrive_warp(q_full + half);
+                        } else {
+                            // a lane finds a row, as it does for keys
+                            const T *q = static_cast<const T *>(a.q);
+                            const int64_t place = half * 128 + quarter * 32 + lane < rows ? q_at(a, at.q, static_cast<int>(qi), head) : -1;
                             const uint32_t to = half * R::kTile + at_chunk;
 #pragma unroll 4
-                            for (int i = 0; i < 32 / kPass; ++i) {
-                                const int rr = i * kPass + sub, r = quarter * 32 + rr;
+                            for (int j = 0; j < 32 / kPass; ++j) {
+                                const int rr = j * kPass + sub, r = quarter * 32 + rr;
                                 const int64_t off = __shfl_sync(0xffffffffu, place, rr);
                                 const bool there = off >= 0 && chunk * 8 < a.d;
                                 const uint32_t dst = to + r * 128 + (((chunk & 7) ^ (r & 7)) * 16);
@@ -632,33 +712,53 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                                                    e[4] | static_cast<uint32_t>(e[5]) << 16, e[6] | static_cast<uint32_t>(e[7]) << 16);
                                 }
                             }
+                            __syncwarp();
+                            if (a.q_vec) copy_arrive(q_full + half);
+                            else mbar_arrive(q_full + half);
                         }
                         __syncwarp();
-                        if (a.q_vec) copy_arrive(q_full);
-                        else mbar_arrive(q_full);
-                        __syncwarp();
                     }
+                    if (!ok) break;
                     claim();
                     if (!ok) break;
-                    fill(a.v, pv);
+                    fill(a.v, v_map, whole, pg, rw, pv);
                 }
                 at.next_tile(a);
             }
             copy_commit();
             copy_wait<0>();
-        } else if (warp == 12) {
-            // ------------------------------------------------ MMAs
+            if (!ok) {  // tiled copies still in flight land before the block may end
+                for (int i = 0; i < min(uses, R::kStages); ++i) {
+                    if (--st < 0) {
+                        st = R::kStages - 1;
+                        phase ^= 1;
+                    }
+                    wait_bar(full + st, phase, status);
+                }
+                if (uses > 0) wait_bar(q_full, q_phase[0] ^ 1, status);
+                if (uses > 0) wait_bar(q_full + 1, q_phase[1] ^ 1, status);
+            }
+        } else if (warp < 14) {
+            // ------------------------------------------------ MMAs: a warp a half, so that neither waits for the other's softmax
             constexpr uint32_t kFmt = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            const int half = warp - 12;
             const uint32_t types = (1u << 4) | (kFmt << 7) | (kFmt << 10) | (8u << 24);
             const uint32_t qk = types | (static_cast<uint32_t>(kTcUnit >> 3) << 17);
             const uint32_t pv = types | (1u << 16) | (static_cast<uint32_t>(width >> 3) << 17);  // values: MN-major
-            const uint32_t base = smem_addr(smem);
-            int st = 0;
-            uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, pv_phase[2] = {0, 0};
-            auto wait_stage = [&]() {
-                if (!wait_bar(full + st, phase, status)) ok = false;
-                fence_proxy_async_smem();  // the copies wrote through the generic proxy
+            const uint32_t base = smem_addr(smem), q_base = base + half * R::kTile;
+            const uint32_t s_to = tmem + half * 128, p_from = tmem + R::kPAt + half * R::kPStep, o_to = tmem + R::kOAt + half * D;
+            int st = 0, unit = 0;
+            uint32_t phase = 0, q_phase = 0, unit_phase = 0;  // unit_phase: of this half's next weights
+            bool first = true;  // no product of this half yet
+            auto wait_on = [&](uint64_t *bar, uint32_t parity) {
+                if (!wait_bar(bar, parity, status)) ok = false;
                 tc_fence_after();
+                return ok;
+            };
+            auto wait_copy = [&](uint64_t *bar, uint32_t parity) {
+                const bool there = wait_on(bar, parity);
+                fence_proxy_async_smem();  // cp.async writes through the generic proxy
+                return there;
             };
             auto advance = [&]() {
                 if (++st == R::kStages) {
@@ -666,81 +766,74 @@ __global__ void __launch_bounds__(kTcThreads, 1) attention_tc_kernel(const AttnA
                     phase ^= 1;
                 }
             };
-            auto scores = [&](int half, int stage) {
-                const uint32_t q = base + half * R::kTile, k = base + R::kRing + stage * R::kTile;
+            // S = Q K^T, once what lies in its place has been used: the weights, or within a tile the scores before (a tile's last
+            // weights have been there when the next begins).
+            auto scores = [&](bool within) {
+                if (!wait_copy(full + st, phase)) return false;
+                if (R::kApart) {
+                    if (within && !wait_on(s_read + half, unit_phase)) return false;
+                } else {
+                    if (!first && !wait_on(pv_done + half, unit_phase ^ 1)) return false;
+                }
+                if (!R::kApart && half == 1) {
+                    // Half a turn behind the first half: while the one's products run, the other's softmax does.  Nothing but
+                    // time depends on it.
+                    const long long t0 = clock64();
+                    while (lead <= unit && clock64() - t0 < 20000) {}
+                    __syncwarp();
+                }
+                ++unit;
+                const uint32_t k = base + R::kRing + st * R::kTile;
                 for (int i = 0; i < steps; ++i) {
                     const uint32_t off = (i >> 2) * R::kHalf + (i & 3) * 32;
-                    mma_f16_ss_warp(tmem + half * 128, swizzled(q + off, 16), swizzled(k + off, 16), qk, i > 0);
+                    mma_f16_ss_warp(s_to, swizzled(q_base + off, 16), swizzled(k + off, 16), qk, i > 0);
                 }
                 mma_commit_warp(s_full + half);
-            };
-            auto weigh = [&](int half, int stage, bool add) {
-                const uint32_t v = base + R::kRing + stage * R::kTile;
-                for (int i = 0; i < kTcUnit / 16; ++i)
-                    mma_f16_ts_warp(tmem + 256 + half * D, tmem + half * 128 + i * 8, swizzled(v + i * 2048, R::kHalf), pv, add || i > 0);
-                mma_commit_warp(pv_done + half);
-            };
-            auto wait_weights = [&](int half) {
-                if (!wait_bar(p_full + half, p_phase[half], status)) ok = false;
-                p_phase[half] ^= 1;
-                tc_fence_after();
-            };
-            auto wait_sum = [&](int half) {  // P, in the place of S, has been read
-                if (!wait_bar(pv_done + half, pv_phase[half], status)) ok = false;
-                pv_phase[half] ^= 1;
-                tc_fence_after();
+                mma_commit_warp(empty + st);
+                advance();
+                return true;
             };
             while (left > 0 && ok) {
-                const bool two = at.rows(a) > 128;
-                const int count = static_cast<int>(at.w.units - at.u < left ? at.w.units - at.u : left);
-                left -= count;
-                if (!wait_bar(q_full, q_phase, status)) ok = false;
-                fence_proxy_async_smem();
-                q_phase ^= 1;
-                if (!ok) break;
-                wait_stage();
-                if (!ok) break;
-                scores(0, st);
-                if (two) scores(1, st);
-                mma_commit_warp(empty + st);
-                if (count == 1) mma_commit_warp(q_empty);
-                advance();
-                for (int i = 0; i < count; ++i) {
-                    const int v = st;
-                    wait_stage();
-                    if (!ok) break;
-                    advance();
-                    const int k = st;
-                    const bool more = i + 1 < count;
-                    wait_weights(0);
-                    if (!ok) break;
-                    weigh(0, v, i > 0);
-                    if (more) wait_stage();
-                    wait_sum(0);
-                    if (!ok) break;
-                    if (more) scores(0, k);
-                    if (two) {
-                        wait_weights(1);
-                        if (!ok) break;
-                        weigh(1, v, i > 0);
+                const bool mine = at.rows(a) > half * 128;
+                const Segment seg = take(at, left);
+                if (seg.count > 0 && !mine) {  // no rows: the stages pass by
+                    unit += seg.count;
+                    for (int i = 0; i < 2 * seg.count && wait_copy(full + st, phase); ++i, advance()) {
+                        if (lane == 0) mbar_arrive(empty + st);
+                        __syncwarp();
                     }
-                    mma_commit_warp(empty + v);
-                    if (two) {
-                        wait_sum(1);
-                        if (!ok) break;
-                        if (more) scores(1, k);
-                    }
-                    if (more) {
-                        mma_commit_warp(empty + k);
-                        if (i + 2 == count) mma_commit_warp(q_empty);
+                } else if (seg.count > 0) {
+                    if (!wait_copy(q_full + half, q_phase)) break;
+                    q_phase ^= 1;
+                    if (!scores(false)) break;
+                    first = false;
+                    for (int i = 0; i < seg.count; ++i) {
+                        const bool more = i + 1 < seg.count;
+                        if (!more) mma_commit_warp(q_empty + half);
+                        const int v_stage = st;
+                        const uint32_t v_phase = phase, v = base + R::kRing + v_stage * R::kTile;
                         advance();
+                        if (R::kApart && more && !scores(true)) break;
+                        if (!wait_copy(full + v_stage, v_phase)) break;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            if (!wait_on(p_full + 2 * half + c, unit_phase)) break;
+#pragma unroll
+                            for (int j = 4 * c; j < 4 * c + 4; ++j)
+                                mma_f16_ts_warp(o_to, p_from + j * 8, swizzled(v + j * 2048, R::kHalf), pv, (i | j) > 0);
+                        }
+                        if (!ok) break;
+                        mma_commit_warp(pv_done + half);
+                        mma_commit_warp(empty + v_stage);
+                        unit_phase ^= 1;
+                        if (!R::kApart && more && !scores(true)) break;
                     }
                 }
                 at.next_tile(a);
             }
             // whatever was issued has ended before the tensor memory is given back
-            mma_commit_warp(drained);
-            wait_bar(drained, 0, status);
+            mma_commit_warp(drained + half);
+            wait_bar(drained + half, 0, status);
         }
     }
     __syncwarp();
@@ -839,16 +932,51 @@ __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const in
 
 int padded(int d) { return d <= 64 ? 64 : 128; }
 
+// A map of (elements, y, z, w), boxes of 64 x rows x tall elements; false where none can be made.
+template <typename T>
+bool map_of(CUtensorMap *map, const void *p, const int64_t (&size)[4], const int64_t (&step)[3], int rows, int tall)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode || !p || reinterpret_cast<uintptr_t>(p) % 16) return false;
+    cuuint64_t dims[4], strides[3];
+    for (int i = 0; i < 4; ++i) {
+        if (size[i] <= 0) return false;
+        dims[i] = static_cast<cuuint64_t>(size[i]);
+    }
+    for (int i = 0; i < 3; ++i) {
+        const int64_t bytes = size[i + 1] == 1 ? 16 : step[i] * 2;
+        if (bytes <= 0 || bytes % 16 || bytes >= INT64_C(1) << 40) return false;
+        strides[i] = static_cast<cuuint64_t>(bytes);
+    }
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(rows), static_cast<cuuint32_t>(tall), 1}, unit[4] = {1, 1, 1, 1};
+    return encode(map, std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                  const_cast<void *>(p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int D>
-cudaError_t launch(const AttnArgs &a, cudaStream_t st)
+cudaError_t launch(AttnArgs a, cudaStream_t st)
 {
     using R = TcRing<D>;
     int *status = device_status_ptr();
     if (!status) return cudaErrorNotSupported;
     cudaError_t e = raise_smem<attention_tc_kernel<T, D>>(R::kSmem);
     if (e != cudaSuccess) return e;
+    // Tiled copies take 32 rows of a page, or 16, where pages hold a multiple of that (or a sequence has one page); smaller
+    // ones would take as long to issue as cp.async.
+    CUtensorMap q_map = {}, k_map = {}, v_map = {};
+    a.box = !a.table || a.page_size % 32 == 0 ? 32 : (a.page_size % 16 == 0 ? 16 : 0);
+    const int64_t size[4] = {a.d, a.page_size, a.kv_heads, a.pages};
+    if (a.box && (!map_of<T>(&k_map, a.k, size, {a.k_row, a.k_head, a.k_page}, a.box, 1) ||
+                  !map_of<T>(&v_map, a.v, size, {a.v_row, a.v_head, a.v_page}, a.box, 1)))
+        a.box = 0;
+    // 32 rows of q are whole tokens' heads, or a part of one's
+    a.q_box = 32 % a.group == 0 || a.group % 32 == 0 ? 32 : 0;
+    const int64_t q_size[4] = {a.d, a.heads, a.offsets ? a.t : a.each, a.offsets ? 1 : a.seqs};
+    if (a.q_box && !map_of<T>(&q_map, a.q, q_size, {a.hq, a.ldq, a.q_seq}, a.group < 32 ? a.group : 32, a.group < 32 ? 32 / a.group : 1))
+        a.q_box = 0;
     const int blocks = device_sm_count();
-    e = launch_pdl(attention_tc_kernel<T, D>, dim3(blocks), kTcThreads, R::kSmem, st, 1, a, status);
+    e = launch_pdl(attention_tc_kernel<T, D>, dim3(blocks), kTcThreads, R::kSmem, st, 1, q_map, k_map, v_map, a, status);
     // nothing is shared where every tile is one unit
     if (e != cudaSuccess || blocks < 2 || static_cast<int64_t>(a.width) * a.page_size <= kTcUnit) return e;
     const int64_t rows = (a.offsets ? a.t : a.each) * static_cast<int64_t>(a.group);

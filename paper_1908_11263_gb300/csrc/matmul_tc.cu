@@ -20,13 +20,12 @@
 // INT-4 and 616 INT-2 in a hundred.  Below 500 rows by the weights (64 x 8192 x 8192 16-bit 28 us) and, for small
 // matrices, by its fixed cost of some 10 us.
 // Every wait is bounded (mbar_wait_warp); a wait that gives up ends its role, and the kernel, with the status word set.
-#include <cuda.h>
 
 #include <cmath>
-#include <mutex>
 #include <type_traits>
 
 #include "matmul.cuh"
+#include "tensor_map.h"
 
 namespace qnn {
 namespace {
@@ -551,25 +550,6 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1)
 }
 
 // ---------------------------------------------------------------- host
-
-using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled()
-{
-    static std::mutex mu;
-    static EncodeTiled fn = nullptr;
-    std::lock_guard<std::mutex> lock(mu);
-    if (!fn) {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiled>(p);
-    }
-    return fn;
-}
 
 TcShape shape_of(const MatmulArgs &a, int bits, int nt, int ranks)
 {
