@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     uint64_t *p_full = s_read + 2, *pv_done = p_full + 4, *drained = pv_done + 2, *live_full = drained + 2;  // p_full: [half][64 keys]
     uint32_t *slot = reinterpret_cast<uint32_t *>(live_full + kLive);
     __shared__ Start start;
-    __shared__ volatile int lead;  // units whose first weights the first half has
+    __shared__ volatile int begun[2];  // units whose weights a half has begun with
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             mbar_init(q_empty + i, 1);
             mbar_init(drained + i, 1);
         }
-        lead = 0;
+        begun[0] = begun[1] = 0;
         for (int i = 0; i < kLive; ++i) mbar_init(live_full + i, 4);
         fence_mbar_init();
     }
@@ -438,6 +438,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             const Segment seg = take(at, left);
             if (rows <= half * 128 || seg.count == 0) {  // nothing in this half
                 unit += seg.count;
+                if (!R::kApart && half == 1 && (warp & 3) == 0 && lane == 0) begun[1] = unit;
                 at.next_tile(a);
                 continue;
             }
@@ -462,6 +463,25 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 }
                 s_phase ^= 1;
                 tc_fence_after();
+                const uint4 there = *reinterpret_cast<const uint4 *>(live + (unit % kLive) * 4);
+                if (!(key0 >= lo_most && key0 + kTcUnit <= hi_least && (there.x & there.y & there.z & there.w) == 0xffffffffu)) {
+                    // few units: their scores are masked where they lie
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        // bits [lo, hi) of the 32 keys
+                        const int b0 = min(max(lo - key0 - 32 * c, 0), 32), b1 = min(max(hi - key0 - 32 * c, 0), 32);
+                        const uint32_t below = b1 == 32 ? 0xffffffffu : (1u << b1) - 1, under = b0 == 32 ? 0xffffffffu : (1u << b0) - 1;
+                        const uint32_t seen = live[(unit % kLive) * 4 + c] & below & ~under;
+                        float v[32];
+                        tmem_ld32(s_at + 32 * c, v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(seen >> e & 1)) v[e] = -INFINITY;
+                        tmem_st32(s_at + 32 * c, v);
+                    }
+                    tmem_wait_st();
+                }
                 float z[128];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, z + 32 * c);
@@ -471,20 +491,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     __syncwarp();
                     if (lane == 0) mbar_arrive(s_read + half);
                     __syncwarp();
-                }
-                const uint4 there = *reinterpret_cast<const uint4 *>(live + (unit % kLive) * 4);
-                if (!(key0 >= lo_most && key0 + kTcUnit <= hi_least && (there.x & there.y & there.z & there.w) == 0xffffffffu)) {
-                    const uint32_t words[4] = {there.x, there.y, there.z, there.w};
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        // bits [lo, hi) of the 32 keys
-                        const int b0 = min(max(lo - key0 - 32 * c, 0), 32), b1 = min(max(hi - key0 - 32 * c, 0), 32);
-                        const uint32_t below = b1 == 32 ? 0xffffffffu : (1u << b1) - 1, under = b0 == 32 ? 0xffffffffu : (1u << b0) - 1;
-                        const uint32_t seen = words[c] & below & ~under;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!(seen >> e & 1)) z[32 * c + e] = -INFINITY;
-                    }
                 }
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -518,6 +524,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         tmem_st32(o_at_ + c, o);
                     }
                 }
+                if (!R::kApart && (warp & 3) == 0 && lane == 0) begun[half] = unit + 1;
                 const float ref = m == -INFINITY ? 0.f : -m;
                 const float2 ref2 = make_float2(ref, ref);
                 float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
@@ -540,7 +547,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(p_full + 2 * half + c);
-                    if (!R::kApart && c == 0 && threadIdx.x == 0) lead = unit + 1;
                     __syncwarp();
                 }
                 l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
@@ -567,18 +573,31 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 tmem_wait_ld();
                 if (r < rows) {
                     if (complete) {
+                        uint32_t w[16];
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8)
-                            if (c + e < a.d) {
-                                if (a.out_vec8) {
-                                    *reinterpret_cast<uint4 *>(y + c + e) =
-                                        make_uint4(pack2<T>(o[e] * inv, o[e + 1] * inv), pack2<T>(o[e + 2] * inv, o[e + 3] * inv),
-                                                   pack2<T>(o[e + 4] * inv, o[e + 5] * inv), pack2<T>(o[e + 6] * inv, o[e + 7] * inv));
-                                } else {
+                        for (int e = 0; e < 16; ++e) w[e] = pack2<T>(o[2 * e] * inv, o[2 * e + 1] * inv);
 #pragma unroll
-                                    for (int j = 0; j < 8; ++j) y[c + e + j] = from_f32<T>(o[e + j] * inv);
-                                }
+                        for (int e = 0; e < 16; e += 8) {  // 32 bytes, a whole sector
+                            if (c + 2 * e >= a.d) break;
+                            uint32_t *to = reinterpret_cast<uint32_t *>(y + c) + e;
+                            if (a.out_vec16 && c + 2 * e + 16 <= a.d) {
+                                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[e]), "r"(w[e + 1]),
+                                             "r"(w[e + 2]), "r"(w[e + 3]), "r"(w[e + 4]), "r"(w[e + 5]), "r"(w[e + 6]), "r"(w[e + 7])
+                                             : "memory");
+                            } else {
+                                uint16_t *h = reinterpret_cast<uint16_t *>(to);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    if (c + 2 * (e + j) < a.d) {
+                                        if (a.out_vec) {
+                                            to[j] = w[e + j];
+                                        } else {
+                                            h[2 * j] = static_cast<uint16_t>(w[e + j]);
+                                            h[2 * j + 1] = static_cast<uint16_t>(w[e + j] >> 16);
+                                        }
+                                    }
                             }
+                        }
                     } else {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
@@ -749,7 +768,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             const uint32_t s_to = tmem + half * 128, p_from = tmem + R::kPAt + half * R::kPStep, o_to = tmem + R::kOAt + half * D;
             int st = 0, unit = 0;
             uint32_t phase = 0, q_phase = 0, unit_phase = 0;  // unit_phase: of this half's next weights
-            bool first = true;  // no product of this half yet
+            bool first = true, both = false;  // no product of this half yet; the tile has rows in both
             auto wait_on = [&](uint64_t *bar, uint32_t parity) {
                 if (!wait_bar(bar, parity, status)) ok = false;
                 tc_fence_after();
@@ -768,18 +787,18 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             };
             // S = Q K^T, once what lies in its place has been used: the weights, or within a tile the scores before (a tile's last
             // weights have been there when the next begins).
-            auto scores = [&](bool within) {
-                if (!wait_copy(full + st, phase)) return false;
+            auto scores = [&](bool within, bool there) {
+                if (!there && !wait_copy(full + st, phase)) return false;
                 if (R::kApart) {
                     if (within && !wait_on(s_read + half, unit_phase)) return false;
                 } else {
                     if (!first && !wait_on(pv_done + half, unit_phase ^ 1)) return false;
                 }
-                if (!R::kApart && half == 1) {
-                    // Half a turn behind the first half: while the one's products run, the other's softmax does.  Nothing but
-                    // time depends on it.
+                if (!R::kApart && both) {
+                    // Half a turn apart: while the one half's products run, the other's softmax does.  Nothing but time depends
+                    // on it.
                     const long long t0 = clock64();
-                    while (lead <= unit && clock64() - t0 < 20000) {}
+                    while (begun[half ^ 1] < unit + half && clock64() - t0 < 20000) __nanosleep(20);
                     __syncwarp();
                 }
                 ++unit;
@@ -795,6 +814,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             };
             while (left > 0 && ok) {
                 const bool mine = at.rows(a) > half * 128;
+                both = at.rows(a) > 128;
                 const Segment seg = take(at, left);
                 if (seg.count > 0 && !mine) {  // no rows: the stages pass by
                     unit += seg.count;
@@ -805,7 +825,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 } else if (seg.count > 0) {
                     if (!wait_copy(q_full + half, q_phase)) break;
                     q_phase ^= 1;
-                    if (!scores(false)) break;
+                    if (!scores(false, false)) break;
                     first = false;
                     for (int i = 0; i < seg.count; ++i) {
                         const bool more = i + 1 < seg.count;
@@ -813,8 +833,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         const int v_stage = st;
                         const uint32_t v_phase = phase, v = base + R::kRing + v_stage * R::kTile;
                         advance();
-                        if (R::kApart && more && !scores(true)) break;
+                        if (R::kApart && more && !scores(true, false)) break;
+                        // the copies are there long before the weights; waiting for them after these would cost the fences' time
                         if (!wait_copy(full + v_stage, v_phase)) break;
+                        if (!R::kApart && more && !wait_copy(full + st, phase)) break;
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             if (!wait_on(p_full + 2 * half + c, unit_phase)) break;
@@ -826,7 +848,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         mma_commit_warp(pv_done + half);
                         mma_commit_warp(empty + v_stage);
                         unit_phase ^= 1;
-                        if (!R::kApart && more && !scores(true)) break;
+                        if (!R::kApart && more && !scores(true, true)) break;
                     }
                 }
                 at.next_tile(a);
