@@ -1,14 +1,14 @@
 // Attention of few rows over a cache: keys and values are streamed once, whatever page they lie in.
 //
-// The work is the sequences' keys in units of 64, for every key head (and every 16 rows, where a sequence has more), one
+// The work is the sequences' keys in units of 64 (128 for heads of 64 and less), for every key head (and every 16 rows, where a sequence has more), one
 // after another; every block takes an even share of all units, so short and long sequences mix without idle SMs and one
 // long sequence occupies them all.  Units of one (sequence, key head) that fall to several blocks leave a part each (the
 // sum of 2^(z - m) v, m and the sum of 2^(z - m)) in the workspace, and a second launch joins them in order, so the result
 // does not depend on which block was first.
 //
-// A block is four warps.  Each warp takes 16 of a unit's keys: S = Q K^T on the m16n8k16 MMA with the rows on the M side,
+// A block is four warps.  Each warp takes a quarter of a unit's keys: S = Q K^T on the m16n8k16 MMA with the rows on the M side,
 // the running maximum of all four warps through shared memory; then each warp takes a quarter of the head's columns over
-// all 64 keys, so a block holds one accumulator and not four that had to be added.  Keys and values come by cp.async, 16
+// all keys, so a block holds one accumulator and not four that had to be added.  Keys and values come by cp.async, 16
 // bytes a lane, several units ahead and across the borders of sequences; keys that the cache does not have (past the
 // length, in no page) are filled with zeros, whatever lies there, and masked.  Rows of 128 bytes and more are stored with
 // 16-byte chunk c of row r at c ^ (r & 7): no bank conflicts for ldmatrix.
@@ -20,18 +20,20 @@
 namespace qnn {
 namespace {
 
-constexpr int kRowsThreads = 128, kUnit = 64;
+constexpr int kRowsThreads = 128;
+// Keys of a unit: 32 KB of keys and values for every head size up to 128, so that a unit's barriers weigh alike.
+constexpr int rows_unit(int d) { return d <= 64 ? 128 : 64; }
 
 template <int D>
 struct RowsRing {
-    static constexpr int kStages = D == 64 ? 6 : 3, kPerSm = D == 256 ? 1 : 2;
+    static constexpr int kUnit = rows_unit(D), kStages = 3, kPerSm = D == 256 ? 1 : 2;
     static constexpr uint32_t kRow = D * 2, kTile = kUnit * kRow, kQ = 16 * kRow, kStage = 2 * kTile + kQ;
-    static constexpr uint32_t kP = kStages * kStage, kSmem = kP + 16 * 128;
+    static constexpr uint32_t kP = kStages * kStage, kPRow = kUnit * 2, kSmem = kP + 16 * kPRow;
 };
 
 // Of a block: where its first unit lies.  total 0: nothing was queued.
 struct PartRecord {
-    int64_t u0, u1, total;  // units of the pair that holds the block's first unit; all units
+    int64_t x0, u0, u1, total;  // first unit; units of the pair that holds the block's first unit; all units
     int s, h, rt, pad;
 };
 
@@ -56,6 +58,7 @@ struct SeqUnits {
     int lo, hi;
 };
 
+template <int kUnit>
 __device__ __forceinline__ SeqUnits seq_units(const AttnArgs &a, const Sequence &q)
 {
     SeqUnits u = {0, 0, 0, 0, 0};
@@ -74,6 +77,7 @@ __device__ __forceinline__ SeqUnits seq_units(const AttnArgs &a, const Sequence 
 }
 
 // A place in the order of units.
+template <int kUnit>
 struct Cursor {
     Sequence q;
     SeqUnits w;
@@ -82,7 +86,7 @@ struct Cursor {
     __device__ __forceinline__ void open(const AttnArgs &a)
     {
         q = sequence(a, s);
-        w = seq_units(a, q);
+        w = seq_units<kUnit>(a, q);
     }
     __device__ __forceinline__ void next(const AttnArgs &a)
     {
@@ -103,6 +107,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_rows_kernel(const AttnArgs a)
 {
     using R = RowsRing<D>;
+    constexpr int kUnit = R::kUnit, kKeys = kUnit / 4;  // of a unit, of a warp
     constexpr int kChunks = D / 8, kSteps = D / 16, kCols = D / 4, kBlocks = kCols / 8;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int64_t scratch[kRowsThreads / 32];
@@ -118,7 +123,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
     // all units, and where this block's share begins
     int64_t mine = 0, total = 0;
     for (int s = tid; s < a.seqs; s += kRowsThreads) {
-        const SeqUnits w = seq_units(a, sequence(a, s));
+        const SeqUnits w = seq_units<kUnit>(a, sequence(a, s));
         mine += static_cast<int64_t>(w.units) * w.tiles * a.kv_heads;
     }
     block_scan<kRowsThreads>(mine, scratch, total);
@@ -134,7 +139,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
         const int s = s0 + tid;
         int64_t n = 0, all;
         if (s < a.seqs) {
-            const SeqUnits w = seq_units(a, sequence(a, s));
+            const SeqUnits w = seq_units<kUnit>(a, sequence(a, s));
             n = static_cast<int64_t>(w.units) * w.tiles * a.kv_heads;
         }
         const int64_t before = carry + block_scan<kRowsThreads>(n, scratch, all);
@@ -147,7 +152,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
     }
     __syncthreads();
 
-    Cursor load;
+    Cursor<kUnit> load;
     load.s = start_seq;
     load.open(a);
     {
@@ -158,6 +163,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
         load.h = pair - load.rt * a.kv_heads;
         if (tid == 0 && a.part) {
             PartRecord &r = space.records[blockIdx.x];
+            r.x0 = x0;
             r.u0 = x0 - load.u;
             r.u1 = r.u0 + load.w.units;
             r.total = total;
@@ -166,37 +172,42 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
             r.rt = load.rt;
         }
     }
-    Cursor at = load;
+    Cursor<kUnit> at = load;
     int64_t left = x1 - x0, to_load = left;
 
-    // Lanes 0-15 know where the warp's 16 keys lie, lanes 16-31 where their values do: an offset, -1 for none.
-    int64_t place = -1;
+    // Where the warp's keys and values lie: a lane knows kKeys / 16 of the 32 or 64 offsets (keys, then values); -1 for none.
+    constexpr int kPlaces = kKeys / 16;
+    int64_t place[kPlaces];
     auto find = [&]() {  // of the load cursor's unit
-        const int key = (load.w.first + load.u) * kUnit + warp * 16 + (lane & 15);
-        place = -1;
-        if (key >= load.w.lo && key < load.w.hi) {
-            const int column = key / a.page_size, row = key - column * a.page_size;
-            const int page = page_of(a, load.s, column);
-            if (page >= 0)
-                place = lane < 16 ? page * a.k_page + load.h * a.k_head + row * a.k_row : page * a.v_page + load.h * a.v_head + row * a.v_row;
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i) {
+            const bool of_k = kPlaces == 1 ? lane < 16 : i == 0;
+            const int key = (load.w.first + load.u) * kUnit + warp * kKeys + (kPlaces == 1 ? lane & 15 : lane);
+            place[i] = -1;
+            if (key >= load.w.lo && key < load.w.hi) {
+                const int column = key / a.page_size, row = key - column * a.page_size;
+                const int page = page_of(a, load.s, column);
+                if (page >= 0)
+                    place[i] = of_k ? page * a.k_page + load.h * a.k_head + row * a.k_row : page * a.v_page + load.h * a.v_head + row * a.v_row;
+            }
         }
     };
     bool opened = true;  // the unit to load is the block's first of its pair
     auto fetch = [&](int stage) {
         const uint32_t to = base + stage * R::kStage;
-        const uint32_t live = __ballot_sync(0xffffffffu, place >= 0);
-        if (lane == 0) vmask[stage][warp] = live & 0xffff;
+        const uint32_t live = __ballot_sync(0xffffffffu, place[0] >= 0);
+        if (lane == 0) vmask[stage][warp] = kKeys == 16 ? live & 0xffff : live;
         constexpr int kPass = 32 / (kChunks < 32 ? kChunks : 32);  // rows a pass
         const int chunk = lane % kChunks, sub = lane / kChunks;
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-            for (int i = 0; i < 16 / kPass; ++i) {
+            for (int i = 0; i < kKeys / kPass; ++i) {
                 const int r = i * kPass + sub;
-                const int64_t off = __shfl_sync(0xffffffffu, place, kv * 16 + r);
+                const int64_t off = __shfl_sync(0xffffffffu, place[kPlaces == 1 ? 0 : kv], kPlaces == 1 ? kv * 16 + r : r);
                 const T *p = static_cast<const T *>(kv ? a.v : a.k);
                 const bool ok = off >= 0 && chunk * 8 < a.d;
-                const int row = warp * 16 + r;
+                const int row = warp * kKeys + r;
                 copy16(to + kv * R::kTile + row * R::kRow + ((chunk ^ (row & 7)) * 16), ok ? p + off + chunk * 8 : p, ok ? 16 : 0);
             }
         if (opened) {  // the pair's rows of q, beside its first keys
@@ -271,26 +282,29 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
             keys_of(a, at.q, q0, x, hi_least);
             keys_of(a, at.q, q1, lo_most, y);
         }
-        // scores of this warp's 16 keys
-        const int key0 = (at.w.first + at.u) * kUnit + warp * 16;
-        float z[2][4];
+        // scores of this warp's keys
+        constexpr int kZ = kKeys / 8;
+        const int key0 = (at.w.first + at.u) * kUnit + warp * kKeys;
+        float z[kZ][4];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < kZ; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) z[n][i] = 0.f;
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            uint32_t b[4];
-            const int r = warp * 16 + (lane & 7) + ((lane >> 4) << 3), c = 2 * k + ((lane >> 3) & 1);
-            ldsm4(b, from + r * R::kRow + ((c ^ (r & 7)) * 16));
-            mma16816<T>(z[0], aq[k], b[0], b[1]);
-            mma16816<T>(z[1], aq[k], b[2], b[3]);
-        }
+        for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+            for (int n = 0; n < kZ; n += 2) {
+                uint32_t b[4];
+                const int r = warp * kKeys + n * 8 + (lane & 7) + ((lane >> 4) << 3), c = 2 * k + ((lane >> 3) & 1);
+                ldsm4(b, from + r * R::kRow + ((c ^ (r & 7)) * 16));
+                mma16816<T>(z[n], aq[k], b[0], b[1]);
+                mma16816<T>(z[n + 1], aq[k], b[2], b[3]);
+            }
         const uint32_t live = vmask[stage][warp];
-        const bool clear = live == 0xffff && key0 >= lo_most && key0 + 16 <= hi_least;
+        const bool clear = live == (kKeys == 16 ? 0xffffu : 0xffffffffu) && key0 >= lo_most && key0 + kKeys <= hi_least;
         float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < kZ; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int col = n * 8 + t4 * 2 + (i & 1), key = key0 + col;
@@ -325,13 +339,13 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
         }
         const uint32_t sp = base + R::kP;
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < kZ; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float p0 = exp2_fast(z[n][2 * i] - at_m[i]), p1 = exp2_fast(z[n][2 * i + 1] - at_m[i]);
                 l[i] += p0 + p1;
                 const int r = g + 8 * i;
-                *reinterpret_cast<uint32_t *>(smem + R::kP + r * 128 + (((warp * 2 + n) ^ (r & 7)) * 16) + t4 * 4) = pack2<T>(p0, p1);
+                *reinterpret_cast<uint32_t *>(smem + R::kP + r * R::kPRow + (((warp * kZ + n) ^ (r & 7)) * 16) + t4 * 4) = pack2<T>(p0, p1);
             }
         __syncthreads();
         // this warp's columns over all keys
@@ -339,7 +353,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
         for (int k = 0; k < kUnit / 16; ++k) {
             uint32_t ap[4];
             const int pr = (lane & 7) + ((lane >> 3) & 1) * 8, pc = 2 * k + (lane >> 4);
-            ldsm4(ap, sp + pr * 128 + ((pc ^ (pr & 7)) * 16));
+            ldsm4(ap, sp + pr * R::kPRow + ((pc ^ (pr & 7)) * 16));
             const int r = k * 16 + (lane & 7) + ((lane >> 3) & 1) * 8;
 #pragma unroll
             for (int n = 0; n < kBlocks; n += 2) {
@@ -418,16 +432,16 @@ __global__ void __launch_bounds__(128) join_rows_kernel(const AttnArgs a, const 
     pdl_begin();
     const PartSpace space = part_space<D>(a.part, blocks);
     const PartRecord rec = space.records[b];
-    if (rec.total == 0) return;
-    auto begin = [&](int c) { return rec.total * c / blocks; };
-    if (begin(b) <= rec.u0 || begin(b) >= rec.u1 || begin(b - 1) > rec.u0) return;
+    const int64_t before = space.records[b - 1].x0;
+    if (rec.total == 0 || rec.x0 <= rec.u0 || rec.x0 >= rec.u1 || before > rec.u0) return;
     const Sequence q = sequence(a, rec.s);
     const int row = rec.rt * 16 + r, qi = row / a.group;
     if (qi >= q.n) return;
     const int head = rec.h * a.group + row - qi * a.group;
     // parts of blocks c0 .. end - 1; with fewer units than blocks, those between that have a share
     const int c0 = b - 1, end = static_cast<int>((rec.u1 * blocks + rec.total - 1) / rec.total);
-    auto none = [&](int c) { return rec.total < blocks && begin(c + 1) <= begin(c); };
+    const bool sparse = rec.total < blocks;
+    auto none = [&](int c) { return sparse && rec.total * (c + 1) / blocks <= rec.total * c / blocks; };
     auto slot_of = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
     float most = -INFINITY;
     for (int c = c0 + threadIdx.x; c < end; c += 128)
@@ -475,7 +489,7 @@ cudaError_t launch(const AttnArgs &a, cudaStream_t st)
     if (e != cudaSuccess || blocks < 2) return e;
     // nothing is shared where every pair is one unit
     const int64_t rows = (a.offsets ? a.t : a.each) * static_cast<int64_t>(a.group);
-    if (static_cast<int64_t>(a.width) * a.page_size <= kUnit) return cudaSuccess;
+    if (static_cast<int64_t>(a.width) * a.page_size <= R::kUnit) return cudaSuccess;
     return launch_pdl(join_rows_kernel<T, D>, dim3(blocks - 1, static_cast<unsigned>(rows < 16 ? rows : 16)), 128, 0, st, 1, a, blocks);
 }
 

@@ -336,7 +336,7 @@ __device__ void find_start(const AttnArgs &a, int64_t *bins, Start *out)
 // ---------------------------------------------------------------- parts of shared tiles
 
 struct TcRecord {
-    int64_t u0, u1, total;
+    int64_t x0, u0, u1, total;  // as in Start
     int s, h, rt, pad;
 };
 struct TcParts {
@@ -403,6 +403,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const TcParts parts = tc_parts<D>(a.tc_part, gridDim.x);
     if (threadIdx.x == 0 && a.tc_part) {
         TcRecord &r = parts.records[blockIdx.x];
+        r.x0 = start.x0;
         r.u0 = start.u0;
         r.u1 = start.u1;
         r.total = start.total;
@@ -867,88 +868,72 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     }
 }
 
-// Joins a tile that several blocks share, as the streaming kernel's parts are: blocks of row (b, 8 rows) do where b is the
-// first block whose share begins inside the tile.  Few parts: a warp a row; many: all warps share a row's parts.
+// Joins a tile that several blocks share, as the streaming kernel's parts are: block (b, 32 rows) does where b is the first
+// block whose share begins inside the tile.  A warp a row.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const int blocks)
 {
     constexpr int kVec = D / 32;
-    __shared__ float part_max[8], part_sum[8], part_o[8][D];
     const int b = blockIdx.x + 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_begin();
     const TcParts space = tc_parts<D>(a.tc_part, blocks);
     const TcRecord rec = space.records[b];
-    if (rec.total == 0) return;
-    auto begin = [&](int c) { return rec.total * c / blocks; };
-    if (begin(b) <= rec.u0 || begin(b) >= rec.u1 || begin(b - 1) > rec.u0) return;
+    const int64_t before = space.records[b - 1].x0;
+    if (rec.total == 0 || rec.x0 <= rec.u0 || rec.x0 >= rec.u1 || before > rec.u0) return;
     const Sequence q = sequence(a, rec.s);
-    const int64_t row0 = static_cast<int64_t>(rec.rt) * kTcRows, left = static_cast<int64_t>(q.n) * a.group - row0;
-    const int r0 = blockIdx.y * 8, rows = left < r0 + 8 ? static_cast<int>(left) - r0 : 8;
-    if (rows <= 0) return;
+    const int left = q.n * a.group - rec.rt * kTcRows, rows = left < kTcRows ? left : kTcRows;
+    if (blockIdx.y * 32 >= rows) return;
+    // parts of blocks c0 .. end - 1; with fewer units than blocks, those between that have a share
     const int c0 = b - 1, end = static_cast<int>((rec.u1 * blocks + rec.total - 1) / rec.total);
-    auto none = [&](int c) { return rec.total < blocks && begin(c + 1) <= begin(c); };
+    const bool sparse = rec.total < blocks;
+    auto none = [&](int c) { return sparse && rec.total * (c + 1) / blocks <= rec.total * c / blocks; };
     auto slot_of = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
-    auto stat = [&](int c, int r) { return space.stats + slot_of(c) * static_cast<int64_t>(2 * kTcRows) + r; };
-    auto finish = [&](int r, float most, float sum, const float *o) {  // o: columns lane + 32 i
-        const int64_t row = row0 + r;
-        const int qi = static_cast<int>(row / a.group), head = rec.h * a.group + static_cast<int>(row - static_cast<int64_t>(qi) * a.group);
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head);
+#pragma unroll 1
+    for (int r = blockIdx.y * 32 + warp; r < rows && r < static_cast<int>(blockIdx.y) * 32 + 32; r += 8) {
+        float most = -INFINITY, sum = 0.f, o[kVec];
+        for (int c = c0 + lane; c < end; c += 32)
+            if (!none(c)) most = fmaxf(most, space.stats[slot_of(c) * static_cast<int64_t>(2 * kTcRows) + r]);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i)
-            if (lane + 32 * i < a.d) y[lane + 32 * i] = from_f32<T>(o[i] * inv);
-        if (a.lse && lane == 0) a.lse[lse_at(a, q, qi, head)] = sum > 0.f ? kLn2 * most + logf(sum) : -INFINITY;
-    };
-    auto gather = [&](int r, int c_from, int step, float ref, float &sum, float (&o)[kVec]) {
-        sum = 0.f;
+        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        const float ref = most == -INFINITY ? 0.f : most;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) o[i] = 0.f;
 #pragma unroll 4
-        for (int c = c_from; c < end; c += step) {
+        for (int c = c0; c < end; ++c) {
             if (none(c)) continue;
-            const float w = exp2_fast(*stat(c, r) - ref);
-            sum += w * stat(c, r)[kTcRows];
-            const float *p = space.sums + (slot_of(c) * static_cast<int64_t>(kTcRows) + r) * D + lane;
-#pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                if (lane + 32 * i < a.d) o[i] += w * p[32 * i];
-        }
-    };
-    if (end - c0 <= 8) {
-        const int r = r0 + warp;
-        if (warp >= rows) return;
-        float most = -INFINITY, sum, o[kVec];
-        for (int c = c0; c < end; ++c)
-            if (!none(c)) most = fmaxf(most, *stat(c, r));
-        gather(r, c0, 1, most == -INFINITY ? 0.f : most, sum, o);
-        finish(r, most, sum, o);
-        return;
-    }
-    for (int r = r0; r < r0 + rows; ++r) {
-        float most = -INFINITY, sum, o[kVec];
-        for (int c = c0 + threadIdx.x; c < end; c += 256)
-            if (!none(c)) most = fmaxf(most, *stat(c, r));
-#pragma unroll
-        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        if (lane == 0) part_max[warp] = most;
-        __syncthreads();
-        for (int w = 0; w < 8; ++w) most = fmaxf(most, part_max[w]);
-        gather(r, c0 + warp, 8, most == -INFINITY ? 0.f : most, sum, o);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) part_o[warp][lane + 32 * i] = o[i];
-        if (lane == 0) part_sum[warp] = sum;
-        __syncthreads();
-        if (warp == 0) {
-            sum = 0.f;
-            for (int w = 0; w < 8; ++w) sum += part_sum[w];
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                o[i] = 0.f;
-                for (int w = 0; w < 8; ++w) o[i] += part_o[w][lane + 32 * i];
+            const float *stat = space.stats + slot_of(c) * static_cast<int64_t>(2 * kTcRows) + r;
+            const float w = exp2_fast(stat[0] - ref);
+            sum += w * stat[kTcRows];
+            const float *p = space.sums + (slot_of(c) * static_cast<int64_t>(kTcRows) + r) * D + lane * kVec;
+            if (lane * kVec >= a.d) continue;
+            if constexpr (kVec == 4) {
+                const float4 v = *reinterpret_cast<const float4 *>(p);
+                o[0] += w * v.x;
+                o[1] += w * v.y;
+                o[2] += w * v.z;
+                o[3] += w * v.w;
+            } else {
+                const float2 v = *reinterpret_cast<const float2 *>(p);
+                o[0] += w * v.x;
+                o[1] += w * v.y;
             }
-            finish(r, most, sum, o);
         }
-        __syncthreads();
+        const uint32_t row = rec.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
+        const int qi = static_cast<int>(row / group), head = rec.h * a.group + static_cast<int>(row - qi * group);
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head) + lane * kVec;
+        if (lane * kVec < a.d) {
+#pragma unroll
+            for (int i = 0; i < kVec; i += 2) {
+                if (a.out_vec) {
+                    *reinterpret_cast<uint32_t *>(y + i) = pack2<T>(o[i] * inv, o[i + 1] * inv);
+                } else {
+                    y[i] = from_f32<T>(o[i] * inv);
+                    y[i + 1] = from_f32<T>(o[i + 1] * inv);
+                }
+            }
+        }
+        if (a.lse && lane == 0) a.lse[lse_at(a, q, qi, head)] = sum > 0.f ? kLn2 * most + logf(sum) : -INFINITY;
     }
 }
 
@@ -1002,7 +987,7 @@ cudaError_t launch(AttnArgs a, cudaStream_t st)
     // nothing is shared where every tile is one unit
     if (e != cudaSuccess || blocks < 2 || static_cast<int64_t>(a.width) * a.page_size <= kTcUnit) return e;
     const int64_t rows = (a.offsets ? a.t : a.each) * static_cast<int64_t>(a.group);
-    return launch_pdl(join_tc_kernel<T, D>, dim3(blocks - 1, static_cast<unsigned>(rows < kTcRows ? (rows + 7) / 8 : kTcRows / 8)), 256, 0, st,
+    return launch_pdl(join_tc_kernel<T, D>, dim3(blocks - 1, static_cast<unsigned>(rows < kTcRows ? (rows + 31) / 32 : kTcRows / 32)), 256, 0, st,
                       1, a, blocks);
 }
 
