@@ -888,35 +888,34 @@ __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const in
     const bool sparse = rec.total < blocks;
     auto none = [&](int c) { return sparse && rec.total * (c + 1) / blocks <= rec.total * c / blocks; };
     auto slot_of = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
-#pragma unroll 1
-    for (int r = blockIdx.y * 32 + warp; r < rows && r < static_cast<int>(blockIdx.y) * 32 + 32; r += 8) {
+    const int r0 = blockIdx.y * 32 + warp * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = r0 + i;
+        if (r >= rows) break;
+        // parts in order, with the maximum so far: the loads of the next ones do not wait for it
         float most = -INFINITY, sum = 0.f, o[kVec];
-        for (int c = c0 + lane; c < end; c += 32)
-            if (!none(c)) most = fmaxf(most, space.stats[slot_of(c) * static_cast<int64_t>(2 * kTcRows) + r]);
 #pragma unroll
-        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        const float ref = most == -INFINITY ? 0.f : most;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) o[i] = 0.f;
+        for (int j = 0; j < kVec; ++j) o[j] = 0.f;
 #pragma unroll 4
         for (int c = c0; c < end; ++c) {
             if (none(c)) continue;
             const float *stat = space.stats + slot_of(c) * static_cast<int64_t>(2 * kTcRows) + r;
-            const float w = exp2_fast(stat[0] - ref);
-            sum += w * stat[kTcRows];
             const float *p = space.sums + (slot_of(c) * static_cast<int64_t>(kTcRows) + r) * D + lane * kVec;
-            if (lane * kVec >= a.d) continue;
-            if constexpr (kVec == 4) {
-                const float4 v = *reinterpret_cast<const float4 *>(p);
-                o[0] += w * v.x;
-                o[1] += w * v.y;
-                o[2] += w * v.z;
-                o[3] += w * v.w;
-            } else {
-                const float2 v = *reinterpret_cast<const float2 *>(p);
-                o[0] += w * v.x;
-                o[1] += w * v.y;
+            const float m = stat[0], l = stat[kTcRows];
+            float v[kVec];
+            if (lane * kVec < a.d) {
+                if constexpr (kVec == 4)
+                    *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(p);
+                else
+                    *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(p);
             }
+            const float raised = fmaxf(most, m), ref = raised == -INFINITY ? 0.f : raised;
+            const float f = exp2_fast(most - ref), w = exp2_fast(m - ref);
+            most = raised;
+            sum = sum * f + l * w;
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) o[j] = o[j] * f + v[j] * w;
         }
         const uint32_t row = rec.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
         const int qi = static_cast<int>(row / group), head = rec.h * a.group + static_cast<int>(row - qi * group);
@@ -924,12 +923,12 @@ __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const in
         T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head) + lane * kVec;
         if (lane * kVec < a.d) {
 #pragma unroll
-            for (int i = 0; i < kVec; i += 2) {
+            for (int j = 0; j < kVec; j += 2) {
                 if (a.out_vec) {
-                    *reinterpret_cast<uint32_t *>(y + i) = pack2<T>(o[i] * inv, o[i + 1] * inv);
+                    *reinterpret_cast<uint32_t *>(y + j) = pack2<T>(o[j] * inv, o[j + 1] * inv);
                 } else {
-                    y[i] = from_f32<T>(o[i] * inv);
-                    y[i + 1] = from_f32<T>(o[i + 1] * inv);
+                    y[j] = from_f32<T>(o[j] * inv);
+                    y[j + 1] = from_f32<T>(o[j + 1] * inv);
                 }
             }
         }
