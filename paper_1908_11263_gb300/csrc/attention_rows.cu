@@ -1,6 +1,6 @@
 // Attention of few rows over a cache: keys and values are streamed once, whatever page they lie in.
 //
-// The work is the sequences' keys in units of 64 (128 for heads of 64 and less), for every key head (and every 16 rows, where a sequence has more), one
+// The work is the sequences' keys in units of 64, for every key head (and every 16 rows, where a sequence has more), one
 // after another; every block takes an even share of all units, so short and long sequences mix without idle SMs and one
 // long sequence occupies them all.  Units of one (sequence, key head) that fall to several blocks leave a part each (the
 // sum of 2^(z - m) v, m and the sum of 2^(z - m)) in the workspace, and a second launch joins them in order, so the result
@@ -21,12 +21,12 @@ namespace qnn {
 namespace {
 
 constexpr int kRowsThreads = 128;
-// Keys of a unit: 32 KB of keys and values for every head size up to 128, so that a unit's barriers weigh alike.
-constexpr int rows_unit(int d) { return d <= 64 ? 128 : 64; }
+constexpr int rows_unit(int) { return 64; }
+constexpr int rows_per_sm(int d) { return d <= 64 ? 3 : (d <= 128 ? 2 : 1); }  // blocks: as the registers and shared memory allow
 
 template <int D>
 struct RowsRing {
-    static constexpr int kUnit = rows_unit(D), kStages = 3, kPerSm = D == 256 ? 1 : 2;
+    static constexpr int kUnit = rows_unit(D), kStages = D == 64 ? 4 : 3, kPerSm = rows_per_sm(D);
     static constexpr uint32_t kRow = D * 2, kTile = kUnit * kRow, kQ = 16 * kRow, kStage = 2 * kTile + kQ;
     static constexpr uint32_t kP = kStages * kStage, kPRow = kUnit * 2, kSmem = kP + 16 * kPRow;
 };
@@ -423,11 +423,12 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
 
 // Joins a pair that several blocks share: block (b, row) does where b is the first block whose share begins inside the pair.
 // The block before it, where the pair begins, left its part in its second slot, the others in their first.
+constexpr int kJoinWarps = 8;
 template <typename T, int D>
-__global__ void __launch_bounds__(128) join_rows_kernel(const AttnArgs a, const int blocks)
+__global__ void __launch_bounds__(32 * kJoinWarps) join_rows_kernel(const AttnArgs a, const int blocks)
 {
     constexpr int kVec = D / 32;
-    __shared__ float part_max[4], part_sum[4], part_o[4][D];
+    __shared__ float part_max[kJoinWarps], part_sum[kJoinWarps], part_o[kJoinWarps][D];
     const int b = blockIdx.x + 1, r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_begin();
     const PartSpace space = part_space<D>(a.part, blocks);
@@ -444,19 +445,20 @@ __global__ void __launch_bounds__(128) join_rows_kernel(const AttnArgs a, const 
     auto none = [&](int c) { return sparse && rec.total * (c + 1) / blocks <= rec.total * c / blocks; };
     auto slot_of = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
     float most = -INFINITY;
-    for (int c = c0 + threadIdx.x; c < end; c += 128)
+    for (int c = c0 + threadIdx.x; c < end; c += 32 * kJoinWarps)
         if (!none(c)) most = fmaxf(most, space.stats[slot_of(c) * 32 + r]);
 #pragma unroll
     for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
     if (lane == 0) part_max[warp] = most;
     __syncthreads();
-    most = fmaxf(fmaxf(part_max[0], part_max[1]), fmaxf(part_max[2], part_max[3]));
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) most = fmaxf(most, part_max[w]);
     const float ref = most == -INFINITY ? 0.f : most;
     float sum = 0.f, o[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) o[i] = 0.f;
 #pragma unroll 4
-    for (int c = c0 + warp; c < end; c += 4) {
+    for (int c = c0 + warp; c < end; c += kJoinWarps) {
         if (none(c)) continue;
         const int slot = slot_of(c);
         const float w = exp2_fast(space.stats[slot * 32 + r] - ref);
@@ -469,10 +471,17 @@ __global__ void __launch_bounds__(128) join_rows_kernel(const AttnArgs a, const 
     for (int i = 0; i < kVec; ++i) part_o[warp][lane + 32 * i] = o[i];
     if (lane == 0) part_sum[warp] = sum;
     __syncthreads();
-    sum = part_sum[0] + part_sum[1] + part_sum[2] + part_sum[3];
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) sum += part_sum[w];
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head);
-    for (int c = threadIdx.x; c < a.d; c += 128) y[c] = from_f32<T>((part_o[0][c] + part_o[1][c] + part_o[2][c] + part_o[3][c]) * inv);
+    for (int c = threadIdx.x; c < a.d; c += 32 * kJoinWarps) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kJoinWarps; ++w) v += part_o[w][c];
+        y[c] = from_f32<T>(v * inv);
+    }
     if (a.lse && threadIdx.x == 0) a.lse[lse_at(a, q, qi, head)] = sum > 0.f ? kLn2 * most + logf(sum) : -INFINITY;
 }
 
@@ -490,7 +499,7 @@ cudaError_t launch(const AttnArgs &a, cudaStream_t st)
     // nothing is shared where every pair is one unit
     const int64_t rows = (a.offsets ? a.t : a.each) * static_cast<int64_t>(a.group);
     if (static_cast<int64_t>(a.width) * a.page_size <= R::kUnit) return cudaSuccess;
-    return launch_pdl(join_rows_kernel<T, D>, dim3(blocks - 1, static_cast<unsigned>(rows < 16 ? rows : 16)), 128, 0, st, 1, a, blocks);
+    return launch_pdl(join_rows_kernel<T, D>, dim3(blocks - 1, static_cast<unsigned>(rows < 16 ? rows : 16)), 32 * kJoinWarps, 0, st, 1, a, blocks);
 }
 
 template <typename T>
@@ -505,7 +514,7 @@ cudaError_t launch_d(const AttnArgs &a, cudaStream_t st)
 
 }  // namespace
 
-int attention_rows_blocks(int d) { return device_sm_count() * (padded(d) == 256 ? 1 : 2); }
+int attention_rows_blocks(int d) { return device_sm_count() * rows_per_sm(d); }
 
 size_t attention_rows_workspace(int d)
 {

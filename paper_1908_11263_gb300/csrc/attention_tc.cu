@@ -223,7 +223,7 @@ __device__ __forceinline__ int64_t warp_scan(int64_t v)  // inclusive
 }
 
 // Units (with the tiles' own cost) of the sequences s0 + lane (those below s1) for one key head; all lanes of a warp.
-__device__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
+__device__ __noinline__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
 {
     const int lane = threadIdx.x & 31, s = s0 + lane;
     Sequence q = {0, 0, 0, 0};
@@ -234,6 +234,7 @@ __device__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
     }
     int64_t sum = 0;
     if (tiles <= 4)
+#pragma unroll 1
         for (int rt = 0; rt < tiles; ++rt) sum += tile_keys(a, q, rt).units + kTileCost;
     for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 4); many; many &= many - 1) {
         const int from = __ffs(many) - 1;
@@ -244,6 +245,7 @@ __device__ int64_t sequence_units(const AttnArgs &a, int s0, int s1)
         o.at = __shfl_sync(0xffffffffu, q.at, from);
         const int t = __shfl_sync(0xffffffffu, tiles, from);
         int64_t part = 0;
+#pragma unroll 1
         for (int rt = lane; rt < t; rt += 32) part += tile_keys(a, o, rt).units + kTileCost;
 #pragma unroll
         for (int d = 16; d; d >>= 1) part += __shfl_xor_sync(0xffffffffu, part, d);
@@ -515,14 +517,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     const float raised = fmaxf(m, most), factor = raised == -INFINITY ? 1.f : exp2_fast(m - raised);
                     m = raised;
                     l *= factor;
-                    for (int c = 0; c < D; c += 32) {
-                        float o[32];
-                        if (c >= width) break;
-                        tmem_ld32(o_at_ + c, o);
+#pragma unroll 1
+                    for (int c = 0; c < width; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(o_at_ + c, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] *= factor;
-                        tmem_st32(o_at_ + c, o);
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                        tmem_st16(o_at_ + c, o);
                     }
                 }
                 if (!R::kApart && (warp & 3) == 0 && lane == 0) begun[half] = unit + 1;
@@ -567,45 +569,39 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             T *y = static_cast<T *>(a.out);
             if (r < rows) y += o_at(a, at.q, qi, head);
             float *sums = parts.sums + part_row * D;
-            for (int c = 0; c < D; c += 32) {
-                float o[32];
+#pragma unroll 1
+            for (int c = 0; c < D; c += 16) {  // short code: each tile comes here once
+                uint32_t raw[16];
                 if (c >= a.d) break;
-                tmem_ld32(o_at_ + c, o);
+                __syncwarp();
+                tmem_ld16(o_at_ + c, raw);
                 tmem_wait_ld();
-                if (r < rows) {
-                    if (complete) {
-                        uint32_t w[16];
+                if (r >= rows) continue;
+                if (!complete) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = pack2<T>(o[2 * e] * inv, o[2 * e + 1] * inv);
+                    for (int e = 0; e < 16; e += 4)
+                        *reinterpret_cast<uint4 *>(sums + c + e) = make_uint4(raw[e], raw[e + 1], raw[e + 2], raw[e + 3]);
+                    continue;
+                }
+                uint32_t w[8];
 #pragma unroll
-                        for (int e = 0; e < 16; e += 8) {  // 32 bytes, a whole sector
-                            if (c + 2 * e >= a.d) break;
-                            uint32_t *to = reinterpret_cast<uint32_t *>(y + c) + e;
-                            if (a.out_vec16 && c + 2 * e + 16 <= a.d) {
-                                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[e]), "r"(w[e + 1]),
-                                             "r"(w[e + 2]), "r"(w[e + 3]), "r"(w[e + 4]), "r"(w[e + 5]), "r"(w[e + 6]), "r"(w[e + 7])
-                                             : "memory");
-                            } else {
-                                uint16_t *h = reinterpret_cast<uint16_t *>(to);
+                for (int e = 0; e < 8; ++e) w[e] = pack2<T>(__uint_as_float(raw[2 * e]) * inv, __uint_as_float(raw[2 * e + 1]) * inv);
+                uint32_t *to = reinterpret_cast<uint32_t *>(y + c);
+                if (a.out_vec16 && c + 16 <= a.d) {  // 32 bytes, a whole sector
+                    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                                 : "memory");
+                } else {
+                    uint16_t *h = reinterpret_cast<uint16_t *>(to);
 #pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    if (c + 2 * (e + j) < a.d) {
-                                        if (a.out_vec) {
-                                            to[j] = w[e + j];
-                                        } else {
-                                            h[2 * j] = static_cast<uint16_t>(w[e + j]);
-                                            h[2 * j + 1] = static_cast<uint16_t>(w[e + j] >> 16);
-                                        }
-                                    }
-                            }
+                    for (int j = 0; j < 8; ++j)
+                        if (c + 2 * j < a.d) {
+                            h[2 * j] = static_cast<uint16_t>(w[j]);
+                            h[2 * j + 1] = static_cast<uint16_t>(w[j] >> 16);
                         }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<float4 *>(sums + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                    }
                 }
             }
+            __syncwarp();
             if (r < rows) {
                 if (!complete) {
                     const int64_t base = (2 * blockIdx.x + (seg.whole ? 1 : 0)) * static_cast<int64_t>(2 * kTcRows);
@@ -888,28 +884,24 @@ __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const in
     const bool sparse = rec.total < blocks;
     auto none = [&](int c) { return sparse && rec.total * (c + 1) / blocks <= rec.total * c / blocks; };
     auto slot_of = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
-    const int r0 = blockIdx.y * 32 + warp * 4;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = r0 + i;
-        if (r >= rows) break;
-        // parts in order, with the maximum so far: the loads of the next ones do not wait for it
+    // (Short code: the launch runs it once, and fetching instructions is what takes the time.)
+#pragma unroll 1
+    for (int r = blockIdx.y * 32 + warp; r < rows && r < static_cast<int>(blockIdx.y) * 32 + 32; r += 8) {
         float most = -INFINITY, sum = 0.f, o[kVec];
 #pragma unroll
         for (int j = 0; j < kVec; ++j) o[j] = 0.f;
-#pragma unroll 4
+#pragma unroll 1
         for (int c = c0; c < end; ++c) {
             if (none(c)) continue;
-            const float *stat = space.stats + slot_of(c) * static_cast<int64_t>(2 * kTcRows) + r;
-            const float *p = space.sums + (slot_of(c) * static_cast<int64_t>(kTcRows) + r) * D + lane * kVec;
+            const int64_t at = slot_of(c) * static_cast<int64_t>(kTcRows);
+            const float *stat = space.stats + 2 * at + r;
+            const float *p = space.sums + (at + r) * D + lane * kVec;
             const float m = stat[0], l = stat[kTcRows];
             float v[kVec];
-            if (lane * kVec < a.d) {
-                if constexpr (kVec == 4)
-                    *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(p);
-                else
-                    *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(p);
-            }
+            if constexpr (kVec == 4)
+                *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(p);
+            else
+                *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(p);
             const float raised = fmaxf(most, m), ref = raised == -INFINITY ? 0.f : raised;
             const float f = exp2_fast(most - ref), w = exp2_fast(m - ref);
             most = raised;
