@@ -88,7 +88,9 @@ qnn_status check_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, con
 }
 
 // Rows (queries times the heads that share a key head) of a sequence up to which the streaming kernel takes it, and which
-// kernels a call may need: without offsets all sequences have as many rows, with them the kernels find out.
+// kernels a call may need.  Without offsets all sequences have as many rows.  With them, the tensor cores' kernel takes all
+// sequences where they have more than that on average (a single token among chunks costs it a few units; a second pair of
+// launches took 24 us of 150 for 12 sequences with up to 600 new tokens over 8000), else the kernels share them.
 constexpr int kFewRows = 16;
 struct Kernels {
     bool rows, tc;
@@ -101,9 +103,10 @@ Kernels kernels_of(const qnn_cache_desc &c, const qnn_batch_desc &b, const qnn_a
     if (b.t == 0 || b.seqs == 0) return k;
     const int64_t most = (b.ragged ? b.t : b.t / b.seqs) * (d.heads / c.kv_heads);
     if (c.head_dim <= 128) {
-        k.few = kFewRows;
+        const bool many = b.t * (d.heads / c.kv_heads) > static_cast<int64_t>(kFewRows) * b.seqs;  // on average
+        k.few = b.ragged && many ? 0 : kFewRows;
         k.tc = most > kFewRows;
-        k.rows = b.ragged || !k.tc;
+        k.rows = !k.tc || (b.ragged && !many);
     }
     const int64_t room = static_cast<int64_t>(b.width) * c.page_size;
     if (k.rows && room > 64) k.rows_bytes = (attention_rows_workspace(c.head_dim) + 255) / 256 * 256;

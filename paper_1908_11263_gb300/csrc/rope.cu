@@ -68,13 +68,10 @@ __device__ Place place_of(const RotateArgs &a, int64_t r)
     return p;
 }
 
-// Sixteen rotated elements of a head: the vectors at x0 and x1, and where they go.
+// Sixteen rotated elements of a head, as loaded from two vectors, and where they go.
 template <typename T>
-__device__ __forceinline__ void rotate16(const T *x0, const T *x1, T *y0, T *y1, const float2 *cs, bool interleaved)
+__device__ __forceinline__ void rotate16(Raw8<T> &r0, Raw8<T> &r1, T *y0, T *y1, const float2 *cs, bool interleaved)
 {
-    Raw8<T> r0, r1;
-    r0.load(x0);
-    r1.load(x1);
     float u[8], w[8];
     r0.get(u);
     r1.get(w);
@@ -103,6 +100,54 @@ __device__ __forceinline__ void rotate16(const T *x0, const T *x1, T *y0, T *y1,
     r1.store(y1);
 }
 
+// A thread's way through the items of a block's tokens and heads, kRopeThreads apart.
+struct Walk {
+    int token, head, item;
+    int per, heads, by_token, by_head, by_item;
+
+    __device__ __forceinline__ Walk(int heads_, int per_) : per(per_), heads(heads_)
+    {
+        place(kRopeThreads);
+        by_token = token;
+        by_head = head;
+        by_item = item;
+        place(threadIdx.x);
+    }
+    __device__ __forceinline__ void place(int i)
+    {
+        const int w = i / per;
+        item = i - w * per;
+        token = w / heads;
+        head = w - token * heads;
+    }
+    __device__ __forceinline__ void next()
+    {
+        item += by_item;
+        head += by_head;
+        token += by_token;
+        if (item >= per) {
+            item -= per;
+            ++head;
+        }
+        if (head >= heads) {
+            head -= heads;
+            ++token;
+        }
+    }
+};
+
+// Cosines and sines of a block's tokens, once their places are known.
+__device__ __forceinline__ void angles(const RotateArgs &a, const Place *places, int count, float2 *cs)
+{
+    for (int i = threadIdx.x; i < count * a.half; i += kRopeThreads) {
+        const int token = i / a.half, pair = i - token * a.half;
+        const uint64_t phase = static_cast<uint64_t>(places[token].position) * a.turns[pair];
+        float s, c;
+        sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 0x1p-31f, &s, &c);
+        cs[i] = make_float2(a.amplitude * c, a.amplitude * s);
+    }
+}
+
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RotateArgs a, const int tokens)
 {
@@ -112,77 +157,88 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RotateArgs a, 
     pdl_begin();
     const int64_t first = static_cast<int64_t>(blockIdx.x) * tokens;
     const int count = static_cast<int>(a.t - first < tokens ? a.t - first : tokens);
+    const int heads = a.heads + a.kv_heads, dim = 2 * a.half;  // rotated heads: the queries', then the keys'
     if (tid < count) places[tid] = place_of(a, first + tid);
-    __syncthreads();
-    for (int i = tid; i < count * a.half; i += kRopeThreads) {
-        const int token = i / a.half, pair = i - token * a.half;
-        const uint64_t phase = static_cast<uint64_t>(places[token].position) * a.turns[pair];
-        float s, c;
-        sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 0x1p-31f, &s, &c);
-        cs[i] = make_float2(a.amplitude * c, a.amplitude * s);
-    }
-    __syncthreads();
 
-    // rotated heads: the queries', then the keys'
-    const int heads = a.heads + a.kv_heads, dim = 2 * a.half;
-    const int per = VEC ? a.half / 8 + (a.d - dim) / 8 : a.half + (a.d - dim);  // items of a head
-    const int slots = kRopeThreads / per > 0 ? kRopeThreads / per : 1;
-    const int step = slots == 1 ? kRopeThreads : per;  // items of a head a pass
-    const int slot = slots == 1 ? 0 : tid / per, item0 = slots == 1 ? tid : tid - slot * per;
-    if (slot < slots)
-        for (int w = slot; w < count * heads; w += slots) {
-            const int token = w / heads, head = w - token * heads;
-            const Place p = places[token];
-            const T *x;
-            T *y;
-            if (head < a.heads) {
-                if (!p.live) continue;
-                x = static_cast<const T *>(a.x) + (first + token) * a.ldx + head * a.hx;
-                y = static_cast<T *>(a.y) + (first + token) * a.ldy + head * a.hy;
+    auto source = [&](const Walk &w) {
+        return w.head < a.heads ? static_cast<const T *>(a.x) + (first + w.token) * a.ldx + w.head * a.hx
+                                : static_cast<const T *>(a.k) + (first + w.token) * a.ldk + (w.head - a.heads) * a.hk;
+    };
+    auto target = [&](const Walk &w) -> T * {  // null: not written
+        const Place p = places[w.token];
+        if (w.head < a.heads) return p.live ? static_cast<T *>(a.y) + (first + w.token) * a.ldy + w.head * a.hy : nullptr;
+        return p.k >= 0 ? static_cast<T *>(a.k_pages) + p.k + (w.head - a.heads) * a.k_head : nullptr;
+    };
+    if constexpr (VEC) {
+        // Items of 16 rotated or 8 copied elements, two a thread at a time; the first ones are on their way while the cosines are
+        // computed.
+        const int turned = a.half / 8, apart = a.interleaved ? 8 : a.half;
+        auto begin = [&](int item) { return item < turned ? (a.interleaved ? 16 : 8) * item : dim + 8 * (item - turned); };
+        auto load = [&](const Walk &w, Raw8<T> &r0, Raw8<T> &r1) {
+            if (w.token >= count) return;
+            const T *x = source(w) + begin(w.item);
+            r0.load(x);
+            if (w.item < turned) r1.load(x + apart);
+        };
+        auto finish = [&](const Walk &w, Raw8<T> &r0, Raw8<T> &r1) {
+            if (w.token >= count) return;
+            T *y = target(w);
+            if (!y) return;
+            y += begin(w.item);
+            if (w.item < turned) rotate16<T>(r0, r1, y, y + apart, cs + w.token * a.half + 8 * w.item, a.interleaved);
+            else r0.store(y);
+        };
+        Walk u(heads, turned + (a.d - dim) / 8), v = u;
+        v.next();
+        Raw8<T> u0, u1, v0, v1;
+        load(u, u0, u1);
+        load(v, v0, v1);
+        __syncthreads();
+        angles(a, places, count, cs);
+        __syncthreads();
+        while (u.token < count) {
+            finish(u, u0, u1);
+            finish(v, v0, v1);
+            u.next();
+            u.next();
+            v.next();
+            v.next();
+            load(u, u0, u1);
+            load(v, v0, v1);
+        }
+        if (a.kv_heads > 0)  // values
+            for (Walk w(a.kv_heads, a.d / 8); w.token < count; w.next()) {
+                const Place p = places[w.token];
+                if (p.v < 0) continue;
+                Raw8<T> r;
+                r.load(static_cast<const T *>(a.v) + (first + w.token) * a.ldv + w.head * a.hv + 8 * w.item);
+                r.store(static_cast<T *>(a.v_pages) + p.v + w.head * a.v_head + 8 * w.item);
+            }
+    } else {
+        __syncthreads();
+        angles(a, places, count, cs);
+        __syncthreads();
+        for (Walk w(heads, a.d - a.half); w.token < count; w.next()) {
+            const T *x = source(w);
+            T *y = target(w);
+            if (!y) continue;
+            if (w.item < a.half) {
+                const float2 c = cs[w.token * a.half + w.item];
+                const int at = a.interleaved ? 2 * w.item : w.item, to = a.interleaved ? at + 1 : at + a.half;
+                const float p = to_f32<T>(x[at]), q = to_f32<T>(x[to]);
+                y[at] = from_f32<T>(p * c.x - q * c.y);
+                y[to] = from_f32<T>(p * c.y + q * c.x);
             } else {
-                if (p.k < 0) continue;
-                x = static_cast<const T *>(a.k) + (first + token) * a.ldk + (head - a.heads) * a.hk;
-                y = static_cast<T *>(a.k_pages) + p.k + (head - a.heads) * a.k_head;
-            }
-            const float2 *c = cs + token * a.half;
-            for (int item = item0; item < per; item += step) {
-                if constexpr (VEC) {
-                    if (item < a.half / 8) {
-                        const int at = a.interleaved ? 16 * item : 8 * item, to = a.interleaved ? at + 8 : at + a.half;
-                        rotate16<T>(x + at, x + to, y + at, y + to, c + 8 * item, a.interleaved);
-                    } else {
-                        const int at = dim + 8 * (item - a.half / 8);
-                        Raw8<T> r;
-                        r.load(x + at);
-                        r.store(y + at);
-                    }
-                } else {
-                    if (item < a.half) {
-                        const int at = a.interleaved ? 2 * item : item, to = a.interleaved ? at + 1 : at + a.half;
-                        const float u = to_f32<T>(x[at]), v = to_f32<T>(x[to]);
-                        y[at] = from_f32<T>(u * c[item].x - v * c[item].y);
-                        y[to] = from_f32<T>(u * c[item].y + v * c[item].x);
-                    } else {
-                        y[a.half + item] = x[a.half + item];
-                    }
-                }
+                y[a.half + w.item] = x[a.half + w.item];
             }
         }
-    // values
-    const int vper = VEC ? a.d / 8 : a.d;
-    for (int i = tid; i < count * a.kv_heads * vper; i += kRopeThreads) {
-        const int row = i / vper, at = i - row * vper, token = row / a.kv_heads, head = row - token * a.kv_heads;
-        const Place p = places[token];
-        if (p.v < 0) continue;
-        const T *x = static_cast<const T *>(a.v) + (first + token) * a.ldv + head * a.hv;
-        T *y = static_cast<T *>(a.v_pages) + p.v + head * a.v_head;
-        if constexpr (VEC) {
-            Raw8<T> r;
-            r.load(x + 8 * at);
-            r.store(y + 8 * at);
-        } else {
-            y[at] = x[at];
-        }
+        if (a.kv_heads > 0)
+            for (Walk w(a.kv_heads, a.d); w.token < count; w.next()) {
+                const Place p = places[w.token];
+                if (p.v < 0) continue;
+                static_cast<T *>(a.v_pages)[p.v + w.head * a.v_head + w.item] =
+                    static_cast<const T *>(a.v)[(first + w.token) * a.ldv + w.head * a.hv + w.item];
+            }
     }
 }
 
