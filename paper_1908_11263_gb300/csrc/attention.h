@@ -48,7 +48,7 @@ struct AttnArgs {
     int seqs, width, page_size, each;  // each: queries of every sequence without offsets
     int heads, kv_heads, group, d;
     int causal, window;         // window 0: none
-    int q_vec, out_vec, out_vec16;  // rows of q are 16-byte aligned; rows of out hold aligned pairs; are 32-byte aligned
+    int q_vec, out_vec, out_vec8;  // rows of q are 16-byte aligned; rows of out hold aligned pairs; are 16-byte aligned
     int box, q_box;             // attention_tc: rows that a tiled copy takes of a page, and of q (0: none)
     int few;                    // rows (queries * group) of a sequence up to which it is the streaming kernel's; the rest is attention_tc's
     float scale;                // of q k, times log2(e)

@@ -32,7 +32,11 @@ struct TcRing {
     static constexpr int kStages = D == 64 ? 8 : 5;
     static constexpr uint32_t kHalf = 128 * 128;                // 128 rows of 64 elements
     static constexpr uint32_t kTile = kHalf * (D / 64);         // 128 rows of D
-    static constexpr uint32_t kRing = 2 * kTile, kBars = kRing + kStages * kTile;
+    static constexpr uint32_t kRing = 2 * kTile, kOut = kRing + kStages * kTile;
+    // Room for the output on its way, where it does not cost a stage (a prompt of 8192 tokens, heads of 128: 497 us with four
+    // stages, 461 with five).
+    static constexpr bool kStaged = D == 64;
+    static constexpr uint32_t kBars = kOut + (kStaged ? 2 * kHalf : 0);
     static constexpr uint32_t kSmem = kBars + kLive * 16 + kBins * 8 + 8 * (2 * kStages + 4 + 10 + 2 + kLive) + 16;
     // P beside S where tensor memory has room: the next scores then need not wait until P V has read the weights
     static constexpr bool kApart = D == 64;
@@ -342,7 +346,7 @@ struct TcRecord {
     int s, h, rt, pad;
 };
 struct TcParts {
-    float *sums, *stats;  // [2 * blocks][256][D], [2 * blocks][2][256]: m, then l
+    float *sums, *stats;  // [2 * blocks][D][256], [2 * blocks][2][256]: m, then l
     TcRecord *records;    // [blocks]
 };
 template <int D>
@@ -563,48 +567,72 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             }
             tc_fence_after();
             const bool complete = seg.whole && seg.last;
-            const int64_t part_row = (2 * blockIdx.x + (seg.whole ? 1 : 0)) * static_cast<int64_t>(kTcRows) + r;
+            const int64_t part_slot = 2 * blockIdx.x + (seg.whole ? 1 : 0);
             const float inv = l > 0.f ? 1.f / l : 0.f;
             const int head = at.h * a.group + static_cast<int>(row - qi * group);
-            T *y = static_cast<T *>(a.out);
-            if (r < rows) y += o_at(a, at.q, qi, head);
-            float *sums = parts.sums + part_row * D;
+            const int64_t place = r < rows ? o_at(a, at.q, qi, head) : -1;
+            // Through shared memory where there is room (chunk c of row r at c ^ (r & 7)), so that stores take whole lines: a
+            // thread's own row touches a line for every 32 bytes, and holds up all else that goes to memory.
+            uint8_t *out = smem + R::kOut + half * R::kHalf + (warp & 3) * 32 * 128;
+            float *sums = parts.sums + (part_slot * D) * kTcRows + r;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 16) {  // short code: each tile comes here once
-                uint32_t raw[16];
-                if (c >= a.d) break;
-                __syncwarp();
-                tmem_ld16(o_at_ + c, raw);
-                tmem_wait_ld();
-                if (r >= rows) continue;
-                if (!complete) {
+            for (int c0 = 0; c0 < a.d; c0 += 64) {
+#pragma unroll 1
+                for (int c = c0; c < c0 + 64 && c < a.d; c += 16) {  // short code: each tile comes here once
+                    uint32_t raw[16];
+                    __syncwarp();
+                    tmem_ld16(o_at_ + c, raw);
+                    tmem_wait_ld();
+                    if (!complete) {
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4)
-                        *reinterpret_cast<uint4 *>(sums + c + e) = make_uint4(raw[e], raw[e + 1], raw[e + 2], raw[e + 3]);
-                    continue;
-                }
-                uint32_t w[8];
+                        for (int e = 0; e < 16; ++e) sums[static_cast<int64_t>(c + e) * kTcRows] = __uint_as_float(raw[e]);
+                    } else {
+                        uint32_t w[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = pack2<T>(__uint_as_float(raw[2 * e]) * inv, __uint_as_float(raw[2 * e + 1]) * inv);
-                uint32_t *to = reinterpret_cast<uint32_t *>(y + c);
-                if (a.out_vec16 && c + 16 <= a.d) {  // 32 bytes, a whole sector
-                    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                                 : "memory");
-                } else {
-                    uint16_t *h = reinterpret_cast<uint16_t *>(to);
+                        for (int e = 0; e < 8; ++e) w[e] = pack2<T>(__uint_as_float(raw[2 * e]) * inv, __uint_as_float(raw[2 * e + 1]) * inv);
+                        if constexpr (!R::kStaged) {
+                            T *y = static_cast<T *>(a.out) + place + c;
+                            if (place < 0) continue;
+                            if (a.out_vec8) {
+                                *reinterpret_cast<uint4 *>(y) = make_uint4(w[0], w[1], w[2], w[3]);
+                                if (c + 8 < a.d) *reinterpret_cast<uint4 *>(y + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                            } else {
+                                uint16_t *h = reinterpret_cast<uint16_t *>(y);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (c + 2 * j < a.d) {
-                            h[2 * j] = static_cast<uint16_t>(w[j]);
-                            h[2 * j + 1] = static_cast<uint16_t>(w[j] >> 16);
+                                for (int j = 0; j < 16; ++j)
+                                    if (c + j < a.d) h[j] = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+                            }
+                            continue;
                         }
+                        const int k = (c - c0) / 8;
+                        *reinterpret_cast<uint4 *>(out + lane * 128 + ((k ^ (lane & 7)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(out + lane * 128 + (((k + 1) ^ (lane & 7)) * 16)) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
                 }
+                __syncwarp();
+                if (!complete || !R::kStaged) continue;
+                const int k = lane & 7, col = c0 + 8 * k;
+#pragma unroll 1
+                for (int i = 0; i < 32; i += 4) {
+                    const int rr = i + (lane >> 3);
+                    const int64_t to = __shfl_sync(0xffffffffu, place, rr);
+                    if (to < 0 || col >= a.d) continue;
+                    const uint4 v = *reinterpret_cast<const uint4 *>(out + rr * 128 + ((k ^ (rr & 7)) * 16));
+                    T *y = static_cast<T *>(a.out) + to + col;
+                    if (a.out_vec8) {
+                        *reinterpret_cast<uint4 *>(y) = v;
+                    } else {
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                        uint16_t *h = reinterpret_cast<uint16_t *>(y);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) h[j] = static_cast<uint16_t>(w[j >> 1] >> (16 * (j & 1)));
+                    }
+                }
+                __syncwarp();
             }
-            __syncwarp();
             if (r < rows) {
                 if (!complete) {
-                    const int64_t base = (2 * blockIdx.x + (seg.whole ? 1 : 0)) * static_cast<int64_t>(2 * kTcRows);
+                    const int64_t base = part_slot * (2 * kTcRows);
                     parts.stats[base + r] = m;
                     parts.stats[base + kTcRows + r] = l;
                 } else if (a.lse) {
@@ -865,67 +893,59 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 }
 
 // Joins a tile that several blocks share, as the streaming kernel's parts are: block (b, 32 rows) does where b is the first
-// block whose share begins inside the tile.  A warp a row.
+// block whose share begins inside the tile.  A lane a row, a warp an eighth of the columns.  (Short code: the launch runs it
+// once, and fetching instructions takes most of the time.)
 template <typename T, int D>
 __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const int blocks)
 {
-    constexpr int kVec = D / 32;
-    const int b = blockIdx.x + 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int kCols = D / 8;
+    const int b = blockIdx.x + 1, lane = threadIdx.x & 31, col = (threadIdx.x >> 5) * kCols;
     pdl_begin();
     const TcParts space = tc_parts<D>(a.tc_part, blocks);
     const TcRecord rec = space.records[b];
     const int64_t before = space.records[b - 1].x0;
     if (rec.total == 0 || rec.x0 <= rec.u0 || rec.x0 >= rec.u1 || before > rec.u0) return;
     const Sequence q = sequence(a, rec.s);
-    const int left = q.n * a.group - rec.rt * kTcRows, rows = left < kTcRows ? left : kTcRows;
-    if (blockIdx.y * 32 >= rows) return;
+    const int left = q.n * a.group - rec.rt * kTcRows, rows = left < kTcRows ? left : kTcRows, r = blockIdx.y * 32 + lane;
+    if (r >= rows || col >= a.d) return;
     // parts of blocks c0 .. end - 1; with fewer units than blocks, those between that have a share
     const int c0 = b - 1, end = static_cast<int>((rec.u1 * blocks + rec.total - 1) / rec.total);
     const bool sparse = rec.total < blocks;
-    auto none = [&](int c) { return sparse && rec.total * (c + 1) / blocks <= rec.total * c / blocks; };
-    auto slot_of = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
-    // (Short code: the launch runs it once, and fetching instructions is what takes the time.)
+    float most = -INFINITY, sum = 0.f, o[kCols];
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) o[j] = 0.f;
 #pragma unroll 1
-    for (int r = blockIdx.y * 32 + warp; r < rows && r < static_cast<int>(blockIdx.y) * 32 + 32; r += 8) {
-        float most = -INFINITY, sum = 0.f, o[kVec];
+    for (int c = c0; c < end; ++c) {
+        if (sparse && rec.total * (c + 1) / blocks <= rec.total * c / blocks) continue;
+        const int64_t slot = 2 * c + (c == c0 ? 1 : 0);
+        const float *stat = space.stats + slot * (2 * kTcRows) + r, *p = space.sums + (slot * D + col) * kTcRows + r;
+        float v[kCols];
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) o[j] = 0.f;
-#pragma unroll 1
-        for (int c = c0; c < end; ++c) {
-            if (none(c)) continue;
-            const int64_t at = slot_of(c) * static_cast<int64_t>(kTcRows);
-            const float *stat = space.stats + 2 * at + r;
-            const float *p = space.sums + (at + r) * D + lane * kVec;
-            const float m = stat[0], l = stat[kTcRows];
-            float v[kVec];
-            if constexpr (kVec == 4)
-                *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(p);
-            else
-                *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(p);
-            const float raised = fmaxf(most, m), ref = raised == -INFINITY ? 0.f : raised;
-            const float f = exp2_fast(most - ref), w = exp2_fast(m - ref);
-            most = raised;
-            sum = sum * f + l * w;
+        for (int j = 0; j < kCols; ++j) v[j] = p[j * kTcRows];
+        const float m = stat[0], l = stat[kTcRows];
+        const float raised = fmaxf(most, m), ref = raised == -INFINITY ? 0.f : raised;
+        const float f = exp2_fast(most - ref), w = exp2_fast(m - ref);
+        most = raised;
+        sum = sum * f + l * w;
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) o[j] = o[j] * f + v[j] * w;
-        }
-        const uint32_t row = rec.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
-        const int qi = static_cast<int>(row / group), head = rec.h * a.group + static_cast<int>(row - qi * group);
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head) + lane * kVec;
-        if (lane * kVec < a.d) {
-#pragma unroll
-            for (int j = 0; j < kVec; j += 2) {
-                if (a.out_vec) {
-                    *reinterpret_cast<uint32_t *>(y + j) = pack2<T>(o[j] * inv, o[j + 1] * inv);
-                } else {
-                    y[j] = from_f32<T>(o[j] * inv);
-                    y[j + 1] = from_f32<T>(o[j + 1] * inv);
-                }
-            }
-        }
-        if (a.lse && lane == 0) a.lse[lse_at(a, q, qi, head)] = sum > 0.f ? kLn2 * most + logf(sum) : -INFINITY;
+        for (int j = 0; j < kCols; ++j) o[j] = o[j] * f + v[j] * w;
     }
+    const uint32_t row = rec.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
+    const int qi = static_cast<int>(row / group), head = rec.h * a.group + static_cast<int>(row - qi * group);
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head) + col;
+#pragma unroll
+    for (int j = 0; j < kCols; j += 8) {
+        if (col + j >= a.d) break;
+        if (a.out_vec8) {
+            *reinterpret_cast<uint4 *>(y + j) = make_uint4(pack2<T>(o[j] * inv, o[j + 1] * inv), pack2<T>(o[j + 2] * inv, o[j + 3] * inv),
+                                                           pack2<T>(o[j + 4] * inv, o[j + 5] * inv), pack2<T>(o[j + 6] * inv, o[j + 7] * inv));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[j + i] = from_f32<T>(o[j + i] * inv);
+        }
+    }
+    if (a.lse && col == 0) a.lse[lse_at(a, q, qi, head)] = sum > 0.f ? kLn2 * most + logf(sum) : -INFINITY;
 }
 
 int padded(int d) { return d <= 64 ? 64 : 128; }

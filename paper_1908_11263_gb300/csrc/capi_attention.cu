@@ -255,7 +255,7 @@ qnn_status qnn_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, const
     a.causal = d->causal; a.window = d->window;
     a.q_vec = aligned(q, 16) && d->q_seq % 8 == 0 && d->ldq % 8 == 0 && d->hq % 8 == 0;
     a.out_vec = aligned(out, 4) && d->o_seq % 2 == 0 && d->ldo % 2 == 0 && d->ho % 2 == 0;
-    a.out_vec16 = aligned(out, 32) && d->o_seq % 16 == 0 && d->ldo % 16 == 0 && d->ho % 16 == 0;
+    a.out_vec8 = aligned(out, 16) && d->o_seq % 8 == 0 && d->ldo % 8 == 0 && d->ho % 8 == 0;
     a.few = use.few;
     a.scale = d->scale * 1.4426950408889634f;
     if (use.rows_bytes) a.part = static_cast<float *>(workspace);

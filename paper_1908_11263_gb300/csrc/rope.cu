@@ -149,7 +149,7 @@ __device__ __forceinline__ void angles(const RotateArgs &a, const Place *places,
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RotateArgs a, const int tokens)
+__global__ void __launch_bounds__(kRopeThreads, 6) rope_kernel(const RotateArgs a, const int tokens)
 {
     extern __shared__ float2 cs[];  // [tokens][half]
     __shared__ Place places[kRopeTokens];
@@ -206,14 +206,27 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RotateArgs a, 
             load(u, u0, u1);
             load(v, v0, v1);
         }
-        if (a.kv_heads > 0)  // values
-            for (Walk w(a.kv_heads, a.d / 8); w.token < count; w.next()) {
-                const Place p = places[w.token];
-                if (p.v < 0) continue;
-                Raw8<T> r;
-                r.load(static_cast<const T *>(a.v) + (first + w.token) * a.ldv + w.head * a.hv + 8 * w.item);
-                r.store(static_cast<T *>(a.v_pages) + p.v + w.head * a.v_head + 8 * w.item);
+        if (a.kv_heads > 0) {  // values, two a thread at a time as well
+            auto take = [&](const Walk &w, Raw8<T> &r) {
+                if (w.token < count) r.load(static_cast<const T *>(a.v) + (first + w.token) * a.ldv + w.head * a.hv + 8 * w.item);
+            };
+            auto put = [&](const Walk &w, const Raw8<T> &r) {
+                if (w.token < count && places[w.token].v >= 0)
+                    r.store(static_cast<T *>(a.v_pages) + places[w.token].v + w.head * a.v_head + 8 * w.item);
+            };
+            Walk x(a.kv_heads, a.d / 8), y = x;
+            y.next();
+            while (x.token < count) {
+                take(x, u0);
+                take(y, v0);
+                put(x, u0);
+                put(y, v0);
+                x.next();
+                x.next();
+                y.next();
+                y.next();
             }
+        }
     } else {
         __syncthreads();
         angles(a, places, count, cs);
