@@ -375,6 +375,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     uint64_t *p_full = s_read + 2, *pv_done = p_full + 4, *drained = pv_done + 2, *live_full = drained + 2;  // p_full: [half][64 keys]
     uint32_t *slot = reinterpret_cast<uint32_t *>(live_full + kLive);
     __shared__ Start start;
+    __shared__ TcCursor kept[8];        // the softmax warps' places: in registers they would push scores out
     __shared__ volatile int begun[2];  // units whose weights a half has begun with
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -406,9 +407,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     find_start(a, bins, &start);
     tc_fence_after();
     const uint32_t tmem = *slot;
-    const TcParts parts = tc_parts<D>(a.tc_part, gridDim.x);
     if (threadIdx.x == 0 && a.tc_part) {
-        TcRecord &r = parts.records[blockIdx.x];
+        TcRecord &r = tc_parts<D>(a.tc_part, gridDim.x).records[blockIdx.x];
         r.x0 = start.x0;
         r.u0 = start.u0;
         r.u1 = start.u1;
@@ -439,31 +439,39 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const uint32_t o_at_ = tmem + lanes + R::kOAt + half * D;
         uint32_t s_phase = 0, pv_phase = 0;  // parities of the next waits
         int unit = 0;                        // of the block, for the ring of masks
-        const float2 scale2 = make_float2(a.scale, a.scale);
+        if (lane == 0) kept[warp] = at;
+        __syncwarp();
+        auto go_on = [&](TcCursor &place) {
+            place.next_tile(a);
+            __syncwarp();
+            if (lane == 0) kept[warp] = place;
+            __syncwarp();
+        };
         while (left > 0 && ok) {
-            const int rows = at.rows(a);
-            const Segment seg = take(at, left);
-            if (rows <= half * 128 || seg.count == 0) {  // nothing in this half
-                unit += seg.count;
-                if (!R::kApart && half == 1 && (warp & 3) == 0 && lane == 0) begun[1] = unit;
-                at.next_tile(a);
-                continue;
-            }
-            const int r = half * 128 + (warp & 3) * 32 + lane;
-            const uint32_t row = at.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
-            const int qi = static_cast<int>(row / group);
-            int lo = 0, hi = 0, lo_most, hi_least, x;
-            if (r < rows) keys_of(a, at.q, qi, lo, hi);
+            Segment seg;
+            int first_key, lo = 0, hi = 0, lo_most, hi_least;
             {
+                TcCursor here = kept[warp];
+                const int rows = here.rows(a);
+                seg = take(here, left);
+                if (rows <= half * 128 || seg.count == 0) {  // nothing in this half
+                    unit += seg.count;
+                    if (!R::kApart && half == 1 && (warp & 3) == 0 && lane == 0) begun[1] = unit;
+                    go_on(here);
+                    continue;
+                }
+                first_key = (here.w.first + seg.begin) * kTcUnit;
+                const int r = half * 128 + (warp & 3) * 32 + lane;
+                const uint32_t r0 = here.rt * static_cast<uint32_t>(kTcRows), group = a.group;
+                if (r < rows) keys_of(a, here.q, static_cast<int>((r0 + r) / group), lo, hi);
                 // keys that every row of the half sees: from the last query's first to the first query's last
-                const uint32_t r0 = at.rt * static_cast<uint32_t>(kTcRows) + half * 128;
-                const uint32_t r1 = at.rt * static_cast<uint32_t>(kTcRows) + min(rows, half * 128 + 128) - 1;
-                keys_of(a, at.q, static_cast<int>(r0 / group), x, hi_least);
-                keys_of(a, at.q, static_cast<int>(r1 / group), lo_most, x);
+                int x;
+                keys_of(a, here.q, static_cast<int>((r0 + half * 128) / group), x, hi_least);
+                keys_of(a, here.q, static_cast<int>((r0 + min(rows, half * 128 + 128) - 1) / group), lo_most, x);
             }
             float m = -INFINITY, l = 0.f;
             for (int i = 0; i < seg.count; ++i, ++unit) {
-                const int key0 = (at.w.first + seg.begin + i) * kTcUnit;
+                const int key0 = first_key + i * kTcUnit;
                 if (!wait_bar(live_full + unit % kLive, (unit / kLive) & 1, status) || !wait_bar(s_full + half, s_phase, status)) {
                     ok = false;
                     break;
@@ -533,7 +541,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 }
                 if (!R::kApart && (warp & 3) == 0 && lane == 0) begun[half] = unit + 1;
                 const float ref = m == -INFINITY ? 0.f : -m;
-                const float2 ref2 = make_float2(ref, ref);
+                const float2 ref2 = make_float2(ref, ref), scale2 = make_float2(a.scale, a.scale);
                 float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -569,8 +577,12 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             const bool complete = seg.whole && seg.last;
             const int64_t part_slot = 2 * blockIdx.x + (seg.whole ? 1 : 0);
             const float inv = l > 0.f ? 1.f / l : 0.f;
-            const int head = at.h * a.group + static_cast<int>(row - qi * group);
-            const int64_t place = r < rows ? o_at(a, at.q, qi, head) : -1;
+            TcCursor here = kept[warp];
+            const int rows = here.rows(a), r = half * 128 + (warp & 3) * 32 + lane;
+            const uint32_t row = here.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
+            const int qi = static_cast<int>(row / group), head = here.h * a.group + static_cast<int>(row - qi * group);
+            const int64_t place = r < rows ? o_at(a, here.q, qi, head) : -1;
+            const TcParts parts = tc_parts<D>(a.tc_part, gridDim.x);
             // Through shared memory where there is room (chunk c of row r at c ^ (r & 7)), so that stores take whole lines: a
             // thread's own row touches a line for every 32 bytes, and holds up all else that goes to memory.
             uint8_t *out = smem + R::kOut + half * R::kHalf + (warp & 3) * 32 * 128;
@@ -636,11 +648,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     parts.stats[base + r] = m;
                     parts.stats[base + kTcRows + r] = l;
                 } else if (a.lse) {
-                    a.lse[lse_at(a, at.q, qi, head)] = l > 0.f ? kLn2 * m + logf(l) : -INFINITY;
+                    a.lse[lse_at(a, here.q, qi, head)] = l > 0.f ? kLn2 * m + logf(l) : -INFINITY;
                 }
             }
             tc_fence_before();  // O is read before the next tile's first P, after which it is written again
-            at.next_tile(a);
+            go_on(here);
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
