@@ -624,8 +624,8 @@ typedef struct {
  *
  * The call's t tokens are the sequences' new ones: ragged, sequence s has rows
  * offsets[s] .. offsets[s + 1] (rising; rows before the first and behind the
- * last are in no sequence, and are neither read nor written); else t / seqs
- * rows each.  New token i of n is token lengths[s] - n + i.
+ * last are in no sequence: what they hold does not matter, and none is
+ * written); else t / seqs rows each.  New token i of n is token lengths[s] - n + i.
  *
  * table int32, lengths int32[seqs], offsets int32[seqs + 1]: device.
  */
@@ -665,7 +665,7 @@ typedef struct {
     int32_t heads;             /* of q, a multiple of kv_heads: query head h reads key head h / (heads / kv_heads) */
     int32_t causal;            /* 1: a new token sees the tokens up to itself; 0: all of its sequence */
     int32_t window;            /* > 0: it sees no token `window` or more before itself; 0: no limit */
-    float scale;               /* of the products, > 0 */
+    float scale;               /* of the products: normal, positive, at most FLT_MAX / 2 */
     int64_t q_seq, ldq, hq;    /* strides of q: sequences (not ragged), tokens, heads */
     int64_t o_seq, ldo, ho;    /* of out */
 } qnn_attention_desc;

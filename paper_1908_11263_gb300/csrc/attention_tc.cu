@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kTcThreads = 512, kTcUnit = 128, kTcRows = 256, kLive = 8, kBins = 128;
 constexpr int kTileCost = 2;       // of a tile beside its units, in units: filling the pipeline, output
+constexpr long long kPassedLimit = 64 * kWaitLimitCycles;
 constexpr float kRaise = 8.f;  // growth of the maximum (log2) that is left to the weights
 
 template <int D>
@@ -439,6 +440,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const uint32_t o_at_ = tmem + lanes + R::kOAt + half * D;
         uint32_t s_phase = 0, pv_phase = 0;  // parities of the next waits
         int unit = 0;                        // of the block, for the ring of masks
+        bool passed = false;                 // the half has passed units by, which the other one takes its time for
         if (lane == 0) kept[warp] = at;
         __syncwarp();
         auto go_on = [&](TcCursor &place) {
@@ -456,6 +458,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 seg = take(here, left);
                 if (rows <= half * 128 || seg.count == 0) {  // nothing in this half
                     unit += seg.count;
+                    passed = true;
                     if (!R::kApart && half == 1 && (warp & 3) == 0 && lane == 0) begun[1] = unit;
                     go_on(here);
                     continue;
@@ -472,10 +475,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             float m = -INFINITY, l = 0.f;
             for (int i = 0; i < seg.count; ++i, ++unit) {
                 const int key0 = first_key + i * kTcUnit;
-                if (!wait_bar(live_full + unit % kLive, (unit / kLive) & 1, status) || !wait_bar(s_full + half, s_phase, status)) {
+                // The scores first: the mask of a unit whose scores are there is in its place, and is not replaced before P V has used
+                // the weights.  (A half that has passed tiles by would take an earlier turn of the mask's barrier for its own.)
+                if ((passed ? !mbar_wait_warp(s_full + half, s_phase, status, kPassedLimit) : !wait_bar(s_full + half, s_phase, status)) ||
+                    !wait_bar(live_full + unit % kLive, (unit / kLive) & 1, status)) {
                     ok = false;
                     break;
                 }
+                passed = false;
                 s_phase ^= 1;
                 tc_fence_after();
                 const uint4 there = *reinterpret_cast<const uint4 *>(live + (unit % kLive) * 4);
@@ -605,7 +612,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         if constexpr (!R::kStaged) {
                             T *y = static_cast<T *>(a.out) + place + c;
                             if (place < 0) continue;
-                            if (a.out_vec8) {
+                            if (a.out_vec8 && c + 16 <= a.d && (reinterpret_cast<uintptr_t>(y) & 31) == 0) {  // a whole sector
+                                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(y), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                                             "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                                             : "memory");
+                            } else if (a.out_vec8) {
                                 *reinterpret_cast<uint4 *>(y) = make_uint4(w[0], w[1], w[2], w[3]);
                                 if (c + 8 < a.d) *reinterpret_cast<uint4 *>(y + 8) = make_uint4(w[4], w[5], w[6], w[7]);
                             } else {

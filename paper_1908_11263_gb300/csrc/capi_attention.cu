@@ -1,6 +1,7 @@
 // C ABI of the attention operators (declared in include/qnn.h): argument validation and dispatch.  Every check happens
 // before anything is enqueued; a call that returns an error has launched nothing.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "attention.h"
@@ -77,7 +78,8 @@ qnn_status check_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, con
     if (sb == QNN_EINVAL) return sb;
     if (!a || a->struct_size != sizeof(qnn_attention_desc)) return QNN_EINVAL;
     if (a->heads <= 0 || a->heads % c->kv_heads || !flag_ok(a->causal) || a->window < 0) return QNN_EINVAL;
-    if (!(a->scale > 0.f) || std::isinf(a->scale)) return QNN_EINVAL;
+    // times log2(e) it has to be a normal number
+    if (!(a->scale >= FLT_MIN) || !(a->scale <= FLT_MAX / 2)) return QNN_EINVAL;
     for (const int64_t s : {a->q_seq, a->ldq, a->hq, a->o_seq, a->ldo, a->ho})
         if (!stride_ok(s)) return QNN_EINVAL;
     if (sb != QNN_OK) return sb;

@@ -980,6 +980,12 @@ def _heads(t, dtype, name, shape=None, device=None):
     return t.data_ptr(), [0 if n == 1 else d for n, d in zip(sizes[:-1], strides)]
 
 
+def _fits(*sizes):
+    """Sizes that the library takes as 32-bit numbers."""
+    if max(sizes) >= 1 << 31:
+        raise ValueError(f"sizes must be below 2^31, got {sizes}")
+
+
 def _int32(t, name, shape, device):
     """A contiguous int32 tensor; returns its pointer."""
     if t.device != device:
@@ -1018,6 +1024,7 @@ class Rotary:
             raise ValueError(f"scaling must be one of {sorted(_SCALINGS)}, got {scaling!r}")
         if dim <= 0 or dim % 2:
             raise ValueError(f"dim must be positive and even, got {dim}")
+        _fits(dim, context)
         if not math.isfinite(amplitude):
             raise ValueError(f"amplitude must be finite, got {amplitude}")
         turns = (ctypes.c_uint64 * (dim // 2))()
@@ -1049,6 +1056,7 @@ def rope(x, positions, rotary, *, out=None, stream=None):
     dtype, dev, shape = x.dtype, x.device, x.shape
     px, (ldx, hx) = _heads(x, dtype, "x")
     t, heads, d = shape
+    _fits(heads, d)
     if rotary.device != dev:
         raise ValueError(f"the rotation must be on {dev}")
     if rotary.dim > d:
@@ -1070,7 +1078,7 @@ def _attention(cache, batch, heads, causal, window, scale, table, lengths, offse
     """The call behind PagedCache.attend and cross_attention; qs, os: strides of sequences, tokens and heads."""
     if window is not None and window <= 0:
         raise ValueError(f"window must be positive, got {window}")
-    desc = AttentionDesc(ctypes.sizeof(AttentionDesc), heads, int(bool(causal)), window or 0,
+    desc = AttentionDesc(ctypes.sizeof(AttentionDesc), heads, int(bool(causal)), min(window or 0, (1 << 31) - 1),
                          1.0 / math.sqrt(cache.head_dim) if scale is None else scale, *qs, *os)
     lib, c, b, d = load(), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(desc)
     need = ctypes.c_size_t(0)
@@ -1105,6 +1113,7 @@ class PagedCache:
         self.k, self.v = k, v
         self.dtype, self.device = k.dtype, k.device
         self.pages, self.heads, self.page_size, self.head_dim = k.shape
+        _fits(*k.shape)
         self._k, ks = _heads(k, k.dtype, "k")
         self._v, vs = _heads(v, k.dtype, "v", k.shape, k.device)
         self.desc = CacheDesc(ctypes.sizeof(CacheDesc), _DTYPES[k.dtype], self.heads, self.head_dim, self.page_size, self.pages, *ks, *vs)
@@ -1122,6 +1131,7 @@ class PagedCache:
         if table.dtype is not torch.int32:
             raise TypeError(f"table must have dtype torch.int32, got {table.dtype}")
         seqs, width = table.shape
+        _fits(seqs, width)
         ld, step = table.stride()
         if step != 1 and width > 1:
             raise ValueError("table must have contiguous rows")
@@ -1151,6 +1161,7 @@ class PagedCache:
             if q.dim() != 3:
                 raise ValueError(f"q must have shape [tokens, heads, head_dim], got {tuple(q.shape)}")
             heads = q.shape[1]
+            _fits(heads)
             shape = (tokens, heads, d)
             pq, qs = _heads(q, dtype, "q", shape, dev)
             if q_out is None:
@@ -1189,6 +1200,7 @@ class PagedCache:
             raise ValueError(f"q must have shape [tokens, heads, head_dim], got {tuple(q.shape)}")
         dtype, dev, shape = self.dtype, self.device, q.shape
         tokens, heads, d = shape
+        _fits(heads)
         batch, ptable, plen, poff = self._batch(tokens, table, lengths, offsets)
         if d != self.head_dim or heads % self.heads or heads == 0:
             raise ValueError(f"q must have heads of {self.head_dim} elements, a multiple of {self.heads} of them, got {tuple(shape)}")
@@ -1217,6 +1229,7 @@ def cross_attention(q, k, v, lengths=None, *, scale=None, out=None, lse=False, s
     dtype, dev, shape = q.dtype, q.device, q.shape
     b, n, heads, d = shape
     kb, source, kv, kd = k.shape
+    _fits(b, heads, source, kv)
     if kb != b or kd != d or kv == 0 or heads == 0 or heads % kv:
         raise ValueError(f"q {tuple(shape)} and k {tuple(k.shape)} must agree on the batch and the head's elements, with a multiple "
                          "of k's heads in q")

@@ -172,7 +172,8 @@ def test_attention_shared_refusals(lib, cache, batch, status):
 
 @pytest.mark.parametrize("desc,args,status", [
     (dict(struct_size=4), {}, EINVAL), (dict(heads=0), {}, EINVAL), (dict(heads=7), {}, EINVAL), (dict(causal=2), {}, EINVAL),
-    (dict(window=-1), {}, EINVAL), (dict(scale=0.0), {}, EINVAL), (dict(scale=math.nan), {}, EINVAL), (dict(scale=math.inf), {}, EINVAL),
+    (dict(window=-1), {}, EINVAL), (dict(scale=0.0), {}, EINVAL), (dict(scale=math.nan), {}, EINVAL), (dict(scale=math.inf), {}, EINVAL), (dict(scale=1e-39), {}, EINVAL),
+    (dict(scale=3e38), {}, EINVAL),
     (dict(ldo=511), {}, EINVAL), (dict(ho=0), {}, EINVAL), (dict(ldq=-1), {}, EINVAL), ({}, dict(q=None), EINVAL),
     ({}, dict(out=None), EINVAL), ({}, dict(k=None), EINVAL), ({}, dict(table=None), EINVAL), ({}, dict(offsets=None), EINVAL),
     ({}, dict(k=FAKE + 8), EALIGN), ({}, dict(v=FAKE + 2), EALIGN), ({}, dict(q=FAKE + 1), EALIGN), ({}, dict(out=FAKE + 1), EALIGN),
@@ -304,8 +305,20 @@ def test_argument_checks(new):
         cache.append(new(6, 2, 64), new(6, 2, 64), i32(3, 4), i32(3), positions=i32(6))
 
 
+def test_sizes_past_32_bits_are_refused_not_cut(new):
+    big = (1 << 32) + 4
+    one = lambda *s: new(*(1 for _ in s)).expand(*s)  # noqa: E731
+    for name, kw in (("rope", dict(q=one(6, big, 64))), ("append", dict(q=one(6, big, 64))), ("attend", dict(q=one(6, big, 64))),
+                     ("attend", dict(kp=one(9, 2, big, 64), vp=one(9, 2, big, 64))), ("cross", dict(q=one(3, 5, big, 64))),
+                     ("cross", dict(k=one(3, big, 2, 64), v=one(3, big, 2, 64)))):
+        with pytest.raises(ValueError, match="2.31|contiguous heads"):
+            calls(new, **kw)[name]()
+    with pytest.raises(AssertionError, match="was reached"):
+        calls(new, window=1 << 40)["attend"]()  # no limit
+
+
 @pytest.mark.parametrize("kw,match", [
-    (dict(dim=7), "even"), (dict(dim=0), "even"), (dict(dim=8, scaling="half"), "scaling"), (dict(dim=8, amplitude=math.nan), "amplitude"),
+    (dict(dim=8, context=1 << 32), "2.31"), (dict(dim=7), "even"), (dict(dim=0), "even"), (dict(dim=8, scaling="half"), "scaling"), (dict(dim=8, amplitude=math.nan), "amplitude"),
     (dict(dim=8, frequencies=[1.0]), "frequencies"), (dict(dim=4, frequencies=[1.0, math.inf]), "frequencies")])
 def test_rotary_checks(kw, match):
     with pytest.raises(ValueError, match=match):
