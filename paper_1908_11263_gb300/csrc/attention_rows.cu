@@ -1,6 +1,6 @@
 // Attention of few rows over a cache: keys and values are streamed once, whatever page they lie in.
 //
-// The work is the sequences' keys in units of 64, for every key head (and every 16 rows, where a sequence has more), one
+// The work is the sequences' keys in units of 64 (128 for heads of 64 and less), for every key head (and every 16 rows, where a sequence has more), one
 // after another; every block takes an even share of all units, so short and long sequences mix without idle SMs and one
 // long sequence occupies them all.  Units of one (sequence, key head) that fall to several blocks leave a part each (the
 // sum of 2^(z - m) v, m and the sum of 2^(z - m)) in the workspace, and a second launch joins them in order, so the result
@@ -21,12 +21,15 @@ namespace qnn {
 namespace {
 
 constexpr int kRowsThreads = 128;
-constexpr int rows_unit(int) { return 64; }
-constexpr int rows_per_sm(int d) { return d <= 64 ? 3 : (d <= 128 ? 2 : 1); }  // blocks: as the registers and shared memory allow
+// Keys of a unit: 32 KB of keys and values up to heads of 128, so that a unit's barriers weigh alike.  (Heads of 64, units of
+// 128 keys, two blocks an SM: 57 us for 32 * 20 heads over 1500 keys, one query each; units of 64 and six stages 68, three
+// blocks with four stages 85.)
+constexpr int rows_unit(int d) { return d <= 64 ? 128 : 64; }
+constexpr int rows_per_sm(int d) { return d <= 128 ? 2 : 1; }  // blocks: as registers and shared memory allow
 
 template <int D>
 struct RowsRing {
-    static constexpr int kUnit = rows_unit(D), kStages = D == 64 ? 4 : 3, kPerSm = rows_per_sm(D);
+    static constexpr int kUnit = rows_unit(D), kStages = 3, kPerSm = rows_per_sm(D);
     static constexpr uint32_t kRow = D * 2, kTile = kUnit * kRow, kQ = 16 * kRow, kStage = 2 * kTile + kQ;
     static constexpr uint32_t kP = kStages * kStage, kPRow = kUnit * 2, kSmem = kP + 16 * kPRow;
 };

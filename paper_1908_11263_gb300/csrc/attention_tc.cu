@@ -24,7 +24,9 @@ namespace qnn {
 namespace {
 
 constexpr int kTcThreads = 512, kTcUnit = 128, kTcRows = 256, kLive = 8, kBins = 128;
-constexpr int kTileCost = 2;       // of a tile beside its units, in units: filling the pipeline, output
+// Of a tile beside its units, in units: filling the pipeline, output.  (A prompt of 8192 tokens 681 us with none, 537 with one,
+// 470 with two and with four; 12 chunks over a cache 119, 117, 117 and 122.)
+constexpr int kTileCost = 2;
 constexpr long long kPassedLimit = 64 * kWaitLimitCycles;
 constexpr float kRaise = 8.f;  // growth of the maximum (log2) that is left to the weights
 
@@ -937,9 +939,7 @@ __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const in
     float most = -INFINITY, sum = 0.f, o[kCols];
 #pragma unroll
     for (int j = 0; j < kCols; ++j) o[j] = 0.f;
-#pragma unroll 1
-    for (int c = c0; c < end; ++c) {
-        if (sparse && rec.total * (c + 1) / blocks <= rec.total * c / blocks) continue;
+    auto add = [&](int c) {
         const int64_t slot = 2 * c + (c == c0 ? 1 : 0);
         const float *stat = space.stats + slot * (2 * kTcRows) + r, *p = space.sums + (slot * D + col) * kTcRows + r;
         float v[kCols];
@@ -952,6 +952,20 @@ __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const in
         sum = sum * f + l * w;
 #pragma unroll
         for (int j = 0; j < kCols; ++j) o[j] = o[j] * f + v[j] * w;
+    };
+    if (sparse) {
+#pragma unroll 1
+        for (int c = c0; c < end; ++c)
+            if (rec.total * (c + 1) / blocks > rec.total * c / blocks) add(c);
+    } else {
+        int c = c0;
+#pragma unroll 1
+        for (; c + 4 <= end; c += 4) {  // four at a time: the loads do not wait for one another
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add(c + i);
+        }
+#pragma unroll 1
+        for (; c < end; ++c) add(c);
     }
     const uint32_t row = rec.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
     const int qi = static_cast<int>(row / group), head = rec.h * a.group + static_cast<int>(row - qi * group);

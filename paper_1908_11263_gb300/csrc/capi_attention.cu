@@ -90,10 +90,14 @@ qnn_status check_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, con
 }
 
 // Rows (queries times the heads that share a key head) of a sequence up to which the streaming kernel takes it, and which
-// kernels a call may need.  Without offsets all sequences have as many rows.  With them, the tensor cores' kernel takes all
+// kernels a call may need.  Without offsets all sequences have as many rows, and small calls, which latency bounds, stay with
+// the streaming kernel: those of at most kFewUnits pieces of 16 rows and 64 keys an SM.  Measured on both sides (us, streaming /
+// tensor cores, 8 key heads of 128): 64 sequences of 2048 keys with 16 rows 123 / 129, with 24 rows 198 / 132; 64 of 256 keys
+// with 24 rows (20 pieces an SM) 48 / 50, with 32 rows 52 / 47; one of 8192 keys with 32 rows (13 pieces) 29 / 38, with 64 rows
+// (27) 39 / 38.  With offsets, the tensor cores' kernel takes all
 // sequences where they have more than that on average (a single token among chunks costs it a few units; a second pair of
 // launches took 24 us of 150 for 12 sequences with up to 600 new tokens over 8000), else the kernels share them.
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 16, kFewUnits = 24;
 struct Kernels {
     bool rows, tc;
     int few;
@@ -108,6 +112,12 @@ Kernels kernels_of(const qnn_cache_desc &c, const qnn_batch_desc &b, const qnn_a
         const bool many = b.t * (d.heads / c.kv_heads) > static_cast<int64_t>(kFewRows) * b.seqs;  // on average
         k.few = b.ragged && many ? 0 : kFewRows;
         k.tc = most > kFewRows;
+        if (!b.ragged) {
+            const int64_t room = static_cast<int64_t>(b.width) * c.page_size;
+            const double units = static_cast<double>(b.seqs) * c.kv_heads * ((most + 15) / 16) * ((room + 63) / 64);
+            if (units <= static_cast<double>(kFewUnits) * device_sm_count()) k.tc = false;
+        }
+        if (!k.tc) k.few = 0x7fffffff;
         k.rows = !k.tc || (b.ragged && !many);
     }
     const int64_t room = static_cast<int64_t>(b.width) * c.page_size;

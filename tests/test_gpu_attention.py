@@ -135,7 +135,8 @@ def test_strided_outputs_and_orders():
     for n in (1, 200):
         g = gen(n)
         cache, table, lengths, offsets, q = paged(g, F16, [n, n], [n + 30, n], 4, 2, 64, 16)
-        want = cache.attend(q, table, lengths, offsets)
+        want, even = cache.attend(q, table, lengths, offsets), cache.attend(q, table, lengths)  # may be other kernels
+        check_cache_attention(even, None, q, cache.k, cache.v, table, lengths, offsets)
         for make in (lambda: torch.full((2 * n, 4, 65), 7.0, dtype=F16, device="cuda")[..., :64],
                      lambda: torch.full((4, 2 * n, 72), 7.0, dtype=F16, device="cuda")[..., 1:65].transpose(0, 1),
                      lambda: torch.full((2 * n, 4, 72), 7.0, dtype=F16, device="cuda")[..., :64]):
@@ -144,7 +145,7 @@ def test_strided_outputs_and_orders():
             cache.attend(q, table, lengths, offsets, out=out)
             assert torch.equal(out, want)
             assert int((whole == 7).sum()) >= whole.numel() - out.numel()
-            assert torch.equal(cache.attend(q, table, lengths, out=out), want)
+            assert torch.equal(cache.attend(q, table, lengths, out=out), even)
         other = q.transpose(0, 1).contiguous().transpose(0, 1)
         assert torch.equal(cache.attend(other, table, lengths, offsets), want)
         one = q[:, :1].expand(2 * n, 4, 64)
@@ -189,7 +190,8 @@ def check_cross(q, k, v, lengths, out, lse, scale=None, name=""):
 @pytest.mark.parametrize("dtype", [BF, F16])
 @pytest.mark.parametrize("b,n,src,heads,kv,d", [
     (1, 1, 1, 1, 1, 64), (3, 1, 333, 20, 20, 64), (5, 77, 333, 10, 5, 80), (2, 448, 1500, 4, 4, 64), (4, 129, 257, 8, 2, 128),
-    (2, 16, 63, 6, 6, 96), (3, 300, 64, 2, 1, 256), (2, 1, 5000, 8, 1, 128), (1, 1000, 2, 3, 1, 128), (2, 130, 1000, 8, 8, 40)])
+    (2, 16, 63, 6, 6, 96), (3, 300, 64, 2, 1, 256), (2, 1, 5000, 8, 1, 128), (1, 1000, 2, 3, 1, 128), (2, 130, 1000, 8, 8, 40),
+    (6, 300, 777, 8, 4, 80), (4, 500, 1030, 8, 2, 128), (3, 1000, 600, 20, 5, 40), (20, 40, 513, 16, 4, 64)])
 @pytest.mark.parametrize("packed", [False, True])
 def test_cross(dtype, b, n, src, heads, kv, d, packed):
     g = gen(b * n + src)
@@ -219,3 +221,25 @@ def test_empty_cross():
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())
     assert qnn.cross_attention(q[:0], none[:0], none[:0]).shape == (0, 3, 4, 64)
     assert qnn.cross_attention(q[:, :0], none, none).shape == (2, 0, 4, 64)
+
+
+# ---------------------------------------------------------------- both halves of a tile, and halves without rows
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_tiles_without_rows_in_one_half_before_others(d):
+    """Many sequences whose rows fill one half of a tile (34 to 128), then some that fill both, many times in a block's share:
+    the second half's warps pass the first ones by."""
+    news = [30, 64, 17, 50] * 12 + [300, 33, 40, 600] * 3
+    lengths = [n + 900 * (i % 5) for i, n in enumerate(news)]
+    run(*paged(gen(d), BF, news, lengths, 2, 1, d, 16))
+
+
+def test_windows_inside_a_tile():
+    """Windows shorter than a tile's queries: its first keys are seen by its first rows only."""
+    for window in (1, 5, 127, 128, 129, 400):
+        run(*paged(gen(window), F16, [700, 90], [1500, 90], 2, 2, 64, 32), window=window)
+
+
+@pytest.mark.parametrize("group", [3, 12, 20, 33, 64, 96])
+def test_shared_heads_that_do_not_divide_a_tile(group):
+    run(*paged(gen(group), BF, [37, 1, 90], [500, 300, 90], 2 * group, 2, 64, 16, pad=16))
