@@ -12,9 +12,15 @@
 // quotient), so that O, in tensor memory too, is rarely rescaled.  P is rounded to the element type, off by half a step (2^-8
 // of it for bf16, as the values are); its sum, m and O have 32 bits.
 //
-// Warps: 0-7 softmax and output, a group of four for each half; 8-11 load by cp.async, which takes rows from wherever their
-// pages lie and fills with zeros what the cache does not have (past the length, in no page), whatever lies there; 12 and 13
-// issue the MMAs of a half each.  While the tensor cores work for one half, the other's softmax runs.
+// Warps: 0-7 softmax and output, a group of four for each half; 8-11 load, each 32 keys of a unit, by tiled copies where all
+// of them are there, else by cp.async, which takes rows from wherever their pages lie and fills with zeros what the cache does
+// not have (past the length, in no page), whatever lies there; 12 and 13 issue the MMAs of a half each.  While the tensor
+// cores work for one half, the other's softmax runs.
+//
+// A prompt of 8192 tokens, 32 heads on 8 key heads of 128: 470 us, 1.17 PFLOP/s (0.60 of a large product's).  Bound by what
+// lies between the products: a unit's softmax takes some 2000 cycles beside the other warps' where its instructions alone take
+// 900, a product starts 350 cycles after it is issued, P V and the next scores follow one another (P lies where S does); with
+// heads of 64 by the softmax.  A tile's output holds its half some 5000 cycles (heads of 128: a thread's own row).
 #include <type_traits>
 
 #include "attention.cuh"
