@@ -101,18 +101,18 @@ __device__ __forceinline__ void rotate16(Raw8<T> &r0, Raw8<T> &r1, T *y0, T *y1,
     r1.store(y1);
 }
 
-// A thread's way through the items of a block's tokens and heads, kRopeThreads apart.
+// A thread's way through the items of a block's tokens and heads, from `first` on, `step` apart.
 struct Walk {
     int token, head, item;
     int per, heads, by_token, by_head, by_item;
 
-    __device__ __forceinline__ Walk(int heads_, int per_) : per(per_), heads(heads_)
+    __device__ __forceinline__ Walk(int heads_, int per_, int first, int step) : per(per_), heads(heads_)
     {
-        place(kRopeThreads);
+        place(step);
         by_token = token;
         by_head = head;
         by_item = item;
-        place(threadIdx.x);
+        place(first);
     }
     __device__ __forceinline__ void place(int i)
     {
@@ -150,9 +150,9 @@ __device__ __forceinline__ void angles(const RotateArgs &a, const Place *places,
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kRopeThreads, 6) rope_kernel(const RotateArgs a, const int tokens)
+__global__ void __launch_bounds__(kRopeThreads, 5) rope_kernel(const RotateArgs a, const int tokens)
 {
-    extern __shared__ float2 cs[];  // [tokens][half]
+    extern __shared__ __align__(16) float2 cs[];  // [tokens][half]
     __shared__ Place places[kRopeTokens];
     const int tid = threadIdx.x;
     pdl_begin();
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kRopeThreads, 6) rope_kernel(const RotateArgs 
                                 : static_cast<const T *>(a.k) + (first + w.token) * a.ldk + (w.head - a.heads) * a.hk;
     };
     auto target = [&](const Walk &w) -> T * {  // null: not written
-        const Place p = places[w.token];
+        const Place &p = places[w.token];
         if (w.head < a.heads) return p.live ? static_cast<T *>(a.y) + (first + w.token) * a.ldy + w.head * a.hy : nullptr;
         return p.k >= 0 ? static_cast<T *>(a.k_pages) + p.k + (w.head - a.heads) * a.k_head : nullptr;
     };
@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(kRopeThreads, 6) rope_kernel(const RotateArgs 
             if (w.item < turned) rotate16<T>(r0, r1, y, y + apart, cs + w.token * a.half + 8 * w.item, a.interleaved);
             else r0.store(y);
         };
-        Walk u(heads, turned + (a.d - dim) / 8), v = u;
-        v.next();
+        Walk u(heads, turned + (a.d - dim) / 8, tid, 2 * kRopeThreads), v = u;
+        v.place(tid + kRopeThreads);
         Raw8<T> u0, u1, v0, v1;
         load(u, u0, u1);
         load(v, v0, v1);
@@ -201,8 +201,6 @@ __global__ void __launch_bounds__(kRopeThreads, 6) rope_kernel(const RotateArgs 
             finish(u, u0, u1);
             finish(v, v0, v1);
             u.next();
-            u.next();
-            v.next();
             v.next();
             load(u, u0, u1);
             load(v, v0, v1);
@@ -215,16 +213,14 @@ __global__ void __launch_bounds__(kRopeThreads, 6) rope_kernel(const RotateArgs 
                 if (w.token < count && places[w.token].v >= 0)
                     r.store(static_cast<T *>(a.v_pages) + places[w.token].v + w.head * a.v_head + 8 * w.item);
             };
-            Walk x(a.kv_heads, a.d / 8), y = x;
-            y.next();
+            Walk x(a.kv_heads, a.d / 8, tid, 2 * kRopeThreads), y = x;
+            y.place(tid + kRopeThreads);
             while (x.token < count) {
                 take(x, u0);
                 take(y, v0);
                 put(x, u0);
                 put(y, v0);
                 x.next();
-                x.next();
-                y.next();
                 y.next();
             }
         }
@@ -232,7 +228,7 @@ __global__ void __launch_bounds__(kRopeThreads, 6) rope_kernel(const RotateArgs 
         __syncthreads();
         angles(a, places, count, cs);
         __syncthreads();
-        for (Walk w(heads, a.d - a.half); w.token < count; w.next()) {
+        for (Walk w(heads, a.d - a.half, tid, kRopeThreads); w.token < count; w.next()) {
             const T *x = source(w);
             T *y = target(w);
             if (!y) continue;
@@ -247,7 +243,7 @@ __global__ void __launch_bounds__(kRopeThreads, 6) rope_kernel(const RotateArgs 
             }
         }
         if (a.kv_heads > 0)
-            for (Walk w(a.kv_heads, a.d); w.token < count; w.next()) {
+            for (Walk w(a.kv_heads, a.d, tid, kRopeThreads); w.token < count; w.next()) {
                 const Place p = places[w.token];
                 if (p.v < 0) continue;
                 static_cast<T *>(a.v_pages)[p.v + w.head * a.v_head + w.item] =
