@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
                 const int head = at.h * a.group + row - qi * a.group;
                 const float sum = wsum[0][r] + wsum[1][r] + wsum[2][r] + wsum[3][r];
                 if (complete) {
-                    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
                     T *y = static_cast<T *>(a.out) + o_at(a, at.q, qi, head);
 #pragma unroll
                     for (int n = 0; n < kBlocks; ++n) {
@@ -406,7 +406,7 @@ __global__ void __launch_bounds__(kRowsThreads, RowsRing<D>::kPerSm) attention_r
                         }
                     }
                     if (a.lse && warp == 0 && t4 == 0)
-                        a.lse[lse_at(a, at.q, qi, head)] = sum > 0.f ? kLn2 * m[i] + logf(sum) : -INFINITY;
+                        a.lse[lse_at(a, at.q, qi, head)] = sum == 0.f ? -INFINITY : kLn2 * m[i] + logf(sum);
                 } else {
                     float *y = space.sums + (static_cast<int64_t>(slot) * 16 + r) * D;
 #pragma unroll
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_rows_kernel(const AttnAr
     sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) sum += part_sum[w];
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head);
     for (int c = threadIdx.x; c < a.d; c += 32 * kJoinWarps) {
         float v = 0.f;
@@ -487,7 +487,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_rows_kernel(const AttnAr
         for (int w = 0; w < kJoinWarps; ++w) v += part_o[w][c];
         y[c] = from_f32<T>(v * inv);
     }
-    if (a.lse && threadIdx.x == 0) a.lse[lse_at(a, q, qi, head)] = sum > 0.f ? kLn2 * most + logf(sum) : -INFINITY;
+    if (a.lse && threadIdx.x == 0) a.lse[lse_at(a, q, qi, head)] = sum == 0.f ? -INFINITY : kLn2 * most + logf(sum);
 }
 
 int padded(int d) { return d <= 64 ? 64 : (d <= 128 ? 128 : 256); }

@@ -591,7 +591,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             tc_fence_after();
             const bool complete = seg.whole && seg.last;
             const int64_t part_slot = 2 * blockIdx.x + (seg.whole ? 1 : 0);
-            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
             TcCursor here = kept[warp];
             const int rows = here.rows(a), r = half * 128 + (warp & 3) * 32 + lane;
             const uint32_t row = here.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
@@ -667,7 +667,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     parts.stats[base + r] = m;
                     parts.stats[base + kTcRows + r] = l;
                 } else if (a.lse) {
-                    a.lse[lse_at(a, here.q, qi, head)] = l > 0.f ? kLn2 * m + logf(l) : -INFINITY;
+                    a.lse[lse_at(a, here.q, qi, head)] = l == 0.f ? -INFINITY : kLn2 * m + logf(l);
                 }
             }
             tc_fence_before();  // O is read before the next tile's first P, after which it is written again
@@ -778,13 +778,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                                 const bool there = off >= 0 && chunk * 8 < a.d;
                                 const uint32_t dst = to + r * 128 + (((chunk & 7) ^ (r & 7)) * 16);
                                 if (chunk >= chunks) continue;
-                                if (a.q_vec || !there) {
+                                if (a.q_vec) {
                                     copy16(base + dst, there ? q + off + chunk * 8 : q, there ? 16 : 0);
-                                } else {
-                                    const uint16_t *e = reinterpret_cast<const uint16_t *>(q + off + chunk * 8);
-                                    *reinterpret_cast<uint4 *>(smem + dst) =
-                                        make_uint4(e[0] | static_cast<uint32_t>(e[1]) << 16, e[2] | static_cast<uint32_t>(e[3]) << 16,
-                                                   e[4] | static_cast<uint32_t>(e[5]) << 16, e[6] | static_cast<uint32_t>(e[7]) << 16);
+                                } else {  // zeros are stored as well: the arrival below does not wait for cp.async
+                                    uint32_t w[4] = {0, 0, 0, 0};
+                                    if (there) {
+                                        const uint16_t *e = reinterpret_cast<const uint16_t *>(q + off + chunk * 8);
+#pragma unroll
+                                        for (int k = 0; k < 4; ++k) w[k] = e[2 * k] | static_cast<uint32_t>(e[2 * k + 1]) << 16;
+                                    }
+                                    *reinterpret_cast<uint4 *>(smem + dst) = make_uint4(w[0], w[1], w[2], w[3]);
                                 }
                             }
                             __syncwarp();
@@ -975,7 +978,7 @@ __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const in
     }
     const uint32_t row = rec.rt * static_cast<uint32_t>(kTcRows) + r, group = a.group;
     const int qi = static_cast<int>(row / group), head = rec.h * a.group + static_cast<int>(row - qi * group);
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T *y = static_cast<T *>(a.out) + o_at(a, q, qi, head) + col;
 #pragma unroll
     for (int j = 0; j < kCols; j += 8) {
@@ -988,7 +991,7 @@ __global__ void __launch_bounds__(256) join_tc_kernel(const AttnArgs a, const in
             for (int i = 0; i < 8; ++i) y[j + i] = from_f32<T>(o[j + i] * inv);
         }
     }
-    if (a.lse && col == 0) a.lse[lse_at(a, q, qi, head)] = sum > 0.f ? kLn2 * most + logf(sum) : -INFINITY;
+    if (a.lse && col == 0) a.lse[lse_at(a, q, qi, head)] = sum == 0.f ? -INFINITY : kLn2 * most + logf(sum);
 }
 
 int padded(int d) { return d <= 64 ? 64 : 128; }

@@ -243,3 +243,28 @@ def test_windows_inside_a_tile():
 @pytest.mark.parametrize("group", [3, 12, 20, 33, 64, 96])
 def test_shared_heads_that_do_not_divide_a_tile(group):
     run(*paged(gen(group), BF, [37, 1, 90], [500, 300, 90], 2 * group, 2, 64, 16, pad=16))
+
+
+@pytest.mark.parametrize("d", [8, 24, 40, 72, 104, 120])
+@pytest.mark.parametrize("pad", [0, 6])
+def test_heads_that_end_inside_a_step(d, pad):
+    """Heads of an odd number of eights: the products take sixteen columns at a time, and the columns behind a head are zeros,
+    also where q is not aligned.  Infinities in the rows of other tokens and heads may not reach them."""
+    for dtype in (BF, F16):
+        cache, table, lengths, offsets, q = paged(gen(d + pad), dtype, [300, 21, 130], [400, 90, 1000], 6, 2, d, 16, pad=pad)
+        run(cache, table, lengths, offsets, q)
+        q[310] = math.inf  # one token's queries: its own output has no value, all others have
+        out, lse = cache.attend(q, table, lengths, offsets, lse=True)
+        good = torch.ones(q.shape[0], dtype=torch.bool, device="cuda")
+        good[310] = False
+        assert bool(out[good].isfinite().all()) and bool(lse[good].isfinite().all())
+        assert bool(out[310].isnan().all()) and bool(lse[310].isnan().all())
+
+
+def test_a_token_without_a_value_where_few_rows_are_streamed():
+    cache, table, lengths, offsets, q = paged(gen(3), BF, [1] * 4, [900, 40, 3000, 70], 8, 2, 128, 16)
+    q[2] = math.nan
+    out, lse = cache.attend(q, table, lengths, lse=True)
+    assert bool(out[2].isnan().all()) and bool(lse[2].isnan().all())
+    keep = [0, 1, 3]
+    assert bool(out[keep].isfinite().all()) and bool(lse[keep].isfinite().all())
