@@ -8,8 +8,9 @@
 // A block takes a few tokens: it finds their places in the cache, computes the cosines of a token once for all of its
 // heads (a quarter of a microsecond, against one for each head), then moves rows as 16-byte vectors.  Rows that are not
 // aligned for that go element by element.
-// Bound by HBM latency for prompts (20011 tokens of 20 heads of 96, two thirds rotated: 35 us, 4.4 TB/s, 0.65 of a copy's; more
-// tokens a block or more blocks an SM change it by 5 %) and by the host for a decode step (5 us of 11).
+// Bound by its instructions for prompts (20011 tokens of 20 heads of 96, two thirds rotated: 35 us, 4.4 TB/s, 0.65 of a
+// copy's, issue slots three quarters busy; eight tokens a block 40, two 50 where four take 41) and by the host for a decode step
+// (5 us of 11).
 #include "attention.h"
 #include "block_common.cuh"
 
