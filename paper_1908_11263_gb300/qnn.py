@@ -1014,7 +1014,7 @@ class Rotary:
     `factor` times as long, scaling is "linear" (frequencies divided by the factor), "base" (a larger base) or "ramp"
     (pairs that turn `high` times or more in the original `context` stay as they are, those that turn `low` times or less
     are divided, those between blended); "none" takes no factor.  `amplitude` multiplies the rotated elements.
-    `frequencies` (dim / 2 numbers, radians a position) replaces all of that."""
+    `frequencies` (dim / 2 numbers of either sign, radians a position) replaces all of that."""
 
     __slots__ = ("dim", "interleaved", "amplitude", "turns", "device")
 
@@ -1035,8 +1035,8 @@ class Rotary:
             frequencies = [float(f) for f in frequencies]
             if len(frequencies) != dim // 2 or not all(math.isfinite(f) for f in frequencies):
                 raise ValueError(f"frequencies must be {dim // 2} finite numbers")
-            for i, f in enumerate(frequencies):
-                turns[i] = int(f / math.tau % 1.0 * 2.0 ** 64) % (1 << 64)
+            for i, f in enumerate(frequencies):  # the sign stays with the fraction: 1 less a small one would lose its low bits
+                turns[i] = int(math.ldexp(math.fmod(f / math.tau, 1.0), 64)) % (1 << 64)
         self.dim, self.interleaved, self.amplitude = dim, int(bool(interleaved)), float(amplitude)
         host = torch.frombuffer(bytearray(turns), dtype=torch.int64)
         self.turns = _empty((dim // 2,), torch.int64, torch.device("cuda", _current_device()) if device is None else
