@@ -1202,7 +1202,7 @@ class PagedCache:
         tokens, heads, d = shape
         _fits(heads)
         batch, ptable, plen, poff = self._batch(tokens, table, lengths, offsets)
-        if d != self.head_dim or heads % self.heads or heads == 0:
+        if d != self.head_dim or not self.heads or heads % self.heads or heads == 0:
             raise ValueError(f"q must have heads of {self.head_dim} elements, a multiple of {self.heads} of them, got {tuple(shape)}")
         pq, (ldq, hq) = _heads(q, dtype, "q", None, dev)
         if out is None:
