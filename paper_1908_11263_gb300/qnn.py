@@ -1096,7 +1096,8 @@ def _attention(cache, batch, heads, causal, window, scale, table, lengths, offse
 class PagedCache:
     """Keys and values in pages: k and v [pages, heads, page_size, head_dim], float16 or bfloat16, with contiguous heads and
     any other strides of 16 bytes (a cache kept as [pages, page_size, heads, head_dim] is given as k.transpose(1, 2)).  The
-    tensors are the caller's, and keep what is appended.
+    tensors are the caller's, and keep what is appended.  They stay where they are: a cache that has to grow is a new
+    PagedCache, and calls refuse tensors that were moved (resized, say).
 
     The sequences of a call are a table int32 [seqs, width] of pages (token j in row j % page_size of page table[s, j //
     page_size]; an entry outside [0, pages) is no page: nothing is written there, nothing read), lengths int32 [seqs] with
@@ -1110,7 +1111,7 @@ class PagedCache:
                 raise TypeError(f"{name} must be float16 or bfloat16, got {t.dtype}")
             if t.dim() != 4:
                 raise ValueError(f"{name} must have shape [pages, heads, page_size, head_dim], got {tuple(t.shape)}")
-        self.k, self.v = k, v
+        self._tensors = k, v
         self.dtype, self.device = k.dtype, k.device
         self.pages, self.heads, self.page_size, self.head_dim = k.shape
         _fits(*k.shape)
@@ -1118,12 +1119,23 @@ class PagedCache:
         self._v, vs = _heads(v, k.dtype, "v", k.shape, k.device)
         self.desc = CacheDesc(ctypes.sizeof(CacheDesc), _DTYPES[k.dtype], self.heads, self.head_dim, self.page_size, self.pages, *ks, *vs)
 
+    @property
+    def k(self):
+        return self._tensors[0]
+
+    @property
+    def v(self):
+        return self._tensors[1]
+
     def _batch(self, tokens, table, lengths, offsets):
         dev = self.device
         _on_current(dev, "the cache")
-        if self.k.requires_grad or self.v.requires_grad:
-            _no_gradient(self.k, "k")
-            _no_gradient(self.v, "v")
+        k, v = self._tensors
+        if k.data_ptr() != self._k or v.data_ptr() != self._v:
+            raise ValueError("the cache's tensors have moved since the PagedCache was made")
+        if k.requires_grad or v.requires_grad:
+            _no_gradient(k, "k")
+            _no_gradient(v, "v")
         if table.dim() != 2:
             raise ValueError(f"table must have shape [seqs, width], got {tuple(table.shape)}")
         if table.device != dev:
