@@ -626,6 +626,9 @@ typedef struct {
  * offsets[s] .. offsets[s + 1] (rising; rows before the first and behind the
  * last are in no sequence: what they hold does not matter, and none is
  * written); else t / seqs rows each.  New token i of n is token lengths[s] - n + i.
+ * The host sees t and seqs, not the offsets: rows in no sequence count when a
+ * call's kernels are chosen (for speed alone), and a step of single tokens is
+ * quicker without offsets.
  *
  * table int32, lengths int32[seqs], offsets int32[seqs + 1]: device.
  */
@@ -652,8 +655,8 @@ typedef struct {
  * rotated queries to q_out (which may be q, same strides).  k and v [t][kv_heads][head_dim], q
  * [t][heads][head_dim].  The rotation goes by the token's place in its
  * sequence, or by positions[t] when given.  A token whose place is not in the
- * cache is not written.  Tokens of one call whose places are the same leave
- * the elements of either.
+ * cache is not written.  Tokens of one call whose places are the same, and
+ * keys and values in the same memory, leave the elements of either.
  */
 qnn_status qnn_cache_append(const qnn_cache_desc *c, const qnn_batch_desc *b, const qnn_append_desc *d, const int32_t *table,
                             const int32_t *lengths, const int32_t *offsets, const uint64_t *turns, const void *positions,

@@ -9,7 +9,8 @@
 // m = max, P = 2^(scale S - m), which replaces S in tensor memory as the A operand of O += P V.  Keys and values lie in
 // shared memory as they come, rows of keys: for Q K^T that is K-major, for P V it is MN-major, so nothing is transposed.
 // m is raised only where the maximum has grown by more than 2^8 (the weights stay below 2^8 then, and any m gives the same
-// quotient), so that O, in tensor memory too, is rarely rescaled.  P is rounded to the element type, off by half a step (2^-8
+// quotient), so that O, in tensor memory too, is rarely rescaled: conditional rescaling, a published refinement of the softmax
+// in one pass.  P is rounded to the element type, off by half a step (2^-8
 // of it for bf16, as the values are); its sum, m and O have 32 bits.
 //
 // Warps: 0-7 softmax and output, a group of four for each half; 8-11 load, each 32 keys of a unit, by tiled copies where all
@@ -19,8 +20,10 @@
 //
 // A prompt of 8192 tokens, 32 heads on 8 key heads of 128: 470 us, 1.17 PFLOP/s (0.60 of a large product's).  Bound by what
 // lies between the products: a unit's softmax takes some 2000 cycles beside the other warps' where its instructions alone take
-// 900, a product starts 350 cycles after it is issued, P V and the next scores follow one another (P lies where S does); with
-// heads of 64 by the softmax.  A tile's output holds its half some 5000 cycles (heads of 128: a thread's own row).
+// 900, a product starts 350 cycles after it is issued, P V and the next scores follow one another (P lies where S does).  A
+// tile's output holds its half some 5000 cycles (heads of 128: a thread's own row).  With heads of 64 nothing is busy (16 * 448
+// queries over up to 1500 keys, 16 heads: 65 us, tensor pipe 17 %, exponentials 22 %, issue slots 41 %): a unit takes
+// more than 5000 cycles, and in which of its waits has not been measured.
 #include <type_traits>
 
 #include "attention.cuh"

@@ -92,11 +92,18 @@ qnn_status check_attention(const qnn_cache_desc *c, const qnn_batch_desc *b, con
 // Rows (queries times the heads that share a key head) of a sequence up to which the streaming kernel takes it, and which
 // kernels a call may need.  Without offsets all sequences have as many rows, and small calls, which latency bounds, stay with
 // the streaming kernel: those of at most kFewUnits pieces of 16 rows and 64 keys an SM.  Measured on both sides (us, streaming /
-// tensor cores, 8 key heads of 128): 64 sequences of 2048 keys with 16 rows 123 / 129, with 24 rows 198 / 132; 64 of 256 keys
-// with 24 rows (20 pieces an SM) 48 / 50, with 32 rows 52 / 47; one of 8192 keys with 32 rows (13 pieces) 29 / 38, with 64 rows
-// (27) 39 / 38.  With offsets, the tensor cores' kernel takes all
-// sequences where they have more than that on average (a single token among chunks costs it a few units; a second pair of
-// launches took 24 us of 150 for 12 sequences with up to 600 new tokens over 8000), else the kernels share them.
+// tensor cores, 8 key heads of 128): 64 sequences of 2048 keys with 16 rows 124 / 128, with 24 rows 199 / 130; 64 of 256 keys
+// with 24 or 32 rows (two tiles of 16, 27 pieces an SM) 50 / 46-49; 8 of 1024 with 32 rows (13 pieces) 31 / 33, with 64 rows
+// (27) 46 / 33; one of 8192 with 32 rows (13) 29 / 38, with 64 rows (27) 38 / 38.  The thresholds are those of heads of 128;
+// heads of 64: 64 of 2048 with 16 rows 85 / 100, with 24 rows 132 / 106; 64 of 256 with 24 rows (27) 38 / 44, the slower side;
+// 8 of 1024 with 64 rows 39 / 26.  Pieces are counted over the table's width, which the host knows; lengths and windows that
+// leave most of it out make a call look larger (a window of 256 and 32 rows in a table of 128 K tokens 20 / 23).
+// With offsets the host knows the call's rows only.  The tensor cores' kernel takes all sequences where those are more than
+// kFewRows for each on average (a single token among chunks costs it a few units; a second pair of launches took 24 us of 150
+// for 12 sequences with up to 600 new tokens over 8000), else the kernels share the sequences, and both are queued where one
+// could have more than kFewRows: 64 single tokens, group 4, over 256 or 4096 keys take 45 or 200 us with offsets, 31 or 187
+// without.  Rows in no sequence count as rows: the same tokens over 8192 keys in a call of 1024 rows take 391 us (tensor
+// cores) against 358 in one of 64 (heads of 128), 289 against 237 (heads of 64).
 constexpr int kFewRows = 16, kFewUnits = 24;
 struct Kernels {
     bool rows, tc;

@@ -1102,8 +1102,8 @@ class PagedCache:
     The sequences of a call are a table int32 [seqs, width] of pages (token j in row j % page_size of page table[s, j //
     page_size]; an entry outside [0, pages) is no page: nothing is written there, nothing read), lengths int32 [seqs] with
     the new tokens counted, and offsets int32 [seqs + 1]: sequence s has the rows offsets[s] .. offsets[s + 1] of the call's
-    tensors as its new tokens, the last of them at position lengths[s] - 1.  Without offsets every sequence has as many.
-    Rows in no sequence are left as they were."""
+    tensors as its new tokens, the last of them at position lengths[s] - 1.  Without offsets every sequence has as many, and a
+    step of single tokens is quicker.  Rows in no sequence are left as they were."""
 
     def __init__(self, k, v):
         for t, name in ((k, "k"), (v, "v")):
@@ -1207,7 +1207,7 @@ class PagedCache:
         sequence or many, each seeing the tokens up to itself (causal), of these the last `window` if one is given.  Heads
         are a multiple of the cache's, which neighbouring heads share.  scale: 1 / sqrt(head_dim) by default.  Returns out
         [tokens, heads, head_dim], zero for a token that sees none, or with lse=True (out, float32 [tokens, heads]): the
-        logarithm of the sum of exponentials."""
+        logarithm of the sum of exponentials.  An out of the caller's overlaps no other tensor of the call."""
         if q.dim() != 3:
             raise ValueError(f"q must have shape [tokens, heads, head_dim], got {tuple(q.shape)}")
         dtype, dev, shape = self.dtype, self.device, q.shape
@@ -1232,7 +1232,7 @@ def cross_attention(q, k, v, lengths=None, *, scale=None, out=None, lse=False, s
     """Attention of q [batch, tokens, heads, head_dim] to the states of an encoder (qnn_attention): k, v [batch, source,
     key heads, head_dim], float16 or bfloat16, of which lengths int32 [batch] (None: all) count; heads are a multiple of the
     key heads.  All but the heads may be strided, keys and values by 16 bytes.  Returns out like q, zero where there are no
-    keys, or with lse=True (out, float32 [batch, tokens, heads])."""
+    keys, or with lse=True (out, float32 [batch, tokens, heads]).  An out of the caller's overlaps no other tensor."""
     if q.dtype not in (torch.float16, torch.bfloat16):
         raise TypeError(f"q must be float16 or bfloat16, got {q.dtype}")
     for t, name in ((q, "q"), (k, "k"), (v, "v")):
